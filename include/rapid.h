@@ -18,6 +18,10 @@
  * (cache bookkeeping of a validation round), rapid_retrieve (the RAG drafter's
  * chunk selection, Sec. 2.2) and rapid_hbm_read_probe (a measurement aid).
  *
+ * Two ways to read less of the cache: a cache in 8 bits (rapid_kv_append_quant,
+ * rapid_verify_attn_quant, rapid_kv_read_quant), and one copy of a prefix that the
+ * sequences of a batch share (rapid_verify_attn_prefix).
+ *
  * Conventions
  *   - Every data pointer is a DEVICE pointer unless it says "host".  The caller
  *     owns all buffers; the library allocates no device memory, keeps no
@@ -375,6 +379,89 @@ int rapid_kv_commit(rapid_ctx* ctx, int batch, int gamma, const int32_t* gammas,
 int rapid_kv_commit_pages(rapid_ctx* ctx, const rapid_attn_shape* shape, const int32_t* gammas,
                           const int32_t* n_accepted, const int32_t* page_table, int32_t* ctx_lens,
                           int32_t* released_pages, int release_cap, int32_t* n_released, void* stream);
+
+/*
+ * A KV cache in 8 bits.  For each token and kv head, K and V each hold head_dim e4m3 codes (one byte each) and one scale
+ * byte E, which stands for 2^(E - 127); the value of element c is code[c] * 2^(E - 127).  A row x of bf16 values is written with
+ *     E - 127 = the smallest integer k in [-100, 119] with max |x_c| <= 448 * 2^k   (over the finite x_c; -100 if there is none)
+ *     code[c] = x_c * 2^-k, clamped to [-448, 448] and rounded to e4m3 (nearest, ties to even);  NaN where x_c is NaN or infinite
+ * Scales are powers of two, so that x_c * 2^-k has no rounding of its own, the stored value is a bf16 number, and rows read back and written again
+ * keep their values.  Where the row's largest lies between 2^-91 and 448 * 2^119, elements within 2^13 of it are at most 2^-4 of themselves off,
+ * smaller ones 2^-17 of the largest.
+ *
+ * The codes are addressed as rapid_attn_shape says, its strides in elements, here bytes: multiples of 16.
+ * The scale byte of (b, token j, kv head h) lies at
+ *   contiguous:  b*scale_batch_stride + h*scale_head_stride + j
+ *   paged:       page_table[b][j / page_size]*scale_page_stride + h*scale_head_stride + j % page_size
+ * Scales of consecutive tokens are consecutive bytes; strides are multiples of 16, and the rows are readable to their end: max_ctx
+ * rounded up to a multiple of 16 (contiguous).  K and V use the same strides.  The natural layouts are [B, Hkv, max_ctx] and [n_pages, Hkv, page_size].
+ */
+typedef struct rapid_quant_layout {
+    int64_t scale_batch_stride;
+    int64_t scale_head_stride;
+    int64_t scale_page_stride;
+} rapid_quant_layout;
+
+/*
+ * rapid_kv_append_quant: rapid_kv_append into a cache in 8 bits.  Row i (0 <= i <= gamma_b) of k_new / v_new is quantised and
+ * becomes token ctx_lens[b] - (gamma_b+1) + i; other tokens' codes and scales are left untouched, and rows whose token would be
+ * negative are not written.  q_max may be anything up to max_ctx: a whole prompt is written by one call (gammas[b] = its length - 1).
+ *   k_new, v_new        bf16 [B, Qmax, Hkv, d], contiguous, 16-byte aligned
+ *   k_codes, v_codes    written in place, 16-byte aligned;  k_scales, v_scales  likewise
+ *   n_q_heads (a multiple of n_kv_heads) and softmax_scale are not used
+ *
+ * rapid_kv_read_quant: the same rows read back: row i of k_out / v_out (bf16 [B, Qmax, Hkv, d], contiguous, 16-byte aligned) is the
+ * value of token ctx_lens[b] - (gamma_b+1) + i, exactly (what is below the smallest normal bf16 number cannot occur).  Rows i > gamma_b, and
+ * rows whose token would be negative, are written as zeros.
+ *
+ * rapid_verify_attn_quant: rapid_verify_attn on such a cache: same operation, same arguments, same rules for lengths, drafts, rows that do not
+ * exist and lse_out, computed on the stored values with fp32 accumulation; weights are rounded to bf16 before the second product.  A NaN
+ * in a token's K or V reaches the rows that attend this token and no others.
+ *   chunk_tokens and ctx_sum_hint are not used: the kernel divides the tokens of the batch by itself
+ *   workspace   >= rapid_verify_attn_quant_workspace_bytes(), 256-byte aligned, any content
+ */
+int rapid_kv_append_quant(rapid_ctx* ctx, const rapid_attn_shape* shape, const rapid_quant_layout* layout,
+                          const void* k_new, const void* v_new,
+                          const int32_t* ctx_lens, const int32_t* gammas, const int32_t* page_table,
+                          void* k_codes, void* v_codes, void* k_scales, void* v_scales, void* stream);
+int rapid_kv_read_quant(rapid_ctx* ctx, const rapid_attn_shape* shape, const rapid_quant_layout* layout,
+                        const void* k_codes, const void* v_codes, const void* k_scales, const void* v_scales,
+                        const int32_t* ctx_lens, const int32_t* gammas, const int32_t* page_table,
+                        void* k_out, void* v_out, void* stream);
+size_t rapid_verify_attn_quant_workspace_bytes(const rapid_ctx* ctx, const rapid_attn_shape* shape);   /* 0 on a bad shape */
+int rapid_verify_attn_quant(rapid_ctx* ctx, const rapid_attn_shape* shape, const rapid_quant_layout* layout, const void* q,
+                            const void* k_codes, const void* v_codes, const void* k_scales, const void* v_scales,
+                            const int32_t* ctx_lens, const int32_t* gammas, const int32_t* page_table,
+                            void* out, float* lse_out, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Verification attention of a batch whose sequences share one prefix (several requests, or several drafts, about one long
+ * context): the prefix is kept once and read once for all of the batch's rows.  With P = prefix_len[0] and the rest as for rapid_verify_attn,
+ * sequence b's own tokens follow the prefix, ctx_lens[b] counts them alone, and row i of head h attends the prefix and its own keys 0 .. L-Q+i:
+ *     out[b,i,h,:] = softmax over (prefix keys, own keys) . (their values);  lse_out likewise over both
+ * Rows i >= Q, and all rows of a sequence with ctx_lens[b] = 0, are written as zeros, their lse_out as 0 and as -infinity.  A NaN or infinity in
+ * a token's K or V reaches the rows that attend this token and no others.
+ *   prefix_len    int32 [1], device data, 0 <= prefix_len[0] <= max_prefix (clamped to that range)
+ *   k_prefix, v_prefix   bf16, 16-byte aligned, element (token j, kv head h, c) at j*token_stride + h*head_stride + c (in elements, multiples
+ *                 of 8); NULL where prefix_table is given, or where max_prefix is 0
+ *   prefix_table  int32 [prefix->max_pages] or NULL; with it the prefix lies in pages of k_cache / v_cache (page_size > 0), addressed like the sequences'
+ *                 own (its strides above are not used), and ids are clamped in the same way
+ *   k_cache, v_cache, ctx_lens, gammas, page_table, out, lse_out   as for rapid_verify_attn (chunk_tokens and ctx_sum_hint are not used)
+ *   workspace     >= rapid_verify_attn_prefix_workspace_bytes(), 256-byte aligned, any content
+ */
+typedef struct rapid_prefix_layout {
+    int32_t max_prefix;       /* upper bound of prefix_len[0], >= 0; sizes the grid and the workspace */
+    int32_t max_pages;        /* length of prefix_table                                             */
+    int64_t token_stride;
+    int64_t head_stride;
+} rapid_prefix_layout;
+size_t rapid_verify_attn_prefix_workspace_bytes(const rapid_ctx* ctx, const rapid_attn_shape* shape,
+                                                const rapid_prefix_layout* prefix);                    /* 0 on a bad shape */
+int rapid_verify_attn_prefix(rapid_ctx* ctx, const rapid_attn_shape* shape, const rapid_prefix_layout* prefix, const void* q,
+                             const void* k_prefix, const void* v_prefix, const int32_t* prefix_len, const int32_t* prefix_table,
+                             const void* k_cache, const void* v_cache,
+                             const int32_t* ctx_lens, const int32_t* gammas, const int32_t* page_table,
+                             void* out, float* lse_out, void* workspace, size_t workspace_bytes, void* stream);
 
 /*
  * Chunk selection of the RAG drafter (Sec. 2.2; "RAG Setup" in Sec. 3): the long context is

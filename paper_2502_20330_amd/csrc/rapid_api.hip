@@ -230,6 +230,100 @@ size_t plan_exchange(const rapid_ctx* ctx, const AttnLaunch& a)
     return attn_exchange_bytes(a.B, a.Hkv, a.nsplit, a.RB, a.D);
 }
 
+// ---- the cache in 8 bits, the shared prefix
+int page_shift_of(const rapid_attn_shape* s)
+{
+    int sh = 0;
+    while ((1 << sh) < s->page_size) ++sh;
+    return s->page_size ? sh : -1;
+}
+
+// Shapes of the calls on a cache in 8 bits; strides are bytes.  `attn`: the packed rows of an attention call.
+int check_quant_shape(const rapid_attn_shape* s, bool attn)
+{
+    if (!s) return RAPID_EINVAL;
+    if (s->batch < 1 || s->q_max < 1 || s->n_q_heads < 1 || s->n_kv_heads < 1 || s->max_ctx < 1) return RAPID_EINVAL;
+    if (s->n_q_heads % s->n_kv_heads) return RAPID_EINVAL;
+    if (s->gamma < 0 || s->gamma >= s->q_max || s->max_ctx < s->q_max) return RAPID_EINVAL;
+    if (attn && !(s->softmax_scale > 0.f)) return RAPID_EINVAL;
+    if (s->chunk_tokens < 0 || s->ctx_sum_hint < 0 || s->n_pages < 0) return RAPID_EINVAL;
+    if (s->head_dim != 64 && s->head_dim != 128) return RAPID_EUNSUPPORTED;
+    if (s->batch > 32767 || s->n_kv_heads > 65535) return RAPID_EUNSUPPORTED;          // grid dimensions
+    if (attn && (int64_t)s->q_max * (s->n_q_heads / s->n_kv_heads) > 96) return RAPID_EUNSUPPORTED;
+    if (attn && (int64_t)s->batch * s->q_max * s->n_q_heads * s->head_dim * 2 >= (int64_t)1 << 32) return RAPID_EUNSUPPORTED;
+    if (s->page_size != 0) {
+        if (s->page_size < 16 || (s->page_size & (s->page_size - 1))) return RAPID_EUNSUPPORTED;
+        if (s->max_pages < 1 || (int64_t)s->max_pages * s->page_size < s->max_ctx) return RAPID_EINVAL;
+        if (s->kv_page_stride % 16) return RAPID_EALIGN;
+    } else if (s->kv_batch_stride % 16) {
+        return RAPID_EALIGN;
+    }
+    if (s->kv_token_stride < s->head_dim || s->kv_token_stride % 16 || s->kv_head_stride % 16) return RAPID_EALIGN;
+    // rows of one (sequence or page, head) are addressed with 32-bit byte offsets
+    const int64_t span_tokens = s->page_size ? s->page_size : s->max_ctx;
+    if (s->kv_token_stride * span_tokens >= (int64_t)1 << 32) return RAPID_EUNSUPPORTED;
+    return RAPID_OK;
+}
+int check_quant_layout(const rapid_attn_shape* s, const rapid_quant_layout* l)
+{
+    if (!l) return RAPID_EINVAL;
+    if (l->scale_head_stride % 16 || (s->page_size ? l->scale_page_stride : l->scale_batch_stride) % 16) return RAPID_EALIGN;
+    return RAPID_OK;
+}
+
+AttnSource source_of(const rapid_attn_shape* s, const void* k, const void* v, const int32_t* page_table)
+{
+    AttnSource r{};
+    r.k = k;
+    r.v = v;
+    r.page_table = s->page_size ? page_table : nullptr;
+    r.bstride = s->kv_batch_stride;
+    r.tstride = s->kv_token_stride;
+    r.hstride = s->kv_head_stride;
+    r.pstride = s->kv_page_stride;
+    r.page_shift = page_shift_of(s);
+    r.page_mask = s->page_size ? s->page_size - 1 : 0;
+    r.max_pages = s->max_pages;
+    r.page_hi = page_hi_of(s);
+    return r;
+}
+
+int check_prefix_shape(const rapid_attn_shape* s, const rapid_prefix_layout* p)
+{
+    const int rc = check_attn_shape(s);
+    if (rc != RAPID_OK) return rc;
+    if (!p || p->max_prefix < 0 || p->max_pages < 0) return RAPID_EINVAL;
+    return RAPID_OK;
+}
+// How the prefix lies: in pages of the sequences' pool, or by strides of its own.
+int check_prefix_place(const rapid_attn_shape* s, const rapid_prefix_layout* p, bool paged)
+{
+    if (paged) return s->page_size != 0 && (int64_t)p->max_pages * s->page_size >= p->max_prefix ? RAPID_OK : RAPID_EINVAL;
+    if (p->token_stride < s->head_dim || p->token_stride % 8 || p->head_stride % 8) return RAPID_EALIGN;
+    return p->token_stride * 2 * p->max_prefix < (int64_t)1 << 32 ? RAPID_OK : RAPID_EUNSUPPORTED;
+}
+
+AttnRowsLaunch rows_launch(const rapid_attn_shape* s, const void* q, const int32_t* ctx_lens, const int32_t* gammas, void* out,
+                           float* lse_out)
+{
+    AttnRowsLaunch a{};
+    a.q = static_cast<const uint16_t*>(q);
+    a.out = static_cast<uint16_t*>(out);
+    a.lse_out = lse_out;
+    a.ctx_lens = ctx_lens;
+    a.gammas = gammas;
+    a.B = s->batch;
+    a.Qmax = s->q_max;
+    a.Hq = s->n_q_heads;
+    a.Hkv = s->n_kv_heads;
+    a.G = a.Hq / a.Hkv;
+    a.D = s->head_dim;
+    a.gamma = s->gamma;
+    a.max_ctx = s->max_ctx;
+    a.scale_log2e = s->softmax_scale * 1.4426950408889634f;
+    return a;
+}
+
 }  // namespace
 
 extern "C" {
@@ -667,6 +761,150 @@ int rapid_kv_commit_pages(rapid_ctx* ctx, const rapid_attn_shape* shape, const i
     DeviceScope dev(ctx->device);
     if (dev.err != hipSuccess) return hip_fail(ctx, dev.err);
     hipError_t e = launch_kv_commit_pages(a, static_cast<hipStream_t>(stream));
+    if (e != hipSuccess) return hip_fail(ctx, e);
+    return RAPID_OK;
+}
+
+static int quant_rows_call(rapid_ctx* ctx, const rapid_attn_shape* shape, const rapid_quant_layout* layout, bool append,
+                           const void* k_rows, const void* v_rows, const void* k_codes, const void* v_codes,
+                           const void* k_scales, const void* v_scales,
+                           const int32_t* ctx_lens, const int32_t* gammas, const int32_t* page_table, void* stream)
+{
+    if (!ctx) return RAPID_EINVAL;
+    int rc = check_quant_shape(shape, false);
+    if (rc == RAPID_OK) rc = check_quant_layout(shape, layout);
+    if (rc != RAPID_OK) return rc;
+    if (!k_rows || !v_rows || !k_codes || !v_codes || !k_scales || !v_scales || !ctx_lens) return RAPID_EINVAL;
+    if (shape->page_size != 0 && !page_table) return RAPID_EINVAL;
+    if (!aligned(k_rows, 16) || !aligned(v_rows, 16) || !aligned(k_codes, 16) || !aligned(v_codes, 16) || !aligned(k_scales, 16) ||
+        !aligned(v_scales, 16)) return RAPID_EALIGN;
+    KvQuantLaunch a{};
+    // one struct for both directions: each kernel only reads its inputs
+    auto side = [](const void* rows, const void* codes, const void* scales) {
+        return KvQuantSide{static_cast<uint16_t*>(const_cast<void*>(rows)), static_cast<uint8_t*>(const_cast<void*>(codes)),
+                           static_cast<uint8_t*>(const_cast<void*>(scales))};
+    };
+    a.side[0] = side(k_rows, k_codes, k_scales);
+    a.side[1] = side(v_rows, v_codes, v_scales);
+    a.ctx_lens = ctx_lens;
+    a.gammas = gammas;
+    a.page_table = shape->page_size ? page_table : nullptr;
+    a.B = shape->batch;
+    a.Qmax = shape->q_max;
+    a.Hkv = shape->n_kv_heads;
+    a.D = shape->head_dim;
+    a.gamma = shape->gamma;
+    a.max_ctx = shape->max_ctx;
+    a.bstride = shape->kv_batch_stride;
+    a.tstride = shape->kv_token_stride;
+    a.hstride = shape->kv_head_stride;
+    a.pstride = shape->kv_page_stride;
+    a.sbstride = layout->scale_batch_stride;
+    a.shstride = layout->scale_head_stride;
+    a.spstride = layout->scale_page_stride;
+    a.page_shift = page_shift_of(shape);
+    a.page_mask = shape->page_size ? shape->page_size - 1 : 0;
+    a.max_pages = shape->max_pages;
+    a.page_hi = page_hi_of(shape);
+    DeviceScope dev(ctx->device);
+    if (dev.err != hipSuccess) return hip_fail(ctx, dev.err);
+    hipError_t e = append ? launch_kv_append_quant(a, static_cast<hipStream_t>(stream))
+                          : launch_kv_read_quant(a, static_cast<hipStream_t>(stream));
+    if (e != hipSuccess) return hip_fail(ctx, e);
+    return RAPID_OK;
+}
+
+int rapid_kv_append_quant(rapid_ctx* ctx, const rapid_attn_shape* shape, const rapid_quant_layout* layout,
+                          const void* k_new, const void* v_new,
+                          const int32_t* ctx_lens, const int32_t* gammas, const int32_t* page_table,
+                          void* k_codes, void* v_codes, void* k_scales, void* v_scales, void* stream)
+{
+    return quant_rows_call(ctx, shape, layout, true, k_new, v_new, k_codes, v_codes, k_scales, v_scales, ctx_lens, gammas, page_table,
+                           stream);
+}
+
+int rapid_kv_read_quant(rapid_ctx* ctx, const rapid_attn_shape* shape, const rapid_quant_layout* layout,
+                        const void* k_codes, const void* v_codes, const void* k_scales, const void* v_scales,
+                        const int32_t* ctx_lens, const int32_t* gammas, const int32_t* page_table,
+                        void* k_out, void* v_out, void* stream)
+{
+    return quant_rows_call(ctx, shape, layout, false, k_out, v_out, k_codes, v_codes, k_scales, v_scales, ctx_lens, gammas, page_table,
+                           stream);
+}
+
+size_t rapid_verify_attn_quant_workspace_bytes(const rapid_ctx*, const rapid_attn_shape* shape)
+{
+    return check_quant_shape(shape, true) == RAPID_OK ? 256 : 0;
+}
+
+int rapid_verify_attn_quant(rapid_ctx* ctx, const rapid_attn_shape* shape, const rapid_quant_layout* layout, const void* q,
+                            const void* k_codes, const void* v_codes, const void* k_scales, const void* v_scales,
+                            const int32_t* ctx_lens, const int32_t* gammas, const int32_t* page_table,
+                            void* out, float* lse_out, void* workspace, size_t workspace_bytes, void* stream)
+{
+    if (!ctx) return RAPID_EINVAL;
+    int rc = check_quant_shape(shape, true);
+    if (rc == RAPID_OK) rc = check_quant_layout(shape, layout);
+    if (rc != RAPID_OK) return rc;
+    if (!q || !k_codes || !v_codes || !k_scales || !v_scales || !ctx_lens || !out) return RAPID_EINVAL;
+    if (shape->page_size != 0 && !page_table) return RAPID_EINVAL;
+    if (!aligned(q, 16) || !aligned(k_codes, 16) || !aligned(v_codes, 16) || !aligned(k_scales, 16) || !aligned(v_scales, 16) ||
+        !aligned(out, 16)) return RAPID_EALIGN;
+    if (!workspace || !aligned(workspace, 256) || workspace_bytes < rapid_verify_attn_quant_workspace_bytes(ctx, shape))
+        return RAPID_EWORKSPACE;
+    AttnRowsLaunch a = rows_launch(shape, q, ctx_lens, gammas, out, lse_out);
+    a.own = source_of(shape, k_codes, v_codes, page_table);
+    a.own.ks = static_cast<const uint8_t*>(k_scales);
+    a.own.vs = static_cast<const uint8_t*>(v_scales);
+    a.own.sbstride = layout->scale_batch_stride;
+    a.own.shstride = layout->scale_head_stride;
+    a.own.spstride = layout->scale_page_stride;
+    DeviceScope dev(ctx->device);
+    if (dev.err != hipSuccess) return hip_fail(ctx, dev.err);
+    hipError_t e = launch_attn_rows(a, static_cast<hipStream_t>(stream));
+    if (e != hipSuccess) return hip_fail(ctx, e);
+    return RAPID_OK;
+}
+
+size_t rapid_verify_attn_prefix_workspace_bytes(const rapid_ctx*, const rapid_attn_shape* shape, const rapid_prefix_layout* prefix)
+{
+    return check_prefix_shape(shape, prefix) == RAPID_OK ? 256 : 0;
+}
+
+int rapid_verify_attn_prefix(rapid_ctx* ctx, const rapid_attn_shape* shape, const rapid_prefix_layout* prefix, const void* q,
+                             const void* k_prefix, const void* v_prefix, const int32_t* prefix_len, const int32_t* prefix_table,
+                             const void* k_cache, const void* v_cache,
+                             const int32_t* ctx_lens, const int32_t* gammas, const int32_t* page_table,
+                             void* out, float* lse_out, void* workspace, size_t workspace_bytes, void* stream)
+{
+    if (!ctx) return RAPID_EINVAL;
+    int rc = check_prefix_shape(shape, prefix);
+    if (rc != RAPID_OK) return rc;
+    if (!q || !k_cache || !v_cache || !ctx_lens || !prefix_len || !out) return RAPID_EINVAL;
+    if (shape->page_size != 0 && !page_table) return RAPID_EINVAL;
+    if (prefix_table ? k_prefix || v_prefix : prefix->max_prefix > 0 && (!k_prefix || !v_prefix)) return RAPID_EINVAL;
+    rc = check_prefix_place(shape, prefix, prefix_table != nullptr);
+    if (rc != RAPID_OK) return rc;
+    if (!aligned(q, 16) || !aligned(k_cache, 16) || !aligned(v_cache, 16) || !aligned(k_prefix, 16) || !aligned(v_prefix, 16) ||
+        !aligned(out, 16)) return RAPID_EALIGN;
+    if (!workspace || !aligned(workspace, 256) || workspace_bytes < rapid_verify_attn_prefix_workspace_bytes(ctx, shape, prefix))
+        return RAPID_EWORKSPACE;
+    AttnRowsLaunch a = rows_launch(shape, q, ctx_lens, gammas, out, lse_out);
+    a.own = source_of(shape, k_cache, v_cache, page_table);
+    a.prefix_len = prefix_len;
+    a.max_prefix = prefix->max_prefix;
+    if (prefix_table) {
+        a.prefix = source_of(shape, k_cache, v_cache, prefix_table);
+        a.prefix.max_pages = prefix->max_pages;
+    } else {
+        a.prefix.k = k_prefix;
+        a.prefix.v = v_prefix;
+        a.prefix.tstride = prefix->token_stride;
+        a.prefix.hstride = prefix->head_stride;
+    }
+    DeviceScope dev(ctx->device);
+    if (dev.err != hipSuccess) return hip_fail(ctx, dev.err);
+    hipError_t e = launch_attn_rows(a, static_cast<hipStream_t>(stream));
     if (e != hipSuccess) return hip_fail(ctx, e);
     return RAPID_OK;
 }

@@ -144,6 +144,52 @@ hipError_t launch_kv_append(const KvAppendLaunch& a, hipStream_t stream);
 hipError_t launch_kv_commit(int B, int gamma, const int32_t* gammas, const int32_t* n_accepted, int32_t* ctx_lens,
                             hipStream_t stream);
 
+// ---- cache in 8 bits (kv_quant.hip)
+// One of the two caches, with the rows that are written to it or read from it.
+struct KvQuantSide {
+    uint16_t* rows;             // [B][Qmax][Hkv][D] bf16
+    uint8_t* codes;
+    uint8_t* scales;
+};
+struct KvQuantLaunch {
+    KvQuantSide side[2];        // K, V
+    const int32_t* ctx_lens;
+    const int32_t* gammas;
+    const int32_t* page_table;
+    int32_t B, Qmax, Hkv, D, gamma;
+    int32_t max_ctx;
+    int64_t bstride, tstride, hstride, pstride;   // of the codes, bytes
+    int64_t sbstride, shstride, spstride;         // of the scales, bytes
+    int32_t page_shift, page_mask, max_pages;     // page_shift < 0: contiguous
+    int32_t page_hi;
+};
+hipError_t launch_kv_append_quant(const KvQuantLaunch& a, hipStream_t stream);
+hipError_t launch_kv_read_quant(const KvQuantLaunch& a, hipStream_t stream);
+
+// ---- attention over a cache in 8 bits, and behind a shared prefix (attn_rows.hip)
+struct AttnSource {             // where keys and values lie; strides in elements
+    const void* k;
+    const void* v;
+    const uint8_t* ks;          // scales, or null (bf16)
+    const uint8_t* vs;
+    const int32_t* page_table;  // or null: contiguous
+    int64_t bstride, tstride, hstride, pstride;
+    int64_t sbstride, shstride, spstride;
+    int32_t page_shift, page_mask, max_pages, page_hi;
+};
+struct AttnRowsLaunch {
+    const uint16_t* q;
+    uint16_t* out;
+    float* lse_out;
+    const int32_t* ctx_lens;
+    const int32_t* gammas;
+    const int32_t* prefix_len;  // or null: no prefix
+    AttnSource own, prefix;
+    int32_t B, Qmax, Hq, Hkv, G, D, gamma, max_ctx, max_prefix;
+    float scale_log2e;
+};
+hipError_t launch_attn_rows(const AttnRowsLaunch& a, hipStream_t stream);
+
 // ---- retrieval chunk selection (retrieve.hip)
 struct RetrieveLaunch {
     const float* emb;       // [n][dim]
