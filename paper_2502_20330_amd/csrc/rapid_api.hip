@@ -1,6 +1,7 @@
 // C ABI of librapid.so: argument checking, split planning, kernel dispatch.
 #include <new>
 
+#include "attn_stream.h"
 #include "rapid_internal.h"
 
 // Scratch memory of the allocation-free entry point (rapid_verify_attn_static): one copy per
@@ -324,6 +325,24 @@ AttnRowsLaunch rows_launch(const rapid_attn_shape* s, const void* q, const int32
     return a;
 }
 
+// The streaming kernel's plan for a shape.
+StreamLaunch stream_launch(const rapid_ctx* ctx, const rapid_attn_shape* s, const AttnSource& own)
+{
+    StreamLaunch a{};
+    a.own = own;
+    a.B = s->batch;
+    a.Qmax = s->q_max;
+    a.Hq = s->n_q_heads;
+    a.Hkv = s->n_kv_heads;
+    a.G = a.Hq / a.Hkv;
+    a.D = s->head_dim;
+    a.gamma = s->gamma;
+    a.max_ctx = s->max_ctx;
+    a.scale_log2e = s->softmax_scale * 1.4426950408889634f;
+    plan_attn_stream(a, ctx && ctx->n_cu > 0 ? ctx->n_cu : 256);
+    return a;
+}
+
 }  // namespace
 
 extern "C" {
@@ -347,6 +366,7 @@ int rapid_create(rapid_ctx** out, int device)
     if ((e = hipSetDevice(device)) != hipSuccess) return RAPID_EHIP;
     hipError_t ec = configure_verify_attn();
     if (ec == hipSuccess) ec = configure_lm_head();
+    if (ec == hipSuccess) ec = configure_attn_stream();
     if (ec == hipSuccess) ec = configure_hbm_read_probe();
     void* scratch_ptr = nullptr;                      // this device's copy of `scratch`
     if (ec == hipSuccess) ec = hipGetSymbolAddress(&scratch_ptr, HIP_SYMBOL(scratch));
@@ -832,9 +852,12 @@ int rapid_kv_read_quant(rapid_ctx* ctx, const rapid_attn_shape* shape, const rap
                            stream);
 }
 
-size_t rapid_verify_attn_quant_workspace_bytes(const rapid_ctx*, const rapid_attn_shape* shape)
+size_t rapid_verify_attn_quant_workspace_bytes(const rapid_ctx* ctx, const rapid_attn_shape* shape)
 {
-    return check_quant_shape(shape, true) == RAPID_OK ? 256 : 0;
+    if (check_quant_shape(shape, true) != RAPID_OK) return 0;
+    AttnSource own{};
+    own.ks = own.vs = reinterpret_cast<const uint8_t*>(1);      // a cache in 8 bits; nothing is read
+    return attn_stream_workspace_bytes(stream_launch(ctx, shape, own));
 }
 
 int rapid_verify_attn_quant(rapid_ctx* ctx, const rapid_attn_shape* shape, const rapid_quant_layout* layout, const void* q,
@@ -850,18 +873,24 @@ int rapid_verify_attn_quant(rapid_ctx* ctx, const rapid_attn_shape* shape, const
     if (shape->page_size != 0 && !page_table) return RAPID_EINVAL;
     if (!aligned(q, 16) || !aligned(k_codes, 16) || !aligned(v_codes, 16) || !aligned(k_scales, 16) || !aligned(v_scales, 16) ||
         !aligned(out, 16)) return RAPID_EALIGN;
-    if (!workspace || !aligned(workspace, 256) || workspace_bytes < rapid_verify_attn_quant_workspace_bytes(ctx, shape))
-        return RAPID_EWORKSPACE;
-    AttnRowsLaunch a = rows_launch(shape, q, ctx_lens, gammas, out, lse_out);
-    a.own = source_of(shape, k_codes, v_codes, page_table);
-    a.own.ks = static_cast<const uint8_t*>(k_scales);
-    a.own.vs = static_cast<const uint8_t*>(v_scales);
-    a.own.sbstride = layout->scale_batch_stride;
-    a.own.shstride = layout->scale_head_stride;
-    a.own.spstride = layout->scale_page_stride;
+    AttnSource own = source_of(shape, k_codes, v_codes, page_table);
+    own.ks = static_cast<const uint8_t*>(k_scales);
+    own.vs = static_cast<const uint8_t*>(v_scales);
+    own.sbstride = layout->scale_batch_stride;
+    own.shstride = layout->scale_head_stride;
+    own.spstride = layout->scale_page_stride;
+    StreamLaunch a = stream_launch(ctx, shape, own);
+    if (!workspace || !aligned(workspace, 256) || workspace_bytes < attn_stream_workspace_bytes(a)) return RAPID_EWORKSPACE;
+    bind_attn_stream(a, workspace);
+    a.q = static_cast<const uint16_t*>(q);
+    a.out = static_cast<uint16_t*>(out);
+    a.lse_out = lse_out;
+    a.ctx_lens = ctx_lens;
+    a.gammas = gammas;
     DeviceScope dev(ctx->device);
     if (dev.err != hipSuccess) return hip_fail(ctx, dev.err);
-    hipError_t e = launch_attn_rows(a, static_cast<hipStream_t>(stream));
+    hipError_t e = launch_attn_stream(a, static_cast<hipStream_t>(stream));
+    if (e == hipSuccess) e = launch_attn_stream_merge(a, static_cast<hipStream_t>(stream));
     if (e != hipSuccess) return hip_fail(ctx, e);
     return RAPID_OK;
 }
