@@ -11,7 +11,7 @@ ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "librapid.so")
 SOURCES = ["rapid_api.hip", "verify_attn.hip", "accept.hip", "accept_greedy.hip", "hbm_probe.hip", "lm_head.hip", "kv_cache.hip", "retrieve.hip",
-           "kv_quant.hip", "attn_rows.hip", "attn_stream.hip"]
+           "kv_quant.hip", "attn_stream.hip", "attn_prefix.hip"]
 # packed-fp32 instructions are switched off on purpose: some of their forms have given
 # wrong results on this hardware generation; plain fp32 code costs nothing here
 FLAGS = ["-O3", "--offload-arch=gfx950", "-std=c++17", "-fPIC", "-Wall", "-Wno-unused-function",

@@ -1,0 +1,286 @@
+// Attention of a whole batch's rows over one shared prefix (gfx950).
+//
+// All rows of the batch, R = B (gamma_max + 1) G per kv head, attend the same P tokens, without a mask: the prefix is one "sequence"
+// with R rows.  Reading it costs 4 d bytes per token and kv head, computing 4 R d multiply-adds and R exponentials, so that from about a hundred rows on the
+// matrix cores and the exponentials bound it and no longer the memory.  Up to 96 rows the streaming kernel (attn_stream.hip) does it; this one takes more:
+//  * A workgroup has eight waves, T of which share a stream of token tiles (8 / T streams) and hold RB blocks of 16 rows each, T RB 16 rows
+//    together.  Tiles go HBM -> LDS once a workgroup; S of them lie in a ring, and one barrier a tile says that a tile has landed and
+//    that the slot of the one before it is free.
+//  * Rows beyond T RB 16 go to other workgroups, which read the same tokens at about the same time on the same die (blockIdx modulo 8), so that its L2
+//    serves all but one of them.
+#include "attn_tile.h"
+
+namespace {
+
+template <int D, int T_, int RB_>
+struct Geo : TileGeo<D, false, D == 64 ? 4 : 2> {
+    using Tile = TileGeo<D, false, D == 64 ? 4 : 2>;
+    using Tile::SLOT, Tile::TT, Tile::NLD;
+    static constexpr int T = T_, RB = RB_;
+    static constexpr int NW = 8, NP = NW / T;                     // waves, token streams
+    static constexpr int H = NLD / T;                             // loads of a tile of K or V that a wave issues
+    static constexpr int QUANTUM = NP * TT;
+    static constexpr int S = 128 * 1024 / NP / (2 * SLOT);        // tiles of a ring
+    static constexpr int RING = S * 2 * SLOT;
+    static constexpr int RP = T * RB * 16;                        // rows of a workgroup
+    static constexpr int NH = NP * RP * (D + 4) * 4 > 140 * 1024 ? 2 : 1;   // passes of the last exchange, D / NH columns each
+    static constexpr int OROW = D / NH + 4;
+    static constexpr int MERGE = NP > 1 ? NP * RP * OROW * 4 : 0;
+    static constexpr int ML = NP * RING > MERGE ? NP * RING : MERGE;
+    static constexpr int TAKEN = ML + NW * RB * 16 * 8;           // a word for each stream
+    static constexpr int LDS = TAKEN + NP * 4;
+};
+
+// Loads of tile part `team` of K and V.
+template <class G, bool PAGED>
+__device__ __forceinline__ void load_both(const RowAddr& ra, uint32_t kslot, uint32_t vslot, int t0, int last_tok, int lane, int team)
+{
+    TilePages<G, PAGED> pages;
+    pages.find(ra, t0, last_tok);
+    load_tile<G, PAGED, false>(ra, pages, kslot, t0, last_tok, lane, team * G::H, G::H);
+    load_tile<G, PAGED, true>(ra, pages, vslot, t0, last_tok, lane, team * G::H, G::H);
+}
+
+// Tokens [c0, c1) for the rows of tile `rt`; the partial goes to the rows from pbase on.
+template <class G, bool PAGED>
+__device__ __forceinline__ void prefix_piece(const StreamLaunch& a, char* smem, int h, int rt, int c0, int c1, int64_t pbase)
+{
+    constexpr int RB = G::RB;
+    const int tid = threadIdx.x, lane = tid & 63, ln = lane & 15, lg = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int part = wave / G::T, team = wave % G::T;
+    const int rows = a.Qmax * a.G - rt * G::RP;          // of this tile, if there are so many
+
+    const int ntile = (c1 - c0 + G::TT - 1) / G::TT;
+    const int nt = (ntile + G::NP - 1) / G::NP;          // tiles of a stream; all run as many, those past the end are masked
+    const int first = part * nt;
+    const int last_tok = min(c1, c0 + (first + nt) * G::TT) - 1;
+    auto tile_t0 = [&](int it) { return c0 + (first + it) * G::TT; };
+    const RowAddr addr = make_row_addr<G, PAGED>(a.own, 0, h);
+    char* kring = smem + part * G::RING;
+    char* vring = kring + G::S * G::SLOT;
+    const uint32_t kring_lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)smem + part * G::RING;
+    const uint32_t vring_lds = kring_lds + G::S * G::SLOT;
+    int* taken_word = reinterpret_cast<int*>(smem + G::TAKEN) + part;
+    if (lane == 0) *taken_word = 0;
+
+    // Q^T as the B operand, straight to registers: each wave has rows of its own
+    bf16x8 qf[RB][G::KS];
+    int lim[RB];
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb) {
+        const int row = team * RB * 16 + rb * 16 + ln, r = rt * G::RP + min(row, rows - 1);
+        lim[rb] = c1 - 1;
+        const u32x4* src = reinterpret_cast<const u32x4*>(a.q + ((int64_t)(r / a.G) * a.Hq + h * a.G + r % a.G) * G::D);
+#pragma unroll
+        for (int ks = 0; ks < G::KS; ++ks) {
+            u32x4 raw = src[ks * 4 + lg];
+            if (row >= rows) raw = u32x4{0, 0, 0, 0};
+            qf[rb][ks] = __builtin_bit_cast(bf16x8, raw);
+        }
+    }
+#pragma unroll
+    for (int it = 0; it < G::S - 1; ++it)
+        load_both<G, PAGED>(addr, kring_lds + it * G::SLOT, vring_lds + it * G::SLOT, tile_t0(it), last_tok, lane, team);
+
+    WaveState<G, RB> st;
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb) {
+        st.m[rb] = -INFINITY;
+        st.l[rb] = 0.f;
+#pragma unroll
+        for (int db = 0; db < G::DB; ++db) st.acc[db][rb] = floatx4{0.f, 0.f, 0.f, 0.f};
+    }
+    const float c = a.scale_log2e;
+    const int first_masked_t0 = c1 - (G::TT - 1);        // tiles from here on reach past the end
+    bool taken = false;
+    const uint32_t no_scales[G::TB] = {};
+
+    int slot = 0, before = G::S - 1;                     // ring slots of tiles it and it - 1
+    for (int it = 0; it < nt; ++it) {
+        char* kt = kring + slot * G::SLOT;
+        char* vt = vring + slot * G::SLOT;
+        const int t0 = tile_t0(it);
+        floatx4 s[G::TB][RB];
+        bf16x8 pb[G::TB / 2][RB];
+
+        wait_loads<(G::S - 2) * 2 * G::H>();             // own part of tile it
+        lds_reads_done();                                // of tile it - 1
+        __syncthreads();
+        load_both<G, PAGED>(addr, kring_lds + before * G::SLOT, vring_lds + before * G::SLOT, tile_t0(it + G::S - 1), last_tok, lane, team);
+        score_tile<G, RB>(s, qf, kt, nullptr, lane);
+        softmax_tile<G, RB>(st, s, pb, no_scales, t0, t0 >= first_masked_t0, lim, c1, c, lane);
+        if (t0 >= first_masked_t0) taken |= take_not_finite<G>(vt, lane);      // (whoever comes second finds zeros)
+        pv_tile<G, RB>(st, pb, vt, lane);
+        before = slot;
+        slot = slot + 1 == G::S ? 0 : slot + 1;
+    }
+    wait_loads<0>();                                     // no load may land after the rings are used below
+    if (taken && lane == 0) *taken_word = 1;
+    __syncthreads();                                     // all rings are dead from here on
+    if (*taken_word != 0) {
+        const int it = max(0, (max(first_masked_t0 - c0, 0) + G::TT - 1) / G::TT - first);
+        add_not_finite<G, RB, PAGED>(st, addr, tile_t0(it), min(c1, tile_t0(nt)), lim, lane);
+    }
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb) st.l[rb] = sum_over_groups(st.l[rb]);
+
+    const int row0 = team * RB * 16 + ln;
+    if constexpr (G::NP == 1) {
+#pragma unroll
+        for (int rb = 0; rb < RB; ++rb) {
+            const int row = row0 + rb * 16;
+            if (row >= rows) continue;
+            if (lg == 0) {
+                a.part_ml[(pbase + row) * 2 + 0] = st.m[rb];
+                a.part_ml[(pbase + row) * 2 + 1] = st.l[rb];
+            }
+#pragma unroll
+            for (int db = 0; db < G::DB; ++db)
+                *reinterpret_cast<floatx4*>(a.part_o + (pbase + row) * G::D + db * 16 + lg * 4) = st.acc[db][rb];
+        }
+        __syncthreads();                                 // everybody has read the words in LDS
+        return;
+    }
+    // ---- join the streams, in a fixed order
+    float* obuf = reinterpret_cast<float*>(smem);                              // [NP][RP][OROW]
+    float* mlbuf = reinterpret_cast<float*>(smem + G::ML);                     // [NP][RP][2]
+    if (lg == 0) {
+#pragma unroll
+        for (int rb = 0; rb < RB; ++rb) {
+            mlbuf[(part * G::RP + row0 + rb * 16) * 2 + 0] = st.m[rb];
+            mlbuf[(part * G::RP + row0 + rb * 16) * 2 + 1] = st.l[rb];
+        }
+    }
+    __syncthreads();
+    float own[RB];
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb) {
+        const int row = row0 + rb * 16;
+        float mw[G::NP], mm = -INFINITY, ll = 0.f;
+#pragma unroll
+        for (int p = 0; p < G::NP; ++p) {
+            mw[p] = mlbuf[(p * G::RP + row) * 2];
+            mm = fmaxf(mm, mw[p]);
+        }
+        const float m_use = (mm == -INFINITY) ? 0.f : mm;
+#pragma unroll
+        for (int p = 0; p < G::NP; ++p) ll += mlbuf[(p * G::RP + row) * 2 + 1] * fast_exp2(mw[p] - m_use);
+        own[rb] = fast_exp2(st.m[rb] - m_use);
+        if (part == 0 && lg == 0 && row < rows) {
+            a.part_ml[(pbase + row) * 2 + 0] = mm;
+            a.part_ml[(pbase + row) * 2 + 1] = ll;
+        }
+    }
+    constexpr int DH = G::D / G::NH;
+#pragma unroll
+    for (int half = 0; half < G::NH; ++half) {
+#pragma unroll
+        for (int rb = 0; rb < RB; ++rb)
+#pragma unroll
+            for (int x = 0; x < G::DB / G::NH; ++x)
+                *reinterpret_cast<floatx4*>(obuf + (part * G::RP + row0 + rb * 16) * G::OROW + x * 16 + lg * 4) =
+                    st.acc[half * (G::DB / G::NH) + x][rb] * own[rb];
+        __syncthreads();
+        for (int f = tid; f < min(rows, G::RP) * (DH / 4); f += G::NW * 64) {
+            const int row = f / (DH / 4), x = f % (DH / 4) * 4;
+            floatx4 sum = *reinterpret_cast<const floatx4*>(obuf + row * G::OROW + x);
+#pragma unroll
+            for (int p = 1; p < G::NP; ++p) sum += *reinterpret_cast<const floatx4*>(obuf + (p * G::RP + row) * G::OROW + x);
+            *reinterpret_cast<floatx4*>(a.part_o + (pbase + row) * G::D + half * DH + x) = sum;
+        }
+        __syncthreads();
+    }
+}
+
+// One workgroup per (share, kv head, row tile); the row tiles of a (share, kv head) are eight apart, on one die.
+template <class G, bool PAGED>
+__global__ void __launch_bounds__(G::NW * 64) attn_prefix(StreamLaunch a)
+{
+    extern __shared__ __attribute__((aligned(1024))) char smem[];
+    const int units = a.groups * a.Hkv, whole = units / 8 * 8, idx = blockIdx.x;
+    int u, rt;
+    if (idx < whole * a.tiles) {
+        u = idx / (8 * a.tiles) * 8 + idx % 8;
+        rt = idx / 8 % a.tiles;
+    } else {
+        u = whole + (idx - whole * a.tiles) % (units - whole);
+        rt = (idx - whole * a.tiles) / (units - whole);
+    }
+    u = __builtin_amdgcn_readfirstlane(u);
+    rt = __builtin_amdgcn_readfirstlane(rt);
+    const int g = u / a.Hkv, h = __builtin_amdgcn_readfirstlane(u % a.Hkv);
+    for_each_piece(a, __builtin_amdgcn_readfirstlane(g), threadIdx.x & 63, G::QUANTUM, [&](int, int, int c0, int c1) {
+        prefix_piece<G, PAGED>(a, smem, h, rt, c0, c1, ((int64_t)(h * a.tiles + rt) * a.nslots + g) * G::RP);
+        wait_loads<0>();
+    });
+}
+
+// Calls f(Geo) for the kernel of `rows` rows a workgroup.
+template <int D, class F>
+hipError_t with_rows(int rows, F f)
+{
+    switch (rows) {
+        case 128: return f(Geo<D, 4, 2>());
+        case 192: return f(Geo<D, 4, 3>());
+        case 256: return f(Geo<D, 8, 2>());
+        case 384: return f(Geo<D, 8, 3>());
+    }
+    return hipErrorInvalidValue;
+}
+template <class F>
+hipError_t with_rows(int D, int rows, F f) { return D == 128 ? with_rows<128>(rows, f) : with_rows<64>(rows, f); }
+
+}  // namespace
+
+hipError_t configure_attn_prefix()
+{
+    for (int D = 64; D <= 128; D += 64)
+        for (int rows : {128, 192, 256, 384}) {
+            const hipError_t e = with_rows(D, rows, [](auto geo) {
+                using G = decltype(geo);
+                static_assert(G::LDS <= 160 * 1024, "LDS of a compute unit");
+                const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(attn_prefix<G, false>),
+                                                         hipFuncAttributeMaxDynamicSharedMemorySize, G::LDS);
+                if (e != hipSuccess) return e;
+                return hipFuncSetAttribute(reinterpret_cast<const void*>(attn_prefix<G, true>),
+                                           hipFuncAttributeMaxDynamicSharedMemorySize, G::LDS);
+            });
+            if (e != hipSuccess) return e;
+        }
+    return hipSuccess;
+}
+
+// Rows a workgroup: the choice that pads least, the larger of equals (fewer readers of the prefix).
+void plan_attn_prefix(StreamLaunch& a, int n_cu)
+{
+    const int R = a.Qmax * a.G;
+    int64_t least = -1;
+    for (int rows : {384, 256, 192, 128}) {
+        const int64_t padded = ((int64_t)R + rows - 1) / rows * rows;
+        if (least >= 0 && padded >= least) continue;
+        least = padded;
+        a.RP = rows;
+    }
+    a.tiles = (R + a.RP - 1) / a.RP;
+    (void)with_rows(a.D, a.RP, [&](auto geo) {
+        a.quantum = decltype(geo)::QUANTUM;
+        return hipSuccess;
+    });
+    const int64_t units = (int64_t)a.Hkv * a.tiles;
+    a.groups = n_cu > units ? (int)(n_cu / units) : 1;
+    const int64_t most = ((int64_t)a.max_ctx + a.quantum - 1) / a.quantum + kPieceQuanta;
+    if (a.groups > most) a.groups = (int)most;
+    a.nslots = a.groups;
+    a.rot = 0;
+}
+
+hipError_t launch_attn_prefix(const StreamLaunch& a, hipStream_t stream)
+{
+    return with_rows(a.D, a.RP, [&](auto geo) {
+        using G = decltype(geo);
+        auto fn = a.own.page_table ? attn_prefix<G, true> : attn_prefix<G, false>;
+        hipLaunchKernelGGL(fn, dim3(a.groups * a.Hkv * a.tiles), dim3(G::NW * 64), G::LDS, stream, a);
+        return hipGetLastError();
+    });
+}

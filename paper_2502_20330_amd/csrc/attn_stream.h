@@ -1,27 +1,44 @@
-// Launch of the streaming attention kernel (attn_stream.hip).
+// Launches of the attention kernels that divide a batch's tokens among the workgroups by themselves (attn_stream.hip, attn_prefix.hip).
 #pragma once
 #include "rapid_internal.h"
 
+struct AttnSource {             // where keys and values lie; strides in elements (scales: bytes)
+    const void* k;
+    const void* v;
+    const uint8_t* ks;          // scales, or null: bf16
+    const uint8_t* vs;
+    const int32_t* page_table;  // or null: contiguous
+    int64_t bstride, tstride, hstride, pstride;
+    int64_t sbstride, shstride, spstride;
+    int32_t page_shift, page_mask, max_pages, page_hi;
+};
 struct StreamLaunch {
     const uint16_t* q;
     uint16_t* out;
     float* lse_out;
     const int32_t* ctx_lens;
     const int32_t* gammas;
-    AttnSource own;             // codes and scales, or bf16
-    float* part_o;              // [Hkv][nslots][RP][D], relative to the maximum in part_ml; slot g + b: share g's piece of sequence b
-    float* part_ml;             // [Hkv][nslots][RP][2] (maximum in log2 units, sum)
+    AttnSource own;
+    float* part_o;              // [Hkv][tiles][nslots][RP][D], relative to the maximum in part_ml; slot g + b: share g's piece of sequence b
+    float* part_ml;             // [Hkv][tiles][nslots][RP][2] (maximum in log2 units, sum)
     int32_t B, Qmax, Hq, Hkv, G, D, gamma, max_ctx;
-    int32_t RP;                 // packed rows of a slot, a multiple of 16
+    int32_t shared;             // 1: a shared prefix: one sequence (ctx_lens: its length) with the rows of the batch, which all attend all of it
+    int32_t RP, tiles;          // packed rows of a slot (a multiple of 16), row tiles (1 but for attn_prefix)
     int32_t groups, nslots;     // shares of a kv head, groups + B - 1
     int32_t quantum;            // tokens that shares are cut by
     int32_t rot;                // 1: share g of slot x serves head (x + g) mod Hkv, 0: head x
     float scale_log2e;
 };
-// Fills the plan (RP .. rot) from the shape and the source's layout.
+constexpr int kStreamRows = 96;      // packed rows that the streaming kernel takes
+// Fill the plan (RP .. rot) from the shape and the source's layout.
 void plan_attn_stream(StreamLaunch& a, int n_cu);
-size_t attn_stream_workspace_bytes(const StreamLaunch& a);
+void plan_attn_prefix(StreamLaunch& a, int n_cu);
+size_t attn_stream_workspace_bytes(const StreamLaunch& a);                       // of either plan
 void bind_attn_stream(StreamLaunch& a, void* workspace);
 hipError_t configure_attn_stream();
-hipError_t launch_attn_stream(const StreamLaunch& a, hipStream_t stream);        // writes the partials
-hipError_t launch_attn_stream_merge(const StreamLaunch& a, hipStream_t stream);
+hipError_t configure_attn_prefix();
+// Write the partials.
+hipError_t launch_attn_stream(const StreamLaunch& a, hipStream_t stream);
+hipError_t launch_attn_prefix(const StreamLaunch& a, hipStream_t stream);        // a shared prefix with more than kStreamRows rows
+// Joins the partials of `own`, and of a shared prefix where `prefix` has any (prefix.part_o not null).
+hipError_t launch_attn_stream_merge(const StreamLaunch& own, const StreamLaunch& prefix, hipStream_t stream);

@@ -16,38 +16,24 @@
 //    tokens) and is multiplied into the token's weight instead, in 32 bits, before the weight's own rounding to bf16.
 //  * ds_read_b64_tr_b8 delivers V^T, eight tokens of one column, straight from LDS.
 #include "attn_exchange.h"
-#include "attn_primitives.h"
 #include "attn_stream.h"
-
-typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
-typedef int i32x2 __attribute__((ext_vector_type(2)));
-typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+#include "attn_tile.h"
 
 namespace {
 
-constexpr float kRescaleLog2 = 8.0f;   // the running maximum only moves when a tile exceeds it by this (log2 units)
-constexpr int kPieceQuanta = 2;        // what a sequence costs a workgroup besides its tokens, in quanta
-
 // RB0: row blocks of 16 that a wave has, or team 0; RB1: those of team 1, 0 = there are no teams.
-template <int D_, bool QUANT_, int RB0_, int RB1_>
-struct Geo {
-    static constexpr int D = D_, RB0 = RB0_, RB1 = RB1_, RB = RB0 + RB1;
-    static constexpr bool QUANT = QUANT_, TEAMS = RB1 > 0;
+template <int D, bool QUANT, int RB0_, int RB1_>
+struct Geo : TileGeo<D, QUANT, QUANT && D == 64 ? 4 : 2> {
+    using Tile = TileGeo<D, QUANT, QUANT && D == 64 ? 4 : 2>;
+    using Tile::SLOT, Tile::SC, Tile::TT, Tile::QROWB;
+    static constexpr int RB0 = RB0_, RB1 = RB1_, RB = RB0 + RB1;
+    static constexpr bool TEAMS = RB1 > 0;
     static constexpr int NP = QUANT && !TEAMS ? 8 : 4;            // token streams of a workgroup
     static constexpr int NW = TEAMS ? 2 * NP : NP;                // waves
-    static constexpr int TB = QUANT && D == 64 ? 4 : 2;           // blocks of 16 tokens in a tile
-    static constexpr int TT = TB * 16;                            // tokens of a tile
     static constexpr int QUANTUM = NP * TT;                       // tokens of a workgroup's step
-    static constexpr int KS = D / 32, DB = D / 16;                // steps of the QK product, blocks of the head dim
-    static constexpr int ROWB = QUANT ? D : 2 * D;                // bytes of a K or V row
-    static constexpr int CPR = ROWB / 16;                         // 16-byte chunks of it
-    static constexpr int RPI = 64 / CPR;                          // rows that one wave-wide 1 KiB load moves
-    static constexpr int NLD = TT / RPI;                          // loads of a tile
-    static constexpr int SLOT = TT * ROWB;                        // bytes of a K or V tile
-    static constexpr int SC = QUANT ? 1 : 0;                      // loads of a tile's scales
     static constexpr int S = 128 * 1024 / NP / (2 * SLOT);        // tiles of a ring: the loads in flight fill 128 KiB
     static constexpr int RING = S * (2 * SLOT + SC * 256);        // S tiles of K, of V, of scales
-    static constexpr int QROWB = 2 * D, QCPR = QROWB / 16, QRPI = 64 / QCPR;
+    static constexpr int QCPR = QROWB / 16, QRPI = 64 / QCPR;
     static constexpr int RP = RB * 16;
     static constexpr int NH = NP * RP * (D + 4) * 4 > 140 * 1024 ? 2 : 1;   // passes of the last exchange, D / NH columns each
     static constexpr int OROW = D / NH + 4;                       // padded row of the exchange (floats)
@@ -57,404 +43,6 @@ struct Geo {
     static constexpr int TAKEN = ML + NW * (TEAMS ? (RB0 > RB1 ? RB0 : RB1) : RB0) * 16 * 8;   // a word for each stream
     static constexpr int LDS = TAKEN + (TEAMS ? NP * 4 : 0);
 };
-
-// Swizzles: chunk c of row r is stored at c ^ f(r).  A 128-bit read of K or Q takes 16 consecutive rows at one logical chunk; a transposed read of
-// V takes, per half of the wave, rows 0..7 and 16..23 (or 8..15 and 24..31) of 32.
-template <int ROWB> __device__ __forceinline__ int k_swz(int r) { return ROWB == 256 ? r & 15 : ROWB == 128 ? (r >> 1) & 7 : (r >> 2) & 3; }
-template <bool QUANT, int ROWB> __device__ __forceinline__ int v_swz(int r)
-{
-    if (QUANT) return ROWB == 128 ? ((r >> 1) & 3) | (r >> 4 & 1) << 2 : (r >> 2 & 1) | (r >> 4 & 1) << 1;
-    return ROWB == 256 ? (r & 7) << 1 : (r >> 1 & 3) << 1;
-}
-
-// ---- shares
-// Each sequence costs its tokens in quanta and kPieceQuanta more, which come first; the sum is cut into equal shares.
-__device__ __forceinline__ int seq_len(const StreamLaunch& a, int b) { return max(min(a.ctx_lens[b], a.max_ctx), 0); }
-__device__ __forceinline__ int seq_queries(const StreamLaunch& a, int b)
-{
-    return min(max(a.gammas ? a.gammas[b] : a.gamma, 0), a.Qmax - 1) + 1;
-}
-__device__ __forceinline__ int seq_cost(int L, int quantum) { return L > 0 ? (L + quantum - 1) / quantum + kPieceQuanta : 0; }
-
-struct Shares {
-    int used, len, rest;                // shares in use; the first `rest` of them have len + 1 quanta
-    __device__ __forceinline__ Shares(int total, int groups) : used(max(1, min(groups, total)))
-    {
-        len = (int)((unsigned)total / (unsigned)used);
-        rest = total - len * used;
-    }
-    __device__ __forceinline__ int begin(int g) const { return g >= used ? 0x7fffffff : g * len + min(g, rest); }
-    __device__ __forceinline__ int owner(int x) const
-    {
-        const int head = rest * (len + 1);
-        return x < head ? (int)((unsigned)x / (unsigned)(len + 1)) : rest + (int)((unsigned)(x - head) / (unsigned)max(len, 1));
-    }
-};
-__device__ __forceinline__ int total_cost(const StreamLaunch& a, int lane, int quantum)
-{
-    int total = 0;
-    for (int b0 = 0; b0 < a.B; b0 += 64)
-        total += __builtin_amdgcn_readlane(scan_costs(b0 + lane < a.B ? seq_cost(seq_len(a, b0 + lane), quantum) : 0), 63);
-    return total;
-}
-// Calls piece(b, L, c0, c1) for every piece [c0, c1) of a sequence b in share g, in order.
-template <class Piece>
-__device__ __forceinline__ void for_each_piece(const StreamLaunch& a, int g, int lane, int quantum, Piece piece)
-{
-    const int total = total_cost(a, lane, quantum);
-    const Shares sh(total, a.groups);
-    const int x0 = sh.begin(g), x1 = min(sh.begin(g + 1), total);
-    if (x0 >= x1) return;
-    int before = 0;                                      // cost of the sequences before b0
-    for (int b0 = 0; b0 < a.B; b0 += 64) {
-        const int len = b0 + lane < a.B ? seq_len(a, b0 + lane) : 0;
-        const int cost = seq_cost(len, quantum);
-        const int end = before + scan_costs(cost);
-        const int tok = end - cost + kPieceQuanta;       // position of the sequence's first tokens
-        const bool mine = cost > 0 && end > x0 && tok < x1;
-        for (unsigned long long todo = __ballot(mine); todo; todo &= todo - 1) {
-            const int l = __ffsll((long long)todo) - 1;
-            const int t = __builtin_amdgcn_readlane(tok, l), L = __builtin_amdgcn_readlane(len, l);
-            const int c0 = max(x0 - t, 0) * quantum;
-            const int c1 = min((min(x1, __builtin_amdgcn_readlane(end, l)) - t) * quantum, L);
-            if (c0 < c1) piece(b0 + l, L, c0, c1);
-        }
-        before = __builtin_amdgcn_readlane(end, 63);
-        if (before >= x1) break;
-    }
-}
-
-// ---- loads
-// Where the rows of this (sequence, kv head) start: uniform bases and a 32-bit byte offset per lane (the host checks that a
-// sequence, or a page, spans less than 4 GiB).
-struct RowAddr {
-    const char *k, *v;
-    const uint8_t *ks, *vs;
-    const __attribute__((address_space(4))) int32_t* pages;      // read as scalars
-    uint32_t tok_bytes;
-    int64_t page_bytes, scale_page_bytes;
-    int page_shift, page_mask, page_hi;
-};
-template <class G, bool PAGED>
-__device__ __forceinline__ RowAddr make_row_addr(const AttnSource& s, int b, int h)
-{
-    constexpr int E = G::QUANT ? 1 : 2;
-    RowAddr r;
-    const int64_t at = ((int64_t)h * s.hstride + (PAGED ? 0 : (int64_t)b * s.bstride)) * E;
-    r.k = static_cast<const char*>(s.k) + at;
-    r.v = static_cast<const char*>(s.v) + at;
-    const int64_t sat = (int64_t)h * s.shstride + (PAGED ? 0 : (int64_t)b * s.sbstride);
-    r.ks = s.ks + sat;
-    r.vs = s.vs + sat;
-    r.pages = PAGED ? (const __attribute__((address_space(4))) int32_t*)(s.page_table + (int64_t)b * s.max_pages) : nullptr;
-    r.tok_bytes = (uint32_t)(s.tstride * E);
-    r.page_bytes = s.pstride * E;
-    r.scale_page_bytes = s.spstride;
-    r.page_shift = s.page_shift;
-    r.page_mask = s.page_mask;
-    r.page_hi = s.page_hi;
-    return r;
-}
-
-// The pages of a tile's blocks of 16 tokens (a page holds 16 tokens at least).
-template <class G, bool PAGED>
-struct TilePages {
-    int id[G::TB];
-    __device__ __forceinline__ void find(const RowAddr& ra, int t0, int last_tok)
-    {
-        if (!PAGED) return;
-#pragma unroll
-        for (int j = 0; j < G::TB; ++j) id[j] = min(max(ra.pages[min(t0 + 16 * j, last_tok) >> ra.page_shift], 0), ra.page_hi);
-    }
-    // the page of block j, which may differ from lane to lane; selected, never indexed
-    __device__ __forceinline__ int of(int j) const
-    {
-        int r = __builtin_amdgcn_readfirstlane(id[0]);
-#pragma unroll
-        for (int x = 1; x < G::TB; ++x) {
-            const int other = __builtin_amdgcn_readfirstlane(id[x]);
-            r = j == x ? other : r;
-        }
-        return r;
-    }
-};
-
-// Loads [E0, E1) of a tile of K or V into `slot`.  Rows past `last_tok` are clamped to it (always a valid address); the softmax masks them.
-template <class G, bool PAGED, bool IS_V>
-__device__ __forceinline__ void load_tile(const RowAddr& ra, const TilePages<G, PAGED>& pages, uint32_t slot, int t0, int last_tok, int lane,
-                                          int e0, int n)
-{
-    const char* base = IS_V ? ra.v : ra.k;
-    const int r_local = lane / G::CPR, cpos = lane % G::CPR;
-#pragma unroll
-    for (int x = 0; x < G::NLD; ++x) {
-        if (x >= n) break;
-        const int e = e0 + x;
-        const int row = e * G::RPI + r_local;
-        const int c = cpos ^ (IS_V ? v_swz<G::QUANT, G::ROWB>(row) : k_swz<G::ROWB>(row));
-        const int tok = min(t0 + row, last_tok);
-        if (PAGED) {
-            const int id = __builtin_amdgcn_readfirstlane(pages.of(e * G::RPI / 16));
-            dma16(base + (int64_t)id * ra.page_bytes, (uint32_t)(tok & ra.page_mask) * ra.tok_bytes + (uint32_t)c * 16u, slot + e * 1024);
-        } else {
-            dma16(base, (uint32_t)tok * ra.tok_bytes + (uint32_t)c * 16u, slot + e * 1024);
-        }
-    }
-}
-
-// 4 bytes a lane, HBM -> LDS bytes [lds_addr + 4 i, + 4).
-__device__ __forceinline__ void dma4(const uint8_t* at, uint32_t lds_addr)
-{
-    asm volatile("s_mov_b32 m0, %1\n\tglobal_load_lds_dword %0, off"
-                 :
-                 : "v"(at), "s"(lds_addr)
-                 : "memory", "m0");
-}
-// The scales of a tile: TT bytes of K's, TT of V's, four a lane (the other lanes repeat them behind).  Groups of four tokens are read
-// whole; bytes past the last token, inside the row's multiple of 16, belong to tokens that the softmax masks.
-template <class G, bool PAGED>
-__device__ __forceinline__ void load_scales(const RowAddr& ra, const TilePages<G, PAGED>& pages, uint32_t slot, int t0, int last_tok, int lane)
-{
-    if (!G::QUANT) return;
-    const int i = lane % (G::TT / 4);
-    const int tok = min(t0 + 4 * i, last_tok & ~3);
-    const uint8_t* at = (lane / (G::TT / 4)) & 1 ? ra.vs : ra.ks;
-    if (PAGED) {
-        at += (int64_t)pages.of(i / 4) * ra.scale_page_bytes + (tok & ra.page_mask);
-    } else {
-        at += tok;
-    }
-    dma4(at, slot);
-}
-
-// ---- mathematics
-__device__ __forceinline__ float scale_value(uint32_t byte) { return __uint_as_float(byte << 23); }
-
-template <bool HI>
-__device__ __forceinline__ bf16x2 two_values(uint32_t w, float scale) { return __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, scale, HI); }
-__device__ __forceinline__ bf16x8 eight_values(uint32_t w0, uint32_t w1, float scale)
-{
-    const bf16x2 a = two_values<false>(w0, scale), b = two_values<true>(w0, scale), c = two_values<false>(w1, scale),
-                 d = two_values<true>(w1, scale);
-    return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
-}
-
-template <class G, int RB>
-struct WaveState {
-    float m[RB];                     // reference maximum per query row, log2 units (score * scale * log2 e)
-    float l[RB];                     // running sum, this lane group's tokens only
-    floatx4 acc[G::DB][RB];          // O^T: column 16 db + 4 (lane / 16) + i, row 16 rb + lane % 16
-};
-
-// S^T[token][row] for the tile in `kt`.  In 8 bits a lane reads 16 codes at a time, which feed two steps: step 2p + h of lane group lg holds
-// elements 64 p + 16 lg + 8 h .. + 7 (of K and of Q alike; any order of a sum's terms will do).
-template <class G, int RB>
-__device__ __forceinline__ void score_tile(floatx4 (&s)[G::TB][RB], const bf16x8 (&qf)[RB][G::KS], const char* kt, const char* sc, int lane)
-{
-    const int ln = lane & 15, lg = lane >> 4;
-#pragma unroll
-    for (int tb = 0; tb < G::TB; ++tb) {
-#pragma unroll
-        for (int rb = 0; rb < RB; ++rb) s[tb][rb] = floatx4{0.f, 0.f, 0.f, 0.f};
-        const int row = tb * 16 + ln;
-        if constexpr (G::QUANT) {
-            const float scale = scale_value(*reinterpret_cast<const uint8_t*>(sc + row));
-#pragma unroll
-            for (int p = 0; p < G::KS / 2; ++p) {
-                const int c = (p * 4 + lg) ^ k_swz<G::ROWB>(row);
-                const u32x4 raw = *reinterpret_cast<const u32x4*>(kt + row * G::ROWB + c * 16);
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const bf16x8 ka = eight_values(raw[2 * h], raw[2 * h + 1], scale);
-#pragma unroll
-                    for (int rb = 0; rb < RB; ++rb)
-                        s[tb][rb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ka, qf[rb][2 * p + h], s[tb][rb], 0, 0, 0);
-                }
-            }
-        } else {
-#pragma unroll
-            for (int ks = 0; ks < G::KS; ++ks) {
-                const int c = (ks * 4 + lg) ^ k_swz<G::ROWB>(row);
-                const bf16x8 ka = *reinterpret_cast<const bf16x8*>(kt + row * G::ROWB + c * 16);
-#pragma unroll
-                for (int rb = 0; rb < RB; ++rb)
-                    s[tb][rb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ka, qf[rb][ks], s[tb][rb], 0, 0, 0);
-            }
-        }
-    }
-}
-
-// The scales of V's tokens, four a block: those of this lane group.
-template <class G>
-__device__ __forceinline__ void value_scales(uint32_t (&vs)[G::TB], const char* sc, int lane)
-{
-    if (!G::QUANT) return;
-#pragma unroll
-    for (int tb = 0; tb < G::TB; ++tb) vs[tb] = *reinterpret_cast<const uint32_t*>(sc + G::TT + tb * 16 + (lane >> 4) * 4);
-}
-
-// Mask, online softmax; leaves P^T (in 8 bits: times V's scales) as the B operand of PV: slot j of lane group lg in step kk is token
-// 32 kk + 16 (j / 4) + 4 lg + j % 4, what this lane holds in s[2 kk + j / 4][.][j % 4].
-template <class G, int RB>
-__device__ __forceinline__ void softmax_tile(WaveState<G, RB>& st, floatx4 (&s)[G::TB][RB], bf16x8 (&pb)[G::TB / 2][RB],
-                                             const uint32_t (&vs)[G::TB], int t0, bool masked, const int (&lim)[RB], int end, float c, int lane)
-{
-    const int lg = lane >> 4;
-    float vscale[G::TB][4];
-    if (G::QUANT) {
-#pragma unroll
-        for (int tb = 0; tb < G::TB; ++tb)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) vscale[tb][i] = scale_value(vs[tb] >> (8 * i) & 0xffu);
-    }
-    if (masked) {
-#pragma unroll
-        for (int tb = 0; tb < G::TB; ++tb)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int tok = t0 + tb * 16 + lg * 4 + i;
-#pragma unroll
-                for (int rb = 0; rb < RB; ++rb)
-                    if (tok > lim[rb]) s[tb][rb][i] = -INFINITY;
-                if (G::QUANT && tok >= end) vscale[tb][i] = 0.f;       // a scale that belongs to no token may be anything
-            }
-    }
-    float alpha[RB];
-    bool changed = false;
-#pragma unroll
-    for (int rb = 0; rb < RB; ++rb) {
-        float mx = -INFINITY;
-#pragma unroll
-        for (int tb = 0; tb < G::TB; ++tb)
-            mx = fmaxf(mx, fmaxf(fmaxf(s[tb][rb][0], s[tb][rb][1]), fmaxf(s[tb][rb][2], s[tb][rb][3])));
-        mx = max_over_groups(mx);
-        const float m_new = (mx * c > st.m[rb] + kRescaleLog2) ? mx * c : st.m[rb];
-        const float m_use = (m_new == -INFINITY) ? 0.f : m_new;
-        alpha[rb] = fast_exp2(st.m[rb] - m_use);
-        changed |= (m_new != st.m[rb]);
-        st.m[rb] = m_new;
-        float sum = 0.f;
-#pragma unroll
-        for (int tb = 0; tb < G::TB; ++tb)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const float p = fast_exp2(fmaf(s[tb][rb][i], c, -m_use));
-                sum += p;
-                pb[tb / 2][rb][(tb & 1) * 4 + i] = (__bf16)(G::QUANT ? p * vscale[tb][i] : p);
-            }
-        st.l[rb] = st.l[rb] * alpha[rb] + sum;
-    }
-    if (__any(changed)) {
-#pragma unroll
-        for (int db = 0; db < G::DB; ++db)
-#pragma unroll
-            for (int rb = 0; rb < RB; ++rb)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) st.acc[db][rb][i] *= alpha[rb];
-    }
-}
-
-// What is not finite, in four codes or two bf16 values: all bits of such an element.
-template <bool QUANT>
-__device__ __forceinline__ uint32_t not_finite(uint32_t w)
-{
-    if (QUANT) {
-        const uint32_t nan = ((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;      // 0x7f + 1 carries into the sign's place
-        return (nan >> 7) * 0xffu;
-    }
-    return ((w & 0x7f80u) == 0x7f80u ? 0xffffu : 0u) | ((w & 0x7f800000u) == 0x7f800000u ? 0xffff0000u : 0u);
-}
-
-// O^T[column][row] += sum_token V[token][column] P[row][token].
-template <class G, int RB>
-__device__ __forceinline__ void pv_tile(WaveState<G, RB>& st, const bf16x8 (&pb)[G::TB / 2][RB], char* vt, int lane)
-{
-    const int ln = lane & 15, lg = lane >> 4;
-#pragma unroll
-    for (int kk = 0; kk < G::TB / 2; ++kk)
-#pragma unroll
-        for (int db = 0; db < G::DB; ++db) {
-            bf16x8 va;
-            if constexpr (G::QUANT) {
-                // eight rows of 16 codes: lane i of a group gives the address of row i / 2, half i % 2, and gets column i
-                const int r = ln >> 1, row = kk * 32 + (r >> 2) * 16 + lg * 4 + (r & 3);
-                const int c = db ^ v_swz<true, G::ROWB>(row);
-                const i32x2 w = __builtin_amdgcn_ds_read_tr8_b64_v2i32(
-                    (i32x2 __attribute__((address_space(3)))*)(vt + row * G::ROWB + c * 16 + (ln & 1) * 8));
-                va = eight_values((uint32_t)w[0], (uint32_t)w[1], 1.0f);
-            } else {
-                s16x4 half[2];
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const int row = kk * 32 + h * 16 + lg * 4 + (ln >> 2);
-                    const int c = (db * 2) ^ v_swz<false, G::ROWB>(row);
-                    half[h] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                        (s16x4 __attribute__((address_space(3)))*)(vt + row * G::ROWB + c * 16 + (ln & 3) * 8));
-                }
-                const s16x8 both = __builtin_shufflevector(half[0], half[1], 0, 1, 2, 3, 4, 5, 6, 7);
-                va = __builtin_bit_cast(bf16x8, both);
-            }
-#pragma unroll
-            for (int rb = 0; rb < RB; ++rb)
-                st.acc[db][rb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va, pb[kk][rb], st.acc[db][rb], 0, 0, 0);
-        }
-}
-
-// In a tile of which some rows do not attend some tokens, a weight of zero times a NaN or an infinity of V would be NaN.  Such elements
-// are taken out of the tile in LDS (true: there were any) and added in the end to the rows that attend their token, whose
-// positive weight does not change them.
-template <class G>
-__device__ __forceinline__ bool take_not_finite(char* vt, int lane)
-{
-    bool any = false;
-#pragma unroll 1
-    for (int x = 0; x < G::SLOT / 1024; ++x) {
-        u32x4* at = reinterpret_cast<u32x4*>(vt + x * 1024 + lane * 16);
-        u32x4 w = *at;
-        uint32_t bad = 0;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const uint32_t n = not_finite<G::QUANT>(w[i]);
-            w[i] &= ~n;
-            bad |= n;
-        }
-        if (bad) *at = w;
-        any |= bad != 0;
-    }
-    return __any(any);
-}
-template <class G, int RB, bool PAGED>
-__device__ __forceinline__ void add_not_finite(WaveState<G, RB>& st, const RowAddr& ra, int begin, int end, const int (&lim)[RB], int lane)
-{
-    const int lg = lane >> 4;
-#pragma unroll 1
-    for (int t = begin; t < end; ++t) {
-        const char* row = ra.v;
-        if (PAGED) row += (int64_t)min(max(ra.pages[t >> ra.page_shift], 0), ra.page_hi) * ra.page_bytes;
-        row += (uint32_t)(PAGED ? t & ra.page_mask : t) * ra.tok_bytes;
-#pragma unroll
-        for (int db = 0; db < G::DB; ++db) {
-            uint32_t bits[4];                            // columns 16 db + 4 lg .. + 3
-            if (G::QUANT) {
-                const uint32_t w = *reinterpret_cast<const uint32_t*>(row + db * 16 + lg * 4);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) bits[i] = (w >> (8 * i) & 0x7fu) == 0x7fu ? 0x7fc00000u : 0u;
-            } else {
-                const u32x2 w = *reinterpret_cast<const u32x2*>(row + db * 32 + lg * 8);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const uint32_t x = i & 1 ? w[i >> 1] & 0xffff0000u : w[i >> 1] << 16;
-                    bits[i] = (x & 0x7f800000u) == 0x7f800000u ? x : 0u;
-                }
-            }
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-#pragma unroll
-                for (int rb = 0; rb < RB; ++rb)
-                    if (bits[i] && t <= lim[rb]) st.acc[db][rb][i] += __uint_as_float(bits[i]);
-        }
-    }
-}
 
 // ---- one piece: tokens [c0, c1) of one (sequence, kv head)
 struct Piece {
@@ -480,7 +68,7 @@ __device__ __forceinline__ void run_piece(const StreamLaunch& a, const Piece& w,
     for (int rb = 0; rb < RB; ++rb) {
         const int row = row0 + rb * 16 + ln;
         const bool real = row < w.R;
-        lim[rb] = min(real ? w.L - w.Q + row / a.G : w.L - 1, w.c1 - 1);
+        lim[rb] = min(real && !a.shared ? w.L - w.Q + row / a.G : w.L - 1, w.c1 - 1);
 #pragma unroll
         for (int ks = 0; ks < G::KS; ++ks) {
             const int chunk = G::QUANT ? (ks >> 1) * 8 + 2 * lg + (ks & 1) : ks * 4 + lg;
@@ -498,7 +86,7 @@ __device__ __forceinline__ void run_piece(const StreamLaunch& a, const Piece& w,
         for (int db = 0; db < G::DB; ++db) st.acc[db][rb] = floatx4{0.f, 0.f, 0.f, 0.f};
     }
     const float c = a.scale_log2e;
-    const int first_masked_t0 = min(w.L - w.Q, w.c1) - (G::TT - 1);     // tiles from here on hold tokens that some row does not attend
+    const int first_masked_t0 = min(a.shared ? w.L : w.L - w.Q, w.c1) - (G::TT - 1);     // tiles from here on hold tokens that some row does not attend
     TilePages<G, PAGED> pages;
     bool taken = false;
 
@@ -720,21 +308,14 @@ __global__ void __launch_bounds__(G::NW * 64) attn_stream(StreamLaunch a)
     });
 }
 
-// One workgroup of D threads per (sequence, kv head, packed row): out = sum 2^(m_s - M) O_s / sum 2^(m_s - M) l_s, over the row's partials.
-template <int D>
-__global__ void __launch_bounds__(D) attn_stream_merge(StreamLaunch a)
+// The partials of one row: `n` of them, from row slot `slot` on, RP slots apart.
+struct Partials {
+    int n = 0;
+    int64_t slot = 0;
+};
+// Those of packed row `row` of sequence b, head h.
+__device__ __forceinline__ Partials find_partials(const StreamLaunch& a, int b, int h, int row, int lane)
 {
-    constexpr int SB = kMergeBlock;
-    const int row = blockIdx.x, h = blockIdx.y, b = blockIdx.z;
-    const int d = threadIdx.x, lane = d & 63;
-    const int Q = seq_queries(a, b), R = Q * a.G;
-    const int qi = row / a.G, hq = h * a.G + row % a.G;
-    uint16_t* dst = a.out + (((int64_t)b * a.Qmax + qi) * a.Hq + hq) * D + d;
-    if (row >= R) {                                       // query rows this sequence does not have
-        *dst = 0;
-        if (a.lse_out && d == 0) a.lse_out[((int64_t)b * a.Hq + hq) * a.Qmax + qi] = 0.f;
-        return;
-    }
     int before = 0, total = 0, cost = 0;
     for (int b0 = 0; b0 < a.B; b0 += 64) {
         const int mine = b0 + lane < a.B ? seq_cost(seq_len(a, b0 + lane), a.quantum) : 0;
@@ -745,25 +326,29 @@ __global__ void __launch_bounds__(D) attn_stream_merge(StreamLaunch a)
         }
         total = __builtin_amdgcn_readlane(end, 63);
     }
-    int ns = 0;
-    int64_t slot = 0;
+    Partials p;
     if (cost > 0) {
         const Shares sh(total, a.groups);
         const int g0 = sh.owner(before + kPieceQuanta), g1 = sh.owner(before + cost - 1);
-        ns = g1 - g0 + 1;
-        slot = ((int64_t)h * a.nslots + g0 + b) * a.RP + row;
+        p.n = g1 - g0 + 1;
+        p.slot = ((int64_t)(h * a.tiles + row / a.RP) * a.nslots + g0 + b) * a.RP + row % a.RP;
     }
-    RowMerge r;
-    float num = 0.f;
-    for (int s0 = 0; s0 < ns; s0 += SB) {
-        const int nb = min(SB, ns - s0), sl = d & (SB - 1);
-        const float* po = a.part_o + (slot + (int64_t)s0 * a.RP) * D + d;
+    return p;
+}
+// Folds them into the row's state and this thread's column.
+template <int D>
+__device__ __forceinline__ void fold_partials(const StreamLaunch& a, const Partials& p, int d, RowMerge& r, float& num)
+{
+    constexpr int SB = kMergeBlock;
+    for (int s0 = 0; s0 < p.n; s0 += SB) {
+        const int nb = min(SB, p.n - s0), sl = d & (SB - 1);
+        const float* po = a.part_o + (p.slot + (int64_t)s0 * a.RP) * D + d;
         float o[SB];
 #pragma unroll
         for (int j = 0; j < SB; ++j) o[j] = j < nb ? po[(int64_t)j * a.RP * D] : 0.f;
         float ms = -INFINITY, ls = 0.f;
         if (sl < nb) {
-            const float* ml = a.part_ml + (slot + (int64_t)(s0 + sl) * a.RP) * 2;
+            const float* ml = a.part_ml + (p.slot + (int64_t)(s0 + sl) * a.RP) * 2;
             ms = ml[0];
             ls = ml[1];
         }
@@ -776,6 +361,30 @@ __global__ void __launch_bounds__(D) attn_stream_merge(StreamLaunch a)
             acc1 = fmaf(lane_of(w, j + 1), o[j + 1], acc1);
         }
         num = num * resc + (acc0 + acc1);
+    }
+}
+
+// One workgroup of D threads per (sequence, kv head, packed row): out = sum 2^(m_s - M) O_s / sum 2^(m_s - M) l_s, over the row's partials of the
+// prefix and of its own tokens.
+template <int D, bool PREFIX>
+__global__ void __launch_bounds__(D) attn_stream_merge(StreamLaunch a, StreamLaunch prefix)
+{
+    const int row = blockIdx.x, h = blockIdx.y, b = blockIdx.z;
+    const int d = threadIdx.x, lane = d & 63;
+    const int R = seq_queries(a, b) * a.G;
+    const int qi = row / a.G, hq = h * a.G + row % a.G;
+    uint16_t* dst = a.out + (((int64_t)b * a.Qmax + qi) * a.Hq + hq) * D + d;
+    if (row >= R) {                                       // query rows this sequence does not have
+        *dst = 0;
+        if (a.lse_out && d == 0) a.lse_out[((int64_t)b * a.Hq + hq) * a.Qmax + qi] = 0.f;
+        return;
+    }
+    RowMerge r;
+    float num = 0.f;
+    const Partials own = find_partials(a, b, h, row, lane);
+    if (own.n) {                                          // else a sequence without tokens
+        if (PREFIX) fold_partials<D>(prefix, find_partials(prefix, 0, h, b * a.Qmax * a.G + row, lane), d, r, num);
+        fold_partials<D>(a, own, d, r, num);
     }
     const __bf16 o = (__bf16)(r.den == 0.f ? 0.f : num / r.den);
     *dst = __builtin_bit_cast(uint16_t, o);
@@ -828,6 +437,7 @@ void plan_attn_stream(StreamLaunch& a, int n_cu)
 {
     const int rb = (a.Qmax * a.G + 15) / 16;
     a.RP = rb * 16;
+    a.tiles = 1;
     a.groups = n_cu > a.Hkv ? n_cu / a.Hkv : 1;          // a workgroup takes a compute unit's LDS
     // no more shares than the longest possible batch has quanta
     (void)with_geo(a.D, a.own.ks != nullptr, rb, [&](auto geo) {
@@ -843,13 +453,13 @@ void plan_attn_stream(StreamLaunch& a, int n_cu)
 
 size_t attn_stream_workspace_bytes(const StreamLaunch& a)
 {
-    const size_t rows = (size_t)a.Hkv * a.nslots * a.RP;
+    const size_t rows = (size_t)a.Hkv * a.tiles * a.nslots * a.RP;
     return (rows * a.D * 4 + 255) / 256 * 256 + (rows * 8 + 255) / 256 * 256;
 }
 
 void bind_attn_stream(StreamLaunch& a, void* workspace)
 {
-    const size_t rows = (size_t)a.Hkv * a.nslots * a.RP;
+    const size_t rows = (size_t)a.Hkv * a.tiles * a.nslots * a.RP;
     a.part_o = static_cast<float*>(workspace);
     a.part_ml = reinterpret_cast<float*>(static_cast<char*>(workspace) + (rows * a.D * 4 + 255) / 256 * 256);
 }
@@ -864,9 +474,10 @@ hipError_t launch_attn_stream(const StreamLaunch& a, hipStream_t stream)
     });
 }
 
-hipError_t launch_attn_stream_merge(const StreamLaunch& a, hipStream_t stream)
+hipError_t launch_attn_stream_merge(const StreamLaunch& a, const StreamLaunch& prefix, hipStream_t stream)
 {
-    auto fn = a.D == 128 ? attn_stream_merge<128> : attn_stream_merge<64>;
-    hipLaunchKernelGGL(fn, dim3(a.Qmax * a.G, a.Hkv, a.B), dim3(a.D), 0, stream, a);
+    auto fn = prefix.part_o ? (a.D == 128 ? attn_stream_merge<128, true> : attn_stream_merge<64, true>)
+                            : (a.D == 128 ? attn_stream_merge<128, false> : attn_stream_merge<64, false>);
+    hipLaunchKernelGGL(fn, dim3(a.Qmax * a.G, a.Hkv, a.B), dim3(a.D), 0, stream, a, prefix);
     return hipGetLastError();
 }

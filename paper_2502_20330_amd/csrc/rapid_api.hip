@@ -304,27 +304,6 @@ int check_prefix_place(const rapid_attn_shape* s, const rapid_prefix_layout* p, 
     return p->token_stride * 2 * p->max_prefix < (int64_t)1 << 32 ? RAPID_OK : RAPID_EUNSUPPORTED;
 }
 
-AttnRowsLaunch rows_launch(const rapid_attn_shape* s, const void* q, const int32_t* ctx_lens, const int32_t* gammas, void* out,
-                           float* lse_out)
-{
-    AttnRowsLaunch a{};
-    a.q = static_cast<const uint16_t*>(q);
-    a.out = static_cast<uint16_t*>(out);
-    a.lse_out = lse_out;
-    a.ctx_lens = ctx_lens;
-    a.gammas = gammas;
-    a.B = s->batch;
-    a.Qmax = s->q_max;
-    a.Hq = s->n_q_heads;
-    a.Hkv = s->n_kv_heads;
-    a.G = a.Hq / a.Hkv;
-    a.D = s->head_dim;
-    a.gamma = s->gamma;
-    a.max_ctx = s->max_ctx;
-    a.scale_log2e = s->softmax_scale * 1.4426950408889634f;
-    return a;
-}
-
 // The streaming kernel's plan for a shape.
 StreamLaunch stream_launch(const rapid_ctx* ctx, const rapid_attn_shape* s, const AttnSource& own)
 {
@@ -340,6 +319,26 @@ StreamLaunch stream_launch(const rapid_ctx* ctx, const rapid_attn_shape* s, cons
     a.max_ctx = s->max_ctx;
     a.scale_log2e = s->softmax_scale * 1.4426950408889634f;
     plan_attn_stream(a, ctx && ctx->n_cu > 0 ? ctx->n_cu : 256);
+    return a;
+}
+// And for the rows of all its sequences over the shared prefix at `source`.
+StreamLaunch prefix_launch(const rapid_ctx* ctx, const rapid_attn_shape* s, int max_prefix, const AttnSource& source)
+{
+    StreamLaunch a{};
+    a.own = source;
+    a.shared = 1;
+    a.B = 1;
+    a.Qmax = s->batch * s->q_max;
+    a.Hq = s->n_q_heads;
+    a.Hkv = s->n_kv_heads;
+    a.G = a.Hq / a.Hkv;
+    a.D = s->head_dim;
+    a.gamma = a.Qmax - 1;
+    a.max_ctx = max_prefix;
+    a.scale_log2e = s->softmax_scale * 1.4426950408889634f;
+    const int n_cu = ctx && ctx->n_cu > 0 ? ctx->n_cu : 256;
+    if (a.Qmax * a.G > kStreamRows) plan_attn_prefix(a, n_cu);
+    else plan_attn_stream(a, n_cu);
     return a;
 }
 
@@ -367,6 +366,7 @@ int rapid_create(rapid_ctx** out, int device)
     hipError_t ec = configure_verify_attn();
     if (ec == hipSuccess) ec = configure_lm_head();
     if (ec == hipSuccess) ec = configure_attn_stream();
+    if (ec == hipSuccess) ec = configure_attn_prefix();
     if (ec == hipSuccess) ec = configure_hbm_read_probe();
     void* scratch_ptr = nullptr;                      // this device's copy of `scratch`
     if (ec == hipSuccess) ec = hipGetSymbolAddress(&scratch_ptr, HIP_SYMBOL(scratch));
@@ -890,14 +890,16 @@ int rapid_verify_attn_quant(rapid_ctx* ctx, const rapid_attn_shape* shape, const
     DeviceScope dev(ctx->device);
     if (dev.err != hipSuccess) return hip_fail(ctx, dev.err);
     hipError_t e = launch_attn_stream(a, static_cast<hipStream_t>(stream));
-    if (e == hipSuccess) e = launch_attn_stream_merge(a, static_cast<hipStream_t>(stream));
+    if (e == hipSuccess) e = launch_attn_stream_merge(a, StreamLaunch{}, static_cast<hipStream_t>(stream));
     if (e != hipSuccess) return hip_fail(ctx, e);
     return RAPID_OK;
 }
 
-size_t rapid_verify_attn_prefix_workspace_bytes(const rapid_ctx*, const rapid_attn_shape* shape, const rapid_prefix_layout* prefix)
+size_t rapid_verify_attn_prefix_workspace_bytes(const rapid_ctx* ctx, const rapid_attn_shape* shape, const rapid_prefix_layout* prefix)
 {
-    return check_prefix_shape(shape, prefix) == RAPID_OK ? 256 : 0;
+    if (check_prefix_shape(shape, prefix) != RAPID_OK) return 0;
+    const size_t own = attn_stream_workspace_bytes(stream_launch(ctx, shape, AttnSource{}));
+    return prefix->max_prefix ? own + attn_stream_workspace_bytes(prefix_launch(ctx, shape, prefix->max_prefix, AttnSource{})) : own;
 }
 
 int rapid_verify_attn_prefix(rapid_ctx* ctx, const rapid_attn_shape* shape, const rapid_prefix_layout* prefix, const void* q,
@@ -916,24 +918,41 @@ int rapid_verify_attn_prefix(rapid_ctx* ctx, const rapid_attn_shape* shape, cons
     if (rc != RAPID_OK) return rc;
     if (!aligned(q, 16) || !aligned(k_cache, 16) || !aligned(v_cache, 16) || !aligned(k_prefix, 16) || !aligned(v_prefix, 16) ||
         !aligned(out, 16)) return RAPID_EALIGN;
-    if (!workspace || !aligned(workspace, 256) || workspace_bytes < rapid_verify_attn_prefix_workspace_bytes(ctx, shape, prefix))
-        return RAPID_EWORKSPACE;
-    AttnRowsLaunch a = rows_launch(shape, q, ctx_lens, gammas, out, lse_out);
-    a.own = source_of(shape, k_cache, v_cache, page_table);
-    a.prefix_len = prefix_len;
-    a.max_prefix = prefix->max_prefix;
-    if (prefix_table) {
-        a.prefix = source_of(shape, k_cache, v_cache, prefix_table);
-        a.prefix.max_pages = prefix->max_pages;
-    } else {
-        a.prefix.k = k_prefix;
-        a.prefix.v = v_prefix;
-        a.prefix.tstride = prefix->token_stride;
-        a.prefix.hstride = prefix->head_stride;
+    StreamLaunch a = stream_launch(ctx, shape, source_of(shape, k_cache, v_cache, page_table));
+    StreamLaunch p{};
+    if (prefix->max_prefix) {
+        AttnSource source{};
+        if (prefix_table) {
+            source = source_of(shape, k_cache, v_cache, prefix_table);
+            source.max_pages = prefix->max_pages;
+        } else {
+            source.k = k_prefix;
+            source.v = v_prefix;
+            source.tstride = prefix->token_stride;
+            source.hstride = prefix->head_stride;
+        }
+        p = prefix_launch(ctx, shape, prefix->max_prefix, source);
     }
+    const size_t own_bytes = attn_stream_workspace_bytes(a), need = own_bytes + (prefix->max_prefix ? attn_stream_workspace_bytes(p) : 0);
+    if (!workspace || !aligned(workspace, 256) || workspace_bytes < need) return RAPID_EWORKSPACE;
+    bind_attn_stream(a, workspace);
+    a.q = static_cast<const uint16_t*>(q);
+    a.out = static_cast<uint16_t*>(out);
+    a.lse_out = lse_out;
+    a.ctx_lens = ctx_lens;
+    a.gammas = gammas;
+    hipStream_t st = static_cast<hipStream_t>(stream);
     DeviceScope dev(ctx->device);
     if (dev.err != hipSuccess) return hip_fail(ctx, dev.err);
-    hipError_t e = launch_attn_rows(a, static_cast<hipStream_t>(stream));
+    hipError_t e = hipSuccess;
+    if (prefix->max_prefix) {
+        bind_attn_stream(p, static_cast<char*>(workspace) + own_bytes);
+        p.q = a.q;
+        p.ctx_lens = prefix_len;
+        e = p.Qmax * p.G > kStreamRows ? launch_attn_prefix(p, st) : launch_attn_stream(p, st);
+    }
+    if (e == hipSuccess) e = launch_attn_stream(a, st);
+    if (e == hipSuccess) e = launch_attn_stream_merge(a, p, st);
     if (e != hipSuccess) return hip_fail(ctx, e);
     return RAPID_OK;
 }

@@ -166,30 +166,6 @@ struct KvQuantLaunch {
 hipError_t launch_kv_append_quant(const KvQuantLaunch& a, hipStream_t stream);
 hipError_t launch_kv_read_quant(const KvQuantLaunch& a, hipStream_t stream);
 
-// ---- attention over a cache in 8 bits, and behind a shared prefix (attn_rows.hip)
-struct AttnSource {             // where keys and values lie; strides in elements
-    const void* k;
-    const void* v;
-    const uint8_t* ks;          // scales, or null (bf16)
-    const uint8_t* vs;
-    const int32_t* page_table;  // or null: contiguous
-    int64_t bstride, tstride, hstride, pstride;
-    int64_t sbstride, shstride, spstride;
-    int32_t page_shift, page_mask, max_pages, page_hi;
-};
-struct AttnRowsLaunch {
-    const uint16_t* q;
-    uint16_t* out;
-    float* lse_out;
-    const int32_t* ctx_lens;
-    const int32_t* gammas;
-    const int32_t* prefix_len;  // or null: no prefix
-    AttnSource own, prefix;
-    int32_t B, Qmax, Hq, Hkv, G, D, gamma, max_ctx, max_prefix;
-    float scale_log2e;
-};
-hipError_t launch_attn_rows(const AttnRowsLaunch& a, hipStream_t stream);
-
 // ---- retrieval chunk selection (retrieve.hip)
 struct RetrieveLaunch {
     const float* emb;       // [n][dim]
