@@ -195,6 +195,7 @@ class Rapid:
         self._ws_args = (None, 0, None, 0)             # address and size of the exchange memory and of the workspace, as a call takes them
         self._ws_accept: Optional[torch.Tensor] = None
         self._ws_shared: list = []                     # workspaces of the quantised and the prefix attention, the last one in use
+        self._plans: dict = {}                         # shapes and layouts of calls by their sizes (_planned)
         self._sink: Optional[torch.Tensor] = None
 
     def close(self):
@@ -410,17 +411,27 @@ class Rapid:
         return rel, cnt
 
     # ------------------------------------------------------------------ cache in 8 bits, shared prefix
-    def _need(self, ok, what: str):
+    def _planned(self, kind: str, scalars, tensors, plan):
+        """What a call of these sizes, strides, types and devices needs besides addresses: plan() checks them and answers, once for
+        each such call (the checks took three times as long as the rest of a small call)."""
+        key = (kind, scalars, tuple([None if t is None else (t.shape, t.stride(), t.dtype, t.device) for t in tensors]))
+        got = self._plans.get(key)
+        if got is None:
+            for t in tensors:
+                self._need(t is None or t.device == self.device, f"a tensor is not on {self.device}")
+            got = plan()
+            if len(self._plans) >= 1024:                       # sizes that change all the time
+                self._plans.clear()
+            self._plans[key] = got
+        return got
+
+    @staticmethod
+    def _need(ok, what: str):
         if not ok:
             raise RapidError(RAPID_EINVAL, what)
 
-    def _on_device(self, **tensors):
-        for name, t in tensors.items():
-            self._need(t is None or t.device == self.device, f"{name} is not on {self.device}")
-
-    def _lengths(self, batch: int, ctx_lens, gammas, page_table):
-        """Checks of the index arrays that the calls on a batch share."""
-        self._on_device(ctx_lens=ctx_lens, gammas=gammas, page_table=page_table)
+    def _check_lengths(self, batch: int, ctx_lens, gammas, page_table):
+        """The index arrays that the calls on a batch share."""
         self._need(ctx_lens.dtype == torch.int32 and ctx_lens.shape == (batch,) and ctx_lens.is_contiguous(),
                    "ctx_lens: int32 [B], contiguous")
         self._need(gammas is None or (gammas.dtype == torch.int32 and gammas.shape == (batch,) and gammas.is_contiguous()),
@@ -429,12 +440,19 @@ class Rapid:
                                           page_table.shape[0] == batch and page_table.is_contiguous()),
                    "page_table: int32 [B, max_pages], contiguous")
 
+    def _check_attn(self, q, out, lse_out):
+        """q and the outputs of an attention call."""
+        self._need(q.dtype == torch.bfloat16 and q.dim() == 4 and q.is_contiguous(), "q: bf16 [B, Qmax, Hq, d], contiguous")
+        self._need(out.dtype == torch.bfloat16 and out.shape == q.shape and out.is_contiguous(), "out: bf16 like q, contiguous")
+        self._need(lse_out is None or (lse_out.dtype == torch.float32 and lse_out.is_contiguous() and
+                                       lse_out.shape == (q.shape[0], q.shape[2], q.shape[1])),
+                   "lse_out: fp32 [B, Hq, Qmax], contiguous")
+
     def _quant_shape(self, batch, q_max, hq, gamma, k_codes, v_codes, k_scales, v_scales, page_table, max_ctx, softmax_scale):
-        """(AttnShape, QuantLayout) of a cache in 8 bits: codes [B or pages, tokens, Hkv, d] with any outer strides, scales
+        """References to the AttnShape and QuantLayout of a cache in 8 bits: codes [B or pages, tokens, Hkv, d] with any outer strides, scales
         [B or pages, Hkv, tokens], tokens contiguous and the rows a multiple of 16 long (views of memory that goes on are fine)."""
         one_byte = (torch.float8_e4m3fn, torch.uint8)
         scale_byte = (torch.float8_e8m0fnu, torch.uint8)
-        self._on_device(k_codes=k_codes, v_codes=v_codes, k_scales=k_scales, v_scales=v_scales)
         self._need(k_codes.dtype in one_byte and v_codes.dtype in one_byte, "codes: float8_e4m3fn or uint8")
         self._need(k_scales.dtype in scale_byte and v_scales.dtype in scale_byte, "scales: float8_e8m0fnu or uint8")
         self._need(k_codes.dim() == 4 and k_codes.shape == v_codes.shape and _strides(k_codes) == _strides(v_codes),
@@ -451,11 +469,11 @@ class Rapid:
             ctx_max = tokens if max_ctx is None else int(max_ctx)
             self._need(rows == batch and ctx_max <= tokens, "the cache holds fewer sequences or tokens than the call names")
             self._need(k_scales.shape[2] >= -(-ctx_max // 16) * 16, "rows of scales: max_ctx rounded up to a multiple of 16")
-            return (AttnShape(batch, q_max, hq, hkv, d, ctx_max, gamma, scale, st[0], st[1], st[2], 0, 0, 0, 0, 0, 0),
-                    QuantLayout(ss[0], ss[1], 0))
+            shape = AttnShape(batch, q_max, hq, hkv, d, ctx_max, gamma, scale, st[0], st[1], st[2], 0, 0, 0, 0, 0, 0)
+            return ctypes.byref(shape), ctypes.byref(QuantLayout(ss[0], ss[1], 0))
         ctx_max = page_table.shape[1] * tokens if max_ctx is None else int(max_ctx)
-        return (AttnShape(batch, q_max, hq, hkv, d, ctx_max, gamma, scale, 0, st[1], st[2], st[0], tokens, page_table.shape[1],
-                          0, rows, 0), QuantLayout(0, ss[1], ss[0]))
+        shape = AttnShape(batch, q_max, hq, hkv, d, ctx_max, gamma, scale, 0, st[1], st[2], st[0], tokens, page_table.shape[1], 0, rows, 0)
+        return ctypes.byref(shape), ctypes.byref(QuantLayout(0, ss[1], ss[0]))
 
     def _shared_workspace(self, nbytes: int) -> torch.Tensor:
         # grows only, and what it has outgrown is kept: a captured graph goes on using the one that it was recorded with
@@ -470,13 +488,15 @@ class Rapid:
         every sequence (ctx_lens counts them).  k_codes/v_codes: float8_e4m3fn or uint8 [B,Lmax,Hkv,d] (any batch/token/head
         strides) or, with page_table, [n_pages,page,Hkv,d]; k_scales/v_scales: float8_e8m0fnu or uint8 [B,Hkv,Lmax] or
         [n_pages,Hkv,page], rows of a multiple of 16."""
-        self._need(k_new.dim() == 4 and k_new.shape == v_new.shape and k_new.is_contiguous() and v_new.is_contiguous()
-                   and k_new.dtype == torch.bfloat16 and v_new.dtype == torch.bfloat16, "k_new and v_new: bf16 [B, Qmax, Hkv, d], contiguous")
-        self._need(k_new.shape[2:] == k_codes.shape[2:], "k_new and the cache differ in heads or head_dim")
-        self._on_device(k_new=k_new, v_new=v_new)
-        self._lengths(k_new.shape[0], ctx_lens, gammas, page_table)
-        shape, layout = self._quant_shape(k_new.shape[0], k_new.shape[1], k_new.shape[2], gamma, k_codes, v_codes, k_scales, v_scales,
-                                          page_table, max_ctx, 1.0)
+        def plan():
+            self._need(k_new.dim() == 4 and k_new.shape == v_new.shape and k_new.is_contiguous() and v_new.is_contiguous()
+                       and k_new.dtype == torch.bfloat16 and v_new.dtype == torch.bfloat16,
+                       "k_new and v_new: bf16 [B, Qmax, Hkv, d], contiguous")
+            self._need(k_new.shape[2:] == k_codes.shape[2:], "k_new and the cache differ in heads or head_dim")
+            self._check_lengths(k_new.shape[0], ctx_lens, gammas, page_table)
+            return self._quant_shape(*k_new.shape[:3], gamma, k_codes, v_codes, k_scales, v_scales, page_table, max_ctx, 1.0)
+        shape, layout = self._planned("append", (gamma, max_ctx), (k_codes, v_codes, k_scales, v_scales, k_new, v_new, ctx_lens, gammas,
+                                                                   page_table), plan)
         rc = self.lib.rapid_kv_append_quant(self._ctx, shape, layout, k_new.data_ptr(), v_new.data_ptr(), ctx_lens.data_ptr(),
                                             _dptr(gammas), _dptr(page_table), k_codes.data_ptr(), v_codes.data_ptr(),
                                             k_scales.data_ptr(), v_scales.data_ptr(), _stream_ptr(self.device))
@@ -487,55 +507,57 @@ class Rapid:
                             gammas=None, page_table=None, max_ctx: Optional[int] = None, outs=None):
         """The last gamma_b+1 tokens of every sequence (gamma_b < rows) as bf16: (k, v) [B,rows,Hkv,d], zeros past a sequence's
         rows.  Cache as for :meth:`rapid_kv_append_quant`; `outs`: two tensors to write to."""
-        batch, (hkv, d) = ctx_lens.numel(), k_codes.shape[2:]
-        self._lengths(batch, ctx_lens, gammas, page_table)
-        shape, layout = self._quant_shape(batch, int(rows), hkv, gamma, k_codes, v_codes, k_scales, v_scales, page_table, max_ctx, 1.0)
         if outs is None:
-            outs = tuple(torch.empty((batch, rows, hkv, d), dtype=torch.bfloat16, device=self.device) for _ in range(2))
-        for t in outs:
-            self._on_device(outs=t)
-            self._need(t.dtype == torch.bfloat16 and t.shape == (batch, rows, hkv, d) and t.is_contiguous(),
+            shape = (ctx_lens.numel(), int(rows), *k_codes.shape[2:])
+            outs = tuple(torch.empty(shape, dtype=torch.bfloat16, device=self.device) for _ in range(2))
+        k_out, v_out = outs
+
+        def plan():
+            batch, (hkv, d) = ctx_lens.numel(), k_codes.shape[2:]
+            self._need(all(t.dtype == torch.bfloat16 and t.shape == (batch, rows, hkv, d) and t.is_contiguous() for t in outs),
                        "outs: two of bf16 [B, rows, Hkv, d], contiguous")
+            self._check_lengths(batch, ctx_lens, gammas, page_table)
+            return self._quant_shape(batch, int(rows), hkv, gamma, k_codes, v_codes, k_scales, v_scales, page_table, max_ctx, 1.0)
+        shape, layout = self._planned("read", (rows, gamma, max_ctx), (k_codes, v_codes, k_scales, v_scales, k_out, v_out, ctx_lens, gammas,
+                                                                       page_table), plan)
         rc = self.lib.rapid_kv_read_quant(self._ctx, shape, layout, k_codes.data_ptr(), v_codes.data_ptr(), k_scales.data_ptr(),
                                           v_scales.data_ptr(), ctx_lens.data_ptr(), _dptr(gammas), _dptr(page_table),
-                                          outs[0].data_ptr(), outs[1].data_ptr(), _stream_ptr(self.device))
+                                          k_out.data_ptr(), v_out.data_ptr(), _stream_ptr(self.device))
         if rc:
             _check(self.lib, rc, self._ctx)
         return outs
 
-    def _attn_tensors(self, q, out, lse_out):
-        """Checks q [B,Qmax,Hq,d] and the outputs of an attention call; returns `out`."""
-        self._need(q.dtype == torch.bfloat16 and q.dim() == 4 and q.is_contiguous(), "q: bf16 [B, Qmax, Hq, d], contiguous")
-        if out is None:
-            out = torch.empty_like(q)
-        self._on_device(q=q, out=out, lse_out=lse_out)
-        self._need(out.dtype == torch.bfloat16 and out.shape == q.shape and out.is_contiguous(), "out: bf16 like q, contiguous")
-        self._need(lse_out is None or (lse_out.dtype == torch.float32 and lse_out.is_contiguous() and
-                                       lse_out.shape == (q.shape[0], q.shape[2], q.shape[1])),
-                   "lse_out: fp32 [B, Hq, Qmax], contiguous")
-        return out
+    def _attn_with_workspace(self, call, need, args, tail):
+        """An attention call on the shared workspace, which grows where it is too small: that is the call's last check, nothing has been
+        launched then."""
+        ws = self._ws_shared[-1] if self._ws_shared else None
+        rc = call(*args, _dptr(ws), 0 if ws is None else ws.numel(), tail)
+        if rc == RAPID_EWORKSPACE:
+            ws = self._shared_workspace(need())
+            rc = call(*args, ws.data_ptr(), ws.numel(), tail)
+        if rc:
+            _check(self.lib, rc, self._ctx)
 
     def rapid_verify_attn_quant(self, q, k_codes, v_codes, k_scales, v_scales, ctx_lens, gamma: Optional[int] = None, *, gammas=None,
                                 page_table=None, max_ctx: Optional[int] = None, softmax_scale: Optional[float] = None,
                                 out=None, lse_out=None):
         """:meth:`rapid_verify_attn` on a cache in 8 bits (layout: :meth:`rapid_kv_append_quant`): q bf16 [B,Qmax,Hq,d]; returns
         out bf16 [B,Qmax,Hq,d] and fills lse_out fp32 [B,Hq,Qmax] if given.  One position (Qmax = 1) is a decode step."""
-        out = self._attn_tensors(q, out, lse_out)
-        self._need(q.shape[3] == k_codes.shape[3], "q and the cache differ in head_dim")
-        self._lengths(q.shape[0], ctx_lens, gammas, page_table)
-        shape, layout = self._quant_shape(q.shape[0], q.shape[1], q.shape[2], gamma, k_codes, v_codes, k_scales, v_scales, page_table,
-                                          max_ctx, softmax_scale)
-        ws = self._ws_shared[-1] if self._ws_shared else None
-        for _ in range(2):
-            rc = self.lib.rapid_verify_attn_quant(self._ctx, shape, layout, q.data_ptr(), k_codes.data_ptr(), v_codes.data_ptr(),
-                                                  k_scales.data_ptr(), v_scales.data_ptr(), ctx_lens.data_ptr(), _dptr(gammas),
-                                                  _dptr(page_table), out.data_ptr(), _dptr(lse_out), _dptr(ws),
-                                                  0 if ws is None else ws.numel(), _stream_ptr(self.device))
-            if rc != RAPID_EWORKSPACE:                         # the last check of the call: nothing has been launched
-                break
-            ws = self._shared_workspace(self.lib.rapid_verify_attn_quant_workspace_bytes(self._ctx, shape))
-        if rc:
-            _check(self.lib, rc, self._ctx)
+        if out is None:
+            out = torch.empty_like(q)
+
+        def plan():
+            self._check_attn(q, out, lse_out)
+            self._need(q.shape[3] == k_codes.shape[3], "q and the cache differ in head_dim")
+            self._check_lengths(q.shape[0], ctx_lens, gammas, page_table)
+            return self._quant_shape(*q.shape[:3], gamma, k_codes, v_codes, k_scales, v_scales, page_table, max_ctx, softmax_scale)
+        shape, layout = self._planned("attn", (gamma, max_ctx, softmax_scale),
+                                      (q, k_codes, v_codes, k_scales, v_scales, ctx_lens, gammas, page_table, out, lse_out), plan)
+        self._attn_with_workspace(self.lib.rapid_verify_attn_quant,
+                                  lambda: self.lib.rapid_verify_attn_quant_workspace_bytes(self._ctx, shape),
+                                  (self._ctx, shape, layout, q.data_ptr(), k_codes.data_ptr(), v_codes.data_ptr(),
+                                   k_scales.data_ptr(), v_scales.data_ptr(), ctx_lens.data_ptr(), _dptr(gammas), _dptr(page_table),
+                                   out.data_ptr(), _dptr(lse_out)), _stream_ptr(self.device))
         return out
 
     def rapid_verify_attn_prefix(self, q, k_cache, v_cache, ctx_lens, prefix_len, gamma: Optional[int] = None, *, k_prefix=None,
@@ -545,51 +567,54 @@ class Rapid:
         [1] (device); the prefix is k_prefix/v_prefix bf16 [P,Hkv,d] (any token/head strides) or, with page_table, pages of
         k_cache/v_cache that prefix_table int32 [max_pages] names; max_prefix bounds prefix_len on the host (default: what is
         given).  ctx_lens counts a sequence's own tokens, which k_cache/v_cache hold as for rapid_verify_attn."""
-        out = self._attn_tensors(q, out, lse_out)
-        self._lengths(q.shape[0], ctx_lens, gammas, page_table)
-        self._on_device(k_cache=k_cache, v_cache=v_cache, prefix_len=prefix_len, k_prefix=k_prefix, v_prefix=v_prefix,
-                        prefix_table=prefix_table)
+        if out is None:
+            out = torch.empty_like(q)
+        shape, prefix = self._planned(
+            "prefix", (gamma, max_prefix, max_ctx, softmax_scale),
+            (q, k_cache, v_cache, ctx_lens, prefix_len, k_prefix, v_prefix, prefix_table, gammas, page_table, out, lse_out),
+            lambda: self._prefix_shape(q, k_cache, v_cache, ctx_lens, prefix_len, gamma, k_prefix, v_prefix, prefix_table, max_prefix,
+                                       gammas, page_table, max_ctx, softmax_scale, out, lse_out))
+        self._attn_with_workspace(self.lib.rapid_verify_attn_prefix,
+                                  lambda: self.lib.rapid_verify_attn_prefix_workspace_bytes(self._ctx, shape, prefix),
+                                  (self._ctx, shape, prefix, q.data_ptr(), _dptr(k_prefix), _dptr(v_prefix), prefix_len.data_ptr(),
+                                   _dptr(prefix_table), k_cache.data_ptr(), v_cache.data_ptr(), ctx_lens.data_ptr(), _dptr(gammas),
+                                   _dptr(page_table), out.data_ptr(), _dptr(lse_out)), _stream_ptr(self.device))
+        return out
+
+    def _prefix_shape(self, q, k_cache, v_cache, ctx_lens, prefix_len, gamma, k_prefix, v_prefix, prefix_table, max_prefix, gammas,
+                      page_table, max_ctx, softmax_scale, out, lse_out):
+        self._check_attn(q, out, lse_out)
+        self._check_lengths(q.shape[0], ctx_lens, gammas, page_table)
         self._need(k_cache.dtype == torch.bfloat16 and v_cache.dtype == torch.bfloat16 and k_cache.dim() == 4
-                   and k_cache.shape == v_cache.shape and k_cache.stride() == v_cache.stride(),
-                   "k_cache and v_cache: bf16 [B or pages, tokens, Hkv, d], the same sizes and strides")
+                   and k_cache.shape == v_cache.shape and _strides(k_cache) == _strides(v_cache) and k_cache.stride(3) == 1,
+                   "k_cache and v_cache: bf16 [B or pages, tokens, Hkv, d], d contiguous, the same sizes and strides")
         self._need(k_cache.shape[3] == q.shape[3], "q and the cache differ in head_dim")
         self._need(prefix_len.dtype == torch.int32 and prefix_len.numel() == 1, "prefix_len: int32 [1]")
-        tokens = k_cache.shape[1]
+        (rows, tokens, hkv, d), st = k_cache.shape, _strides(k_cache)
+        gamma = q.shape[1] - 1 if gamma is None else int(gamma)
+        scale = d ** -0.5 if softmax_scale is None else float(softmax_scale)
         if page_table is None:
-            self._need(k_cache.shape[0] == q.shape[0] and (max_ctx is None or max_ctx <= tokens),
-                       "the cache holds fewer sequences or tokens than the call names")
-        if max_ctx is None:
-            max_ctx = tokens if page_table is None else page_table.shape[1] * tokens
-        shape = self.attn_shape(q, k_cache, max_ctx, gamma=gamma, page_table=page_table, softmax_scale=softmax_scale)
+            ctx_max = tokens if max_ctx is None else int(max_ctx)
+            self._need(rows == q.shape[0] and ctx_max <= tokens, "the cache holds fewer sequences or tokens than the call names")
+            shape = AttnShape(*q.shape[:3], hkv, d, ctx_max, gamma, scale, st[0], st[1], st[2], 0, 0, 0, 0, 0, 0)
+        else:
+            ctx_max = page_table.shape[1] * tokens if max_ctx is None else int(max_ctx)
+            shape = AttnShape(*q.shape[:3], hkv, d, ctx_max, gamma, scale, 0, st[1], st[2], st[0], tokens, page_table.shape[1], 0, rows, 0)
         if prefix_table is not None:
             self._need(page_table is not None and k_prefix is None and v_prefix is None,
                        "prefix_table names pages of a paged cache, in the place of k_prefix and v_prefix")
             self._need(prefix_table.dtype == torch.int32 and prefix_table.dim() == 1 and prefix_table.is_contiguous(),
                        "prefix_table: int32 [max_pages], contiguous")
             n = prefix_table.numel()
-            prefix = PrefixLayout(n * tokens if max_prefix is None else int(max_prefix), n, 0, 0)
-        else:
-            self._need(k_prefix is not None and v_prefix is not None and k_prefix.dtype == torch.bfloat16
-                       and v_prefix.dtype == torch.bfloat16 and k_prefix.dim() == 3 and k_prefix.shape == v_prefix.shape
-                       and k_prefix.stride() == v_prefix.stride() and k_prefix.stride(2) == 1
-                       and k_prefix.shape[1:] == k_cache.shape[2:],
-                       "k_prefix and v_prefix: bf16 [P, Hkv, d] as the cache's, the same sizes and strides")
-            n = k_prefix.shape[0]
-            self._need(max_prefix is None or max_prefix <= n, "the prefix holds fewer tokens than max_prefix")
-            prefix = PrefixLayout(n if max_prefix is None else int(max_prefix), 0, k_prefix.stride(0), k_prefix.stride(1))
-        ws = self._ws_shared[-1] if self._ws_shared else None
-        for _ in range(2):
-            rc = self.lib.rapid_verify_attn_prefix(self._ctx, shape, prefix, q.data_ptr(), _dptr(k_prefix), _dptr(v_prefix),
-                                                   prefix_len.data_ptr(), _dptr(prefix_table), k_cache.data_ptr(),
-                                                   v_cache.data_ptr(), ctx_lens.data_ptr(), _dptr(gammas), _dptr(page_table),
-                                                   out.data_ptr(), _dptr(lse_out), _dptr(ws), 0 if ws is None else ws.numel(),
-                                                   _stream_ptr(self.device))
-            if rc != RAPID_EWORKSPACE:                         # the last check of the call: nothing has been launched
-                break
-            ws = self._shared_workspace(self.lib.rapid_verify_attn_prefix_workspace_bytes(self._ctx, shape, prefix))
-        if rc:
-            _check(self.lib, rc, self._ctx)
-        return out
+            return ctypes.byref(shape), ctypes.byref(PrefixLayout(n * tokens if max_prefix is None else int(max_prefix), n, 0, 0))
+        self._need(k_prefix is not None and v_prefix is not None and k_prefix.dtype == torch.bfloat16
+                   and v_prefix.dtype == torch.bfloat16 and k_prefix.dim() == 3 and k_prefix.shape == v_prefix.shape
+                   and k_prefix.shape[1:] == (hkv, d), "k_prefix and v_prefix: bf16 [P, Hkv, d] as the cache's, the same sizes and strides")
+        sp = _strides(k_prefix[None])
+        self._need(sp == _strides(v_prefix[None]) and sp[3] == 1, "k_prefix and v_prefix: d contiguous, the same strides")
+        n = k_prefix.shape[0]
+        self._need(max_prefix is None or max_prefix <= n, "the prefix holds fewer tokens than max_prefix")
+        return ctypes.byref(shape), ctypes.byref(PrefixLayout(n if max_prefix is None else int(max_prefix), 0, sp[1], sp[2]))
 
     # ------------------------------------------------------------------ retrieval
     def rapid_retrieve(self, chunk_emb, query_emb, top_k: int, threshold: float = 0.3):
