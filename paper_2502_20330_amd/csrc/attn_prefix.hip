@@ -80,13 +80,13 @@ __device__ __forceinline__ void prefix_piece(const StreamLaunch& a, char* smem, 
         }
     }
 #pragma unroll
-    for (int it = 0; it < G::S - 1; ++it)
+    for (int it = 0; it < G::S - 2; ++it)
         load_both<G, PAGED>(addr, kring_lds + it * G::SLOT, vring_lds + it * G::SLOT, tile_t0(it), last_tok, lane, team);
 
     WaveState<G, RB> st;
 #pragma unroll
     for (int rb = 0; rb < RB; ++rb) {
-        st.m[rb] = -INFINITY;
+        st.m[rb] = kNoMaximum;
         st.l[rb] = 0.f;
 #pragma unroll
         for (int db = 0; db < G::DB; ++db) st.acc[db][rb] = floatx4{0.f, 0.f, 0.f, 0.f};
@@ -96,25 +96,40 @@ __device__ __forceinline__ void prefix_piece(const StreamLaunch& a, char* smem, 
     bool taken = false;
     const uint32_t no_scales[G::TB] = {};
 
-    int slot = 0, before = G::S - 1;                     // ring slots of tiles it and it - 1
-    for (int it = 0; it < nt; ++it) {
-        char* kt = kring + slot * G::SLOT;
-        char* vt = vring + slot * G::SLOT;
-        const int t0 = tile_t0(it);
-        floatx4 s[G::TB][RB];
-        bf16x8 pb[G::TB / 2][RB];
-
-        wait_loads<(G::S - 2) * 2 * G::H>();             // own part of tile it
-        lds_reads_done();                                // of tile it - 1
+    // Two waves share a SIMD, w and w + 4.  They take turns: while one is at its matrix products, those of V(it-1) and K(it), the other is at the softmax
+    // of its scores, so that the matrix core and the vector unit run side by side.  Phases are numbered through: the first four waves have the products
+    // of step `it` in phase 2 it and its softmax in 2 it + 1, the other four each one phase later.
+    // Before phase 2 it every wave has its part of tile `it`; then tile it - 2 is behind everybody, and its slot takes tile it - 2 + S.
+    const bool second = wave >= 4;
+    int refill = G::S - 2;                               // slot of that tile
+    auto even_phase = [&](int it) {
+        wait_loads<(G::S - 3) * 2 * G::H>();
+        lds_reads_done();
         __syncthreads();
-        load_both<G, PAGED>(addr, kring_lds + before * G::SLOT, vring_lds + before * G::SLOT, tile_t0(it + G::S - 1), last_tok, lane, team);
-        score_tile<G, RB>(s, qf, kt, nullptr, lane);
+        load_both<G, PAGED>(addr, kring_lds + refill * G::SLOT, vring_lds + refill * G::SLOT, tile_t0(it - 2 + G::S), last_tok, lane, team);
+        refill = refill + 1 == G::S ? 0 : refill + 1;
+    };
+    auto odd_phase = [&]() {
+        lds_reads_done();
+        __syncthreads();
+    };
+    floatx4 s[G::TB][RB];
+    bf16x8 pb[G::TB / 2][RB];
+    int slot = 0, before = 0;                            // ring slots of tiles it and it - 1
+    if (second) even_phase(0);
+    for (int it = 0; it < nt; ++it) {
+        if (second) odd_phase(); else even_phase(it);
+        if (it) pv_tile<G, RB>(st, pb, vring + before * G::SLOT, lane);
+        score_tile<G, RB>(s, qf, kring + slot * G::SLOT, nullptr, lane);
+        if (second) even_phase(it + 1); else odd_phase();
+        const int t0 = tile_t0(it);
         softmax_tile<G, RB>(st, s, pb, no_scales, t0, t0 >= first_masked_t0, lim, c1, c, lane);
-        if (t0 >= first_masked_t0) taken |= take_not_finite<G>(vt, lane);      // (whoever comes second finds zeros)
-        pv_tile<G, RB>(st, pb, vt, lane);
+        if (t0 >= first_masked_t0) taken |= take_not_finite<G>(vring + slot * G::SLOT, lane);      // (whoever comes second finds zeros)
         before = slot;
         slot = slot + 1 == G::S ? 0 : slot + 1;
     }
+    if (!second) even_phase(nt);
+    pv_tile<G, RB>(st, pb, vring + before * G::SLOT, lane);
     wait_loads<0>();                                     // no load may land after the rings are used below
     if (taken && lane == 0) *taken_word = 1;
     __syncthreads();                                     // all rings are dead from here on
@@ -157,16 +172,15 @@ __device__ __forceinline__ void prefix_piece(const StreamLaunch& a, char* smem, 
 #pragma unroll
     for (int rb = 0; rb < RB; ++rb) {
         const int row = row0 + rb * 16;
-        float mw[G::NP], mm = -INFINITY, ll = 0.f;
+        float mw[G::NP], mm = kNoMaximum, ll = 0.f;
 #pragma unroll
         for (int p = 0; p < G::NP; ++p) {
             mw[p] = mlbuf[(p * G::RP + row) * 2];
             mm = fmaxf(mm, mw[p]);
         }
-        const float m_use = (mm == -INFINITY) ? 0.f : mm;
 #pragma unroll
-        for (int p = 0; p < G::NP; ++p) ll += mlbuf[(p * G::RP + row) * 2 + 1] * fast_exp2(mw[p] - m_use);
-        own[rb] = fast_exp2(st.m[rb] - m_use);
+        for (int p = 0; p < G::NP; ++p) ll += mlbuf[(p * G::RP + row) * 2 + 1] * fast_exp2(mw[p] - mm);
+        own[rb] = fast_exp2(st.m[rb] - mm);
         if (part == 0 && lg == 0 && row < rows) {
             a.part_ml[(pbase + row) * 2 + 0] = mm;
             a.part_ml[(pbase + row) * 2 + 1] = ll;

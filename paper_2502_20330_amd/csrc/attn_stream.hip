@@ -80,7 +80,7 @@ __device__ __forceinline__ void run_piece(const StreamLaunch& a, const Piece& w,
     WaveState<G, RB> st;
 #pragma unroll
     for (int rb = 0; rb < RB; ++rb) {
-        st.m[rb] = -INFINITY;
+        st.m[rb] = kNoMaximum;
         st.l[rb] = 0.f;
 #pragma unroll
         for (int db = 0; db < G::DB; ++db) st.acc[db][rb] = floatx4{0.f, 0.f, 0.f, 0.f};
@@ -183,16 +183,15 @@ __device__ __forceinline__ void run_piece(const StreamLaunch& a, const Piece& w,
     float own[RB];
 #pragma unroll
     for (int rb = 0; rb < RB; ++rb) {
-        float mw[G::NP], mm = -INFINITY, ll = 0.f;
+        float mw[G::NP], mm = kNoMaximum, ll = 0.f;
 #pragma unroll
         for (int p = 0; p < G::NP; ++p) {
             mw[p] = mlbuf[((w.team * G::NP + p) * MLS + rb * 16 + ln) * 2];
             mm = fmaxf(mm, mw[p]);
         }
-        const float m_use = (mm == -INFINITY) ? 0.f : mm;
 #pragma unroll
-        for (int p = 0; p < G::NP; ++p) ll += mlbuf[((w.team * G::NP + p) * MLS + rb * 16 + ln) * 2 + 1] * fast_exp2(mw[p] - m_use);
-        own[rb] = fast_exp2(st.m[rb] - m_use);
+        for (int p = 0; p < G::NP; ++p) ll += mlbuf[((w.team * G::NP + p) * MLS + rb * 16 + ln) * 2 + 1] * fast_exp2(mw[p] - mm);
+        own[rb] = fast_exp2(st.m[rb] - mm);
         const int row = row0 + rb * 16 + ln;
         if (w.part == 0 && lg == 0 && row < w.R) {
             a.part_ml[(pbase + row) * 2 + 0] = mm;

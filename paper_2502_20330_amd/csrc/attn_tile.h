@@ -12,6 +12,7 @@ typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 namespace {
 
 constexpr float kRescaleLog2 = 8.0f;   // the running maximum only moves when a tile exceeds it by this (log2 units)
+constexpr float kNoMaximum = -1e30f;   // a row that has met no score yet: finite, so that differences are numbers; every score exceeds it
 constexpr int kPieceQuanta = 2;        // what a sequence costs a workgroup besides its tokens, in quanta
 
 template <int D_, bool QUANT_, int TB_>
@@ -212,7 +213,7 @@ __device__ __forceinline__ bf16x8 eight_values(uint32_t w0, uint32_t w1, float s
 
 template <class G, int RB>
 struct WaveState {
-    float m[RB];                     // reference maximum per query row, log2 units (score * scale * log2 e)
+    float m[RB];                     // reference maximum per query row, log2 units (score * scale * log2 e); kNoMaximum at first
     float l[RB];                     // running sum, this lane group's tokens only
     floatx4 acc[G::DB][RB];          // O^T: column 16 db + 4 (lane / 16) + i, row 16 rb + lane % 16
 };
@@ -266,6 +267,8 @@ __device__ __forceinline__ void value_scales(uint32_t (&vs)[G::TB], const char* 
 
 // Mask, online softmax; leaves P^T (in 8 bits: times V's scales) as the B operand of PV: slot j of lane group lg in step kk is token
 // 32 kk + 16 (j / 4) + 4 lg + j % 4, what this lane holds in s[2 kk + j / 4][.][j % 4].
+// The reference maximum only moves when a score exceeds it by kRescaleLog2; until then p = 2^(s - ref) <= 2^kRescaleLog2, exact in the final
+// ratio.  So a tile's own maxima are only looked at lane by lane, and brought together over the lanes of a row when one of them asks for it.
 template <class G, int RB>
 __device__ __forceinline__ void softmax_tile(WaveState<G, RB>& st, floatx4 (&s)[G::TB][RB], bf16x8 (&pb)[G::TB / 2][RB],
                                              const uint32_t (&vs)[G::TB], int t0, bool masked, const int (&lim)[RB], int end, float c, int lane)
@@ -279,6 +282,7 @@ __device__ __forceinline__ void softmax_tile(WaveState<G, RB>& st, floatx4 (&s)[
             for (int i = 0; i < 4; ++i) vscale[tb][i] = scale_value(vs[tb] >> (8 * i) & 0xffu);
     }
     if (masked) {
+        asm volatile("" : "+s"(t0));                       // a branch, not selects in every tile
 #pragma unroll
         for (int tb = 0; tb < G::TB; ++tb)
 #pragma unroll
@@ -290,38 +294,42 @@ __device__ __forceinline__ void softmax_tile(WaveState<G, RB>& st, floatx4 (&s)[
                 if (G::QUANT && tok >= end) vscale[tb][i] = 0.f;       // a scale that belongs to no token may be anything
             }
     }
-    float alpha[RB];
-    bool changed = false;
+    float mx[RB];
+    bool above = false;
 #pragma unroll
     for (int rb = 0; rb < RB; ++rb) {
-        float mx = -INFINITY;
+        mx[rb] = fmaxf(fmaxf(s[0][rb][0], s[0][rb][1]), fmaxf(s[0][rb][2], s[0][rb][3]));
 #pragma unroll
-        for (int tb = 0; tb < G::TB; ++tb)
-            mx = fmaxf(mx, fmaxf(fmaxf(s[tb][rb][0], s[tb][rb][1]), fmaxf(s[tb][rb][2], s[tb][rb][3])));
-        mx = max_over_groups(mx);
-        const float m_new = (mx * c > st.m[rb] + kRescaleLog2) ? mx * c : st.m[rb];
-        const float m_use = (m_new == -INFINITY) ? 0.f : m_new;
-        alpha[rb] = fast_exp2(st.m[rb] - m_use);
-        changed |= (m_new != st.m[rb]);
-        st.m[rb] = m_new;
+        for (int tb = 1; tb < G::TB; ++tb)
+            mx[rb] = fmaxf(mx[rb], fmaxf(fmaxf(s[tb][rb][0], s[tb][rb][1]), fmaxf(s[tb][rb][2], s[tb][rb][3])));
+        above |= mx[rb] * c > st.m[rb] + kRescaleLog2;
+    }
+    if (__any(above)) {
+#pragma unroll
+        for (int rb = 0; rb < RB; ++rb) {
+            const float top = max_over_groups(mx[rb]) * c;
+            const float m_new = top > st.m[rb] + kRescaleLog2 ? top : st.m[rb];
+            const float alpha = fast_exp2(st.m[rb] - m_new);
+            st.m[rb] = m_new;
+            st.l[rb] *= alpha;
+#pragma unroll
+            for (int db = 0; db < G::DB; ++db)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) st.acc[db][rb][i] *= alpha;
+        }
+    }
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb) {
         float sum = 0.f;
 #pragma unroll
         for (int tb = 0; tb < G::TB; ++tb)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const float p = fast_exp2(fmaf(s[tb][rb][i], c, -m_use));
+                const float p = fast_exp2(fmaf(s[tb][rb][i], c, -st.m[rb]));
                 sum += p;
                 pb[tb / 2][rb][(tb & 1) * 4 + i] = (__bf16)(G::QUANT ? p * vscale[tb][i] : p);
             }
-        st.l[rb] = st.l[rb] * alpha[rb] + sum;
-    }
-    if (__any(changed)) {
-#pragma unroll
-        for (int db = 0; db < G::DB; ++db)
-#pragma unroll
-            for (int rb = 0; rb < RB; ++rb)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) st.acc[db][rb][i] *= alpha[rb];
+        st.l[rb] += sum;
     }
 }
 
