@@ -3,49 +3,119 @@
 // All rows of the batch, R = B (gamma_max + 1) G per kv head, attend the same P tokens, without a mask: the prefix is one "sequence"
 // with R rows.  Reading it costs 4 d bytes per token and kv head, computing 4 R d multiply-adds and R exponentials, so that from about a hundred rows on the
 // matrix cores and the exponentials bound it and no longer the memory.  Up to 96 rows the streaming kernel (attn_stream.hip) does it; this one takes more:
-//  * A workgroup has eight waves, T of which share a stream of token tiles (8 / T streams) and hold RB blocks of 16 rows each, T RB 16 rows
-//    together.  Tiles go HBM -> LDS once a workgroup; S of them lie in a ring, and one barrier a tile says that a tile has landed and
-//    that the slot of the one before it is free.
-//  * Rows beyond T RB 16 go to other workgroups, which read the same tokens at about the same time on the same die (blockIdx modulo 8), so that its L2
+//  * A workgroup has eight waves, T of which share a stream of token tiles (8 / T streams) and hold one to three blocks of 16 rows each, 128 to 384 rows
+//    together.  Tiles go HBM -> LDS once a workgroup; S of them lie in a ring, and the waves meet every S / 4 tiles: then the next ones have landed
+//    and the slots of the ones before are free.
+//  * Rows beyond that go to other workgroups, which read the same tokens at about the same time on the same die (blockIdx modulo 8), so that its L2
 //    serves all but one of them.
 #include "attn_tile.h"
 
 namespace {
 
-template <int D, int T_, int RB_>
+// T: waves that share a stream; RB0, RB1: row blocks of the first and of the last four waves (equal where T = 4).
+template <int D, int T_, int RB0_, int RB1_>
 struct Geo : TileGeo<D, false, D == 64 ? 4 : 2> {
     using Tile = TileGeo<D, false, D == 64 ? 4 : 2>;
     using Tile::SLOT, Tile::TT, Tile::NLD;
-    static constexpr int T = T_, RB = RB_;
+    static constexpr int T = T_, RB0 = RB0_, RB1 = RB1_;
     static constexpr int NW = 8, NP = NW / T;                     // waves, token streams
     static constexpr int H = NLD / T;                             // loads of a tile of K or V that a wave issues
     static constexpr int QUANTUM = NP * TT;
     static constexpr int S = 128 * 1024 / NP / (2 * SLOT);        // tiles of a ring
     static constexpr int RING = S * 2 * SLOT;
-    static constexpr int RP = T * RB * 16;                        // rows of a workgroup
+    static constexpr int NB = S / 4;                              // tiles from one meeting of the waves to the next
+    static constexpr int RP = (T == 8 ? RB0 + RB1 : RB0) * 64;    // rows of a workgroup
     static constexpr int NH = NP * RP * (D + 4) * 4 > 140 * 1024 ? 2 : 1;   // passes of the last exchange, D / NH columns each
     static constexpr int OROW = D / NH + 4;
     static constexpr int MERGE = NP > 1 ? NP * RP * OROW * 4 : 0;
     static constexpr int ML = NP * RING > MERGE ? NP * RING : MERGE;
-    static constexpr int TAKEN = ML + NW * RB * 16 * 8;           // a word for each stream
+    static constexpr int TAKEN = ML + NP * RP * 8;                // a word for each stream
     static constexpr int LDS = TAKEN + NP * 4;
 };
 
 // Loads of tile part `team` of K and V.
 template <class G, bool PAGED>
-__device__ __forceinline__ void load_both(const RowAddr& ra, uint32_t kslot, uint32_t vslot, int t0, int last_tok, int lane, int team)
+__device__ __forceinline__ void load_both(const RowAddr& ra, const TilePages<G, PAGED>& pages, uint32_t kslot, uint32_t vslot, int t0, int last_tok,
+                                          int lane, int team)
 {
-    TilePages<G, PAGED> pages;
-    pages.find(ra, t0, last_tok);
     load_tile<G, PAGED, false>(ra, pages, kslot, t0, last_tok, lane, team * G::H, G::H);
     load_tile<G, PAGED, true>(ra, pages, vslot, t0, last_tok, lane, team * G::H, G::H);
 }
 
-// Tokens [c0, c1) for the rows of tile `rt`; the partial goes to the rows from pbase on.
-template <class G, bool PAGED>
-__device__ __forceinline__ void prefix_piece(const StreamLaunch& a, char* smem, int h, int rt, int c0, int c1, int64_t pbase)
+// The operands of a tile's two products, from LDS to registers: half `x` of V^T's blocks, and half `x` of K's.
+template <class G>
+constexpr int kHalfV = G::TB / 2 * G::DB / 2;
+template <class G>
+__device__ __forceinline__ void read_v(bf16x8 (&vf)[kHalfV<G>], char* vt, int x, int lane)
 {
-    constexpr int RB = G::RB;
+    const int ln = lane & 15, lg = lane >> 4;
+#pragma unroll
+    for (int i = 0; i < kHalfV<G>; ++i) {
+        const int kk = (x * kHalfV<G> + i) / G::DB, db = (x * kHalfV<G> + i) % G::DB;
+        s16x4 half[2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int row = kk * 32 + h * 16 + lg * 4 + (ln >> 2);
+            const int c = (db * 2) ^ v_swz<false, G::ROWB>(row);
+            half[h] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                (s16x4 __attribute__((address_space(3)))*)(vt + row * G::ROWB + c * 16 + (ln & 3) * 8));
+        }
+        const s16x8 both = __builtin_shufflevector(half[0], half[1], 0, 1, 2, 3, 4, 5, 6, 7);
+        vf[i] = __builtin_bit_cast(bf16x8, both);
+    }
+}
+template <class G>
+__device__ __forceinline__ void read_k(bf16x8 (&kf)[G::TB / 2][G::KS], const char* kt, int x, int lane)
+{
+#pragma unroll
+    for (int i = 0; i < G::TB / 2; ++i) {
+        const int row = (x * (G::TB / 2) + i) * 16 + (lane & 15);
+#pragma unroll
+        for (int ks = 0; ks < G::KS; ++ks)
+            kf[i][ks] = *reinterpret_cast<const bf16x8*>(kt + row * G::ROWB + ((ks * 4 + (lane >> 4)) ^ k_swz<G::ROWB>(row)) * 16);
+    }
+}
+// Half `x` of V^T P^T, of K Q^T.
+template <class G, int RB>
+__device__ __forceinline__ void mma_v(WaveState<G, RB>& st, const bf16x8 (&vf)[kHalfV<G>], const bf16x8 (&pb)[G::TB / 2][RB], int x)
+{
+#pragma unroll
+    for (int i = 0; i < kHalfV<G>; ++i) {
+        const int kk = (x * kHalfV<G> + i) / G::DB, db = (x * kHalfV<G> + i) % G::DB;
+#pragma unroll
+        for (int rb = 0; rb < RB; ++rb)
+            st.acc[db][rb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf[i], pb[kk][rb], st.acc[db][rb], 0, 0, 0);
+    }
+}
+template <class G, int RB>
+__device__ __forceinline__ void mma_k(floatx4 (&s)[G::TB][RB], const bf16x8 (&kf)[G::TB / 2][G::KS], const bf16x8 (&qf)[RB][G::KS], int x)
+{
+#pragma unroll
+    for (int i = 0; i < G::TB / 2; ++i) {
+        const int tb = x * (G::TB / 2) + i;
+#pragma unroll
+        for (int rb = 0; rb < RB; ++rb) s[tb][rb] = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int ks = 0; ks < G::KS; ++ks)
+#pragma unroll
+            for (int rb = 0; rb < RB; ++rb)
+                s[tb][rb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[i][ks], qf[rb][ks], s[tb][rb], 0, 0, 0);
+    }
+}
+// The order of what stands before and after stays.
+__device__ __forceinline__ void in_order() { __builtin_amdgcn_sched_barrier(0); }
+// A barrier that waits for nothing: reads of LDS may be under way across it.
+__device__ __forceinline__ void meet()
+{
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+}
+
+// Tokens [c0, c1) for the rows of tile `rt`, of which this wave has RB blocks from team_row on; the partial goes to the rows from pbase on.
+template <class G, int RB, bool PAGED>
+__device__ __forceinline__ void prefix_piece(const StreamLaunch& a, char* smem, int h, int rt, int c0, int c1, int64_t pbase, int team_row)
+{
     const int tid = threadIdx.x, lane = tid & 63, ln = lane & 15, lg = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int part = wave / G::T, team = wave % G::T;
@@ -69,7 +139,7 @@ __device__ __forceinline__ void prefix_piece(const StreamLaunch& a, char* smem, 
     int lim[RB];
 #pragma unroll
     for (int rb = 0; rb < RB; ++rb) {
-        const int row = team * RB * 16 + rb * 16 + ln, r = rt * G::RP + min(row, rows - 1);
+        const int row = team_row + rb * 16 + ln, r = rt * G::RP + min(row, rows - 1);
         lim[rb] = c1 - 1;
         const u32x4* src = reinterpret_cast<const u32x4*>(a.q + ((int64_t)(r / a.G) * a.Hq + h * a.G + r % a.G) * G::D);
 #pragma unroll
@@ -79,9 +149,12 @@ __device__ __forceinline__ void prefix_piece(const StreamLaunch& a, char* smem, 
             qf[rb][ks] = __builtin_bit_cast(bf16x8, raw);
         }
     }
+    TilePages<G, PAGED> pages;
 #pragma unroll
-    for (int it = 0; it < G::S - 2; ++it)
-        load_both<G, PAGED>(addr, kring_lds + it * G::SLOT, vring_lds + it * G::SLOT, tile_t0(it), last_tok, lane, team);
+    for (int it = 0; it < G::S - G::NB; ++it) {
+        pages.find(addr, tile_t0(it), last_tok);
+        load_both<G, PAGED>(addr, pages, kring_lds + it * G::SLOT, vring_lds + it * G::SLOT, tile_t0(it), last_tok, lane, team);
+    }
 
     WaveState<G, RB> st;
 #pragma unroll
@@ -96,40 +169,61 @@ __device__ __forceinline__ void prefix_piece(const StreamLaunch& a, char* smem, 
     bool taken = false;
     const uint32_t no_scales[G::TB] = {};
 
-    // Two waves share a SIMD, w and w + 4.  They take turns: while one is at its matrix products, those of V(it-1) and K(it), the other is at the softmax
-    // of its scores, so that the matrix core and the vector unit run side by side.  Phases are numbered through: the first four waves have the products
-    // of step `it` in phase 2 it and its softmax in 2 it + 1, the other four each one phase later.
-    // Before phase 2 it every wave has its part of tile `it`; then tile it - 2 is behind everybody, and its slot takes tile it - 2 + S.
-    const bool second = wave >= 4;
-    int refill = G::S - 2;                               // slot of that tile
-    auto even_phase = [&](int it) {
-        wait_loads<(G::S - 3) * 2 * G::H>();
+    // The waves run freely between meetings, NB tiles apart, so that of the two waves of a SIMD one is at its matrix products while the other is at its
+    // softmax.  (Meetings at every tile hold all waves to the same step: the products of the two then wait for one another, and so do
+    // the softmaxes.  Handing the two halves of a step to and fro between them was no better: the halves are not equally long.)
+    // Before the first K of a block of NB tiles every wave has its part of the block, and nobody needs the block before any more: its slots take the tiles
+    // three blocks on.
+    int fill = G::S - G::NB, fill_slot = G::S - G::NB;   // the tile that is loaded next, and its slot
+    auto next_block = [&]() {
+        wait_loads<(G::S - 2 * G::NB) * 2 * G::H>();
         lds_reads_done();
-        __syncthreads();
-        load_both<G, PAGED>(addr, kring_lds + refill * G::SLOT, vring_lds + refill * G::SLOT, tile_t0(it - 2 + G::S), last_tok, lane, team);
-        refill = refill + 1 == G::S ? 0 : refill + 1;
+        meet();
+#pragma unroll
+        for (int x = 0; x < G::NB; ++x) {
+            pages.find(addr, tile_t0(fill), last_tok);
+            load_both<G, PAGED>(addr, pages, kring_lds + fill_slot * G::SLOT, vring_lds + fill_slot * G::SLOT, tile_t0(fill), last_tok, lane, team);
+            ++fill;
+            fill_slot = fill_slot + 1 == G::S ? 0 : fill_slot + 1;
+        }
     };
-    auto odd_phase = [&]() {
-        lds_reads_done();
-        __syncthreads();
-    };
+    // Products of step `it`: V(it-1) and K(it); the last step's K is behind the end, and its scores are not used.  Their operands come from LDS ahead of them:
+    // half of V's before the step, the rest and K's under the products with V.
     floatx4 s[G::TB][RB];
-    bf16x8 pb[G::TB / 2][RB];
-    int slot = 0, before = 0;                            // ring slots of tiles it and it - 1
-    if (second) even_phase(0);
+    bf16x8 pb[G::TB / 2][RB], v0[kHalfV<G>];             // weights of a tile, the first half of its V
+    char *kt = kring, *vt = vring;
+    next_block();
+    {
+        bf16x8 k0[G::TB / 2][G::KS], k1[G::TB / 2][G::KS];
+        read_k<G>(k0, kt, 0, lane);
+        read_k<G>(k1, kt, 1, lane);
+        mma_k<G, RB>(s, k0, qf, 0);
+        mma_k<G, RB>(s, k1, qf, 1);
+    }
     for (int it = 0; it < nt; ++it) {
-        if (second) odd_phase(); else even_phase(it);
-        if (it) pv_tile<G, RB>(st, pb, vring + before * G::SLOT, lane);
-        score_tile<G, RB>(s, qf, kring + slot * G::SLOT, nullptr, lane);
-        if (second) even_phase(it + 1); else odd_phase();
         const int t0 = tile_t0(it);
         softmax_tile<G, RB>(st, s, pb, no_scales, t0, t0 >= first_masked_t0, lim, c1, c, lane);
-        if (t0 >= first_masked_t0) taken |= take_not_finite<G>(vring + slot * G::SLOT, lane);      // (whoever comes second finds zeros)
-        before = slot;
-        slot = slot + 1 == G::S ? 0 : slot + 1;
+        if (t0 >= first_masked_t0) taken |= take_not_finite<G>(vt, lane);      // (whoever comes second finds zeros)
+        in_order();
+        bf16x8 v1[kHalfV<G>], k0[G::TB / 2][G::KS], k1[G::TB / 2][G::KS];
+        read_v<G>(v0, vt, 0, lane);
+        read_v<G>(v1, vt, 1, lane);
+        in_order();
+        mma_v<G, RB>(st, v0, pb, 0);
+        in_order();
+        if ((it + 1) % G::NB == 0) next_block();
+        const bool wrap = kt == kring + (G::S - 1) * G::SLOT;
+        kt = wrap ? kring : kt + G::SLOT;
+        read_k<G>(k0, kt, 0, lane);
+        in_order();
+        mma_v<G, RB>(st, v1, pb, 1);
+        read_k<G>(k1, kt, 1, lane);
+        in_order();
+        mma_k<G, RB>(s, k0, qf, 0);
+        mma_k<G, RB>(s, k1, qf, 1);
+        in_order();
+        vt = wrap ? vring : vt + G::SLOT;
     }
-    if (!second) even_phase(nt);
-    pv_tile<G, RB>(st, pb, vring + before * G::SLOT, lane);
     wait_loads<0>();                                     // no load may land after the rings are used below
     if (taken && lane == 0) *taken_word = 1;
     __syncthreads();                                     // all rings are dead from here on
@@ -140,7 +234,7 @@ __device__ __forceinline__ void prefix_piece(const StreamLaunch& a, char* smem, 
 #pragma unroll
     for (int rb = 0; rb < RB; ++rb) st.l[rb] = sum_over_groups(st.l[rb]);
 
-    const int row0 = team * RB * 16 + ln;
+    const int row0 = team_row + ln;
     if constexpr (G::NP == 1) {
 #pragma unroll
         for (int rb = 0; rb < RB; ++rb) {
@@ -225,7 +319,11 @@ __global__ void __launch_bounds__(G::NW * 64) attn_prefix(StreamLaunch a)
     rt = __builtin_amdgcn_readfirstlane(rt);
     const int g = u / a.Hkv, h = __builtin_amdgcn_readfirstlane(u % a.Hkv);
     for_each_piece(a, __builtin_amdgcn_readfirstlane(g), threadIdx.x & 63, G::QUANTUM, [&](int, int, int c0, int c1) {
-        prefix_piece<G, PAGED>(a, smem, h, rt, c0, c1, ((int64_t)(h * a.tiles + rt) * a.nslots + g) * G::RP);
+        const int64_t pbase = ((int64_t)(h * a.tiles + rt) * a.nslots + g) * G::RP;
+        const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        // (the two arms run the same barriers)
+        if (G::RB0 == G::RB1 || wave < 4) prefix_piece<G, G::RB0, PAGED>(a, smem, h, rt, c0, c1, pbase, wave % G::T * G::RB0 * 16);
+        else prefix_piece<G, G::RB1, PAGED>(a, smem, h, rt, c0, c1, pbase, G::RB0 * 64 + (wave - 4) * G::RB1 * 16);
         wait_loads<0>();
     });
 }
@@ -235,10 +333,11 @@ template <int D, class F>
 hipError_t with_rows(int rows, F f)
 {
     switch (rows) {
-        case 128: return f(Geo<D, 4, 2>());
-        case 192: return f(Geo<D, 4, 3>());
-        case 256: return f(Geo<D, 8, 2>());
-        case 384: return f(Geo<D, 8, 3>());
+        case 128: return f(Geo<D, 4, 2, 2>());
+        case 192: return f(Geo<D, 4, 3, 3>());
+        case 256: return f(Geo<D, 8, 2, 2>());
+        case 320: return f(Geo<D, 8, 3, 2>());
+        case 384: return f(Geo<D, 8, 3, 3>());
     }
     return hipErrorInvalidValue;
 }
@@ -250,7 +349,7 @@ hipError_t with_rows(int D, int rows, F f) { return D == 128 ? with_rows<128>(ro
 hipError_t configure_attn_prefix()
 {
     for (int D = 64; D <= 128; D += 64)
-        for (int rows : {128, 192, 256, 384}) {
+        for (int rows : {128, 192, 256, 320, 384}) {
             const hipError_t e = with_rows(D, rows, [](auto geo) {
                 using G = decltype(geo);
                 static_assert(G::LDS <= 160 * 1024, "LDS of a compute unit");
@@ -270,7 +369,7 @@ void plan_attn_prefix(StreamLaunch& a, int n_cu)
 {
     const int R = a.Qmax * a.G;
     int64_t least = -1;
-    for (int rows : {384, 256, 192, 128}) {
+    for (int rows : {384, 320, 256, 192, 128}) {
         const int64_t padded = ((int64_t)R + rows - 1) / rows * rows;
         if (least >= 0 && padded >= least) continue;
         least = padded;
