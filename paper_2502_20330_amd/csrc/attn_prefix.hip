@@ -38,8 +38,8 @@ template <class G, bool PAGED>
 __device__ __forceinline__ void load_both(const RowAddr& ra, const TilePages<G, PAGED>& pages, uint32_t kslot, uint32_t vslot, int t0, int last_tok,
                                           int lane, int team)
 {
-    load_tile<G, PAGED, false>(ra, pages, kslot, t0, last_tok, lane, team * G::H, G::H);
-    load_tile<G, PAGED, true>(ra, pages, vslot, t0, last_tok, lane, team * G::H, G::H);
+    load_tile<G, PAGED, false, G::H>(ra, pages, kslot, t0, last_tok, lane, team * G::H);
+    load_tile<G, PAGED, true, G::H>(ra, pages, vslot, t0, last_tok, lane, team * G::H);
 }
 
 // The operands of a tile's two products, from LDS to registers: half `x` of V^T's blocks, and half `x` of K's.
@@ -102,21 +102,11 @@ __device__ __forceinline__ void mma_k(floatx4 (&s)[G::TB][RB], const bf16x8 (&kf
                 s[tb][rb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[i][ks], qf[rb][ks], s[tb][rb], 0, 0, 0);
     }
 }
-// The order of what stands before and after stays.
-__device__ __forceinline__ void in_order() { __builtin_amdgcn_sched_barrier(0); }
-// A barrier that waits for nothing: reads of LDS may be under way across it.
-__device__ __forceinline__ void meet()
-{
-    asm volatile("" ::: "memory");
-    __builtin_amdgcn_s_barrier();
-    asm volatile("" ::: "memory");
-}
-
 // Tokens [c0, c1) for the rows of tile `rt`, of which this wave has RB blocks from team_row on; the partial goes to the rows from pbase on.
 template <class G, int RB, bool PAGED>
 __device__ __forceinline__ void prefix_piece(const StreamLaunch& a, char* smem, int h, int rt, int c0, int c1, int64_t pbase, int team_row)
 {
-    const int tid = threadIdx.x, lane = tid & 63, ln = lane & 15, lg = lane >> 4;
+    const int tid = opaque(threadIdx.x), lane = tid & 63, ln = lane & 15, lg = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int part = wave / G::T, team = wave % G::T;
     const int rows = a.Qmax * a.G - rt * G::RP;          // of this tile, if there are so many

@@ -89,67 +89,94 @@ __device__ __forceinline__ void run_piece(const StreamLaunch& a, const Piece& w,
     const int first_masked_t0 = min(a.shared ? w.L : w.L - w.Q, w.c1) - (G::TT - 1);     // tiles from here on hold tokens that some row does not attend
     TilePages<G, PAGED> pages;
     bool taken = false;
+    [[maybe_unused]] const uint32_t no_scales[G::TB] = {};
 
-    // Ring slots of tile `it`, and of the one that takes a slot next.
-    int slot = 0;
+    int slot = 0;                                        // ring slot of tile it
     auto next = [](int s) { return s + 1 == G::S ? 0 : s + 1; };
-    if constexpr (!G::TEAMS) {
-        // oldest load first: K(it) V(it) K(it+1) V(it+1) .., the scales ahead of K
+    if constexpr (G::QUANT) {
+        // A tile's codes of V are in registers before the softmax, so that the products with V wait for nothing and the tile's slots are free early.
+        // Streams of their own: S tiles are under way, and the slot is filled again by the wave that has read it.
+        // Two waves a stream: each issues half of a tile's loads (both the scales); at the meeting tile `it` is complete and everybody has read
+        // tile it - 1, whose slot takes tile it + S - 1.
+        int before = G::S - 1;
+        for (int it = 0; it < w.nt; ++it, before = slot, slot = next(slot)) {
+            char* kt = w.kring + slot * G::SLOT;
+            char* vt = w.vring + slot * G::SLOT;
+            const int t0 = tile_t0(it), fill = G::TEAMS ? before : slot, t_fill = tile_t0(it + G::S - (G::TEAMS ? 1 : 0));
+            constexpr int H = G::TEAMS ? G::NLD / 2 : G::NLD;
+            auto refill = [&]() {
+                load_scales<G, PAGED>(w.addr, pages, w.sring_lds + fill * 256, t_fill, w.last_tok, lane);
+                load_tile<G, PAGED, false, H>(w.addr, pages, w.kring_lds + fill * G::SLOT, t_fill, w.last_tok, lane, w.team * H);
+                load_tile<G, PAGED, true, H>(w.addr, pages, w.vring_lds + fill * G::SLOT, t_fill, w.last_tok, lane, w.team * H);
+            };
+            pages.find(w.addr, t_fill, w.last_tok);
+            wait_loads<(G::S - (G::TEAMS ? 2 : 1)) * (2 * H + G::SC)>();
+            if (G::TEAMS) {
+                meet();
+                refill();
+            }
+            if (t0 >= first_masked_t0) taken |= take_not_finite<G>(vt, lane);      // (of a team, whoever comes second finds zeros)
+            RawTile<G> x;
+            x.read_k(kt, w.sring + slot * 256, lane);
+            in_order();
+            floatx4 s[G::TB][RB];
+            bf16x8 pb[G::TB / 2][RB];
+            x.scores(s, qf);
+            x.read_v(vt, lane);
+            lds_reads_done();
+            if (!G::TEAMS) refill();
+            softmax_tile<G, RB>(st, s, pb, x.vs, t0, t0 >= first_masked_t0, lim, w.c1, c, lane);
+            x.add_values(st, pb);
+        }
+    } else if constexpr (!G::TEAMS) {
+        // oldest load first: K(it) V(it) K(it+1) V(it+1) ..
         for (int it = 0; it < w.nt; ++it, slot = next(slot)) {
             char* kt = w.kring + slot * G::SLOT;
             char* vt = w.vring + slot * G::SLOT;
-            char* sc = w.sring + slot * 256;
             const int t0 = tile_t0(it), t_next = tile_t0(it + G::S);
             floatx4 s[G::TB][RB];
             bf16x8 pb[G::TB / 2][RB];
-            uint32_t vs[G::TB];
 
             pages.find(w.addr, t_next, w.last_tok);
-            wait_loads<(2 * G::S - 1) * G::NLD + (G::S - 1) * G::SC>();        // K(it)
-            score_tile<G, RB>(s, qf, kt, sc, lane);
-            value_scales<G>(vs, sc, lane);
+            wait_loads<(2 * G::S - 1) * G::NLD>();              // K(it)
+            score_tile<G, RB>(s, qf, kt, lane);
             lds_reads_done();
-            load_scales<G, PAGED>(w.addr, pages, w.sring_lds + slot * 256, t_next, w.last_tok, lane);
-            load_tile<G, PAGED, false>(w.addr, pages, w.kring_lds + slot * G::SLOT, t_next, w.last_tok, lane, 0, G::NLD);
+            load_tile<G, PAGED, false, G::NLD>(w.addr, pages, w.kring_lds + slot * G::SLOT, t_next, w.last_tok, lane, 0);
 
-            softmax_tile<G, RB>(st, s, pb, vs, t0, t0 >= first_masked_t0, lim, w.c1, c, lane);
+            softmax_tile<G, RB>(st, s, pb, no_scales, t0, t0 >= first_masked_t0, lim, w.c1, c, lane);
 
-            wait_loads<(2 * G::S - 1) * G::NLD + G::S * G::SC>();              // V(it)
+            wait_loads<(2 * G::S - 1) * G::NLD>();              // V(it)
             if (t0 >= first_masked_t0) taken |= take_not_finite<G>(vt, lane);
             pv_tile<G, RB>(st, pb, vt, lane);
             lds_reads_done();
-            load_tile<G, PAGED, true>(w.addr, pages, w.vring_lds + slot * G::SLOT, t_next, w.last_tok, lane, 0, G::NLD);
+            load_tile<G, PAGED, true, G::NLD>(w.addr, pages, w.vring_lds + slot * G::SLOT, t_next, w.last_tok, lane, 0);
         }
     } else {
-        // Two waves share a stream; each issues half of a tile's loads (both the scales).
+        // Two waves share a stream; each issues half of a tile's loads.
         // Barrier A: K(it) is complete, and everybody has done with V(it-1), whose slot V(it+S-1) takes.
         // Barrier B: V(it) is complete, and everybody has done with K(it), whose slot K(it+S) takes.
-        constexpr int H = G::NLD / 2, BEHIND = 2 * (G::S - 1) * H + (G::S - 1) * G::SC;
+        constexpr int H = G::NLD / 2, BEHIND = 2 * (G::S - 1) * H;
         TilePages<G, PAGED> vpages;
         vpages.find(w.addr, tile_t0(G::S - 1), w.last_tok);
         int before = G::S - 1;                                  // the slot of tile it - 1
         for (int it = 0; it < w.nt; ++it, before = slot, slot = next(slot)) {
             char* kt = w.kring + slot * G::SLOT;
             char* vt = w.vring + slot * G::SLOT;
-            char* sc = w.sring + slot * 256;
             const int t0 = tile_t0(it), t_next = tile_t0(it + G::S);
             floatx4 s[G::TB][RB];
             bf16x8 pb[G::TB / 2][RB];
-            uint32_t vs[G::TB];
 
             pages.find(w.addr, t_next, w.last_tok);
             wait_loads<BEHIND>();                               // own half of K(it)
             __syncthreads();                                    // A
-            load_tile<G, PAGED, true>(w.addr, vpages, w.vring_lds + before * G::SLOT, t_next - G::TT, w.last_tok, lane, w.team * H, H);
-            score_tile<G, RB>(s, qf, kt, sc, lane);
-            value_scales<G>(vs, sc, lane);
-            softmax_tile<G, RB>(st, s, pb, vs, t0, t0 >= first_masked_t0, lim, w.c1, c, lane);
+            load_tile<G, PAGED, true, H>(w.addr, vpages, w.vring_lds + before * G::SLOT, t_next - G::TT, w.last_tok, lane, w.team * H);
+            score_tile<G, RB>(s, qf, kt, lane);
+            softmax_tile<G, RB>(st, s, pb, no_scales, t0, t0 >= first_masked_t0, lim, w.c1, c, lane);
 
             wait_loads<BEHIND>();                               // own half of V(it)
             lds_reads_done();
             __syncthreads();                                    // B
-            load_scales<G, PAGED>(w.addr, pages, w.sring_lds + slot * 256, t_next, w.last_tok, lane);
-            load_tile<G, PAGED, false>(w.addr, pages, w.kring_lds + slot * G::SLOT, t_next, w.last_tok, lane, w.team * H, H);
+            load_tile<G, PAGED, false, H>(w.addr, pages, w.kring_lds + slot * G::SLOT, t_next, w.last_tok, lane, w.team * H);
             if (t0 >= first_masked_t0) taken |= take_not_finite<G>(vt, lane);      // (whoever comes second finds zeros)
             pv_tile<G, RB>(st, pb, vt, lane);
             lds_reads_done();
@@ -223,7 +250,7 @@ template <class G, bool PAGED>
 __device__ __forceinline__ void stream_piece(const StreamLaunch& a, char* smem, int b, int h, int L, int c0, int c1, int64_t pbase)
 {
     Piece w;
-    const int tid = threadIdx.x;
+    const int tid = opaque(threadIdx.x);
     w.lane = tid & 63;
     w.wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     w.part = w.wave % G::NP;
@@ -268,16 +295,17 @@ __device__ __forceinline__ void stream_piece(const StreamLaunch& a, char* smem, 
     constexpr int H = G::TEAMS ? G::NLD / 2 : G::NLD;
     const int e0 = G::TEAMS ? w.team * H : 0;
     if (w.nt > 0) {
+        // tiles 0 .. S-1; of teams, the last is left to the first steps (bf16: its V)
+        constexpr int NK = G::S - (G::TEAMS && G::QUANT ? 1 : 0), NV = G::S - (G::TEAMS ? 1 : 0);
 #pragma unroll
-        for (int it = 0; it < G::S; ++it) {
+        for (int it = 0; it < NK; ++it) {
             const int t0 = tile_t0(it);
             pages.find(w.addr, t0, w.last_tok);
             load_scales<G, PAGED>(w.addr, pages, w.sring_lds + it * 256, t0, w.last_tok, w.lane);
-            load_tile<G, PAGED, false>(w.addr, pages, w.kring_lds + it * G::SLOT, t0, w.last_tok, w.lane, e0, H);
-            // (teams: the last V follows barrier A)
-            if (!G::TEAMS || it + 1 < G::S) load_tile<G, PAGED, true>(w.addr, pages, w.vring_lds + it * G::SLOT, t0, w.last_tok, w.lane, e0, H);
+            load_tile<G, PAGED, false, H>(w.addr, pages, w.kring_lds + it * G::SLOT, t0, w.last_tok, w.lane, e0);
+            if (it < NV) load_tile<G, PAGED, true, H>(w.addr, pages, w.vring_lds + it * G::SLOT, t0, w.last_tok, w.lane, e0);
         }
-        wait_loads<(2 * G::S - (G::TEAMS ? 1 : 0)) * H + G::S * G::SC>();
+        wait_loads<(NK + NV) * H + NK * G::SC>();
     } else {
         wait_loads<0>();
     }
@@ -299,8 +327,8 @@ template <class G, bool PAGED>
 __global__ void __launch_bounds__(G::NW * 64) attn_stream(StreamLaunch a)
 {
     extern __shared__ __attribute__((aligned(1024))) char smem[];
-    const int g = __builtin_amdgcn_readfirstlane(blockIdx.x / a.Hkv), x = blockIdx.x % a.Hkv;
-    const int h = __builtin_amdgcn_readfirstlane(a.rot ? (x + g) % a.Hkv : x);     // (base addresses go through scalar registers)
+    const int g = blockIdx.y;
+    const int h = __builtin_amdgcn_readfirstlane(a.rot ? (blockIdx.x + g) % a.Hkv : blockIdx.x);     // (base addresses go through scalar registers)
     for_each_piece(a, g, threadIdx.x & 63, G::QUANTUM, [&](int b, int L, int c0, int c1) {
         stream_piece<G, PAGED>(a, smem, b, h, L, c0, c1, ((int64_t)h * a.nslots + g + b) * G::RP);
         wait_loads<0>();                                 // the partial's stores are out of the load account
@@ -317,7 +345,7 @@ __device__ __forceinline__ Partials find_partials(const StreamLaunch& a, int b, 
 {
     int before = 0, total = 0, cost = 0;
     for (int b0 = 0; b0 < a.B; b0 += 64) {
-        const int mine = b0 + lane < a.B ? seq_cost(seq_len(a, b0 + lane), a.quantum) : 0;
+        const int mine = b0 + lane < a.B ? seq_cost(seq_len(a, b0 + lane), b0 + lane, a.quantum) : 0;
         const int end = total + scan_costs(mine);
         if (b >= b0 && b < b0 + 64) {
             cost = __builtin_amdgcn_readlane(mine, b - b0);
@@ -328,7 +356,7 @@ __device__ __forceinline__ Partials find_partials(const StreamLaunch& a, int b, 
     Partials p;
     if (cost > 0) {
         const Shares sh(total, a.groups);
-        const int g0 = sh.owner(before + kPieceQuanta), g1 = sh.owner(before + cost - 1);
+        const int g0 = sh.owner(before + piece_cost(b)), g1 = sh.owner(before + cost - 1);
         p.n = g1 - g0 + 1;
         p.slot = ((int64_t)(h * a.tiles + row / a.RP) * a.nslots + g0 + b) * a.RP + row % a.RP;
     }
@@ -468,7 +496,7 @@ hipError_t launch_attn_stream(const StreamLaunch& a, hipStream_t stream)
     return with_geo(a.D, a.own.ks != nullptr, a.RP / 16, [&](auto geo) {
         using G = decltype(geo);
         auto fn = a.own.page_table ? attn_stream<G, true> : attn_stream<G, false>;
-        hipLaunchKernelGGL(fn, dim3(a.Hkv * a.groups), dim3(G::NW * 64), G::LDS, stream, a);
+        hipLaunchKernelGGL(fn, dim3(a.Hkv, a.groups), dim3(G::NW * 64), G::LDS, stream, a);
         return hipGetLastError();
     });
 }

@@ -40,13 +40,15 @@ template <bool QUANT, int ROWB> __device__ __forceinline__ int v_swz(int r)
 }
 
 // ---- shares
-// Each sequence costs its tokens in quanta and kPieceQuanta more, which come first; the sum is cut into equal shares.
+// Each sequence costs its tokens in quanta and, but for the first, kPieceQuanta more, which come first; the sum is cut into equal shares.  (A share
+// has one piece anyhow, and a piece more for each sequence that begins in it.)
 __device__ __forceinline__ int seq_len(const StreamLaunch& a, int b) { return max(min(a.ctx_lens[b], a.max_ctx), 0); }
 __device__ __forceinline__ int seq_queries(const StreamLaunch& a, int b)
 {
     return min(max(a.gammas ? a.gammas[b] : a.gamma, 0), a.Qmax - 1) + 1;
 }
-__device__ __forceinline__ int seq_cost(int L, int quantum) { return L > 0 ? (L + quantum - 1) / quantum + kPieceQuanta : 0; }
+__device__ __forceinline__ int piece_cost(int b) { return b ? kPieceQuanta : 0; }
+__device__ __forceinline__ int seq_cost(int L, int b, int quantum) { return L > 0 ? (L + quantum - 1) / quantum + piece_cost(b) : 0; }
 
 struct Shares {
     int used, len, rest;                // shares in use; the first `rest` of them have len + 1 quanta
@@ -62,27 +64,21 @@ struct Shares {
         return x < head ? (int)((unsigned)x / (unsigned)(len + 1)) : rest + (int)((unsigned)(x - head) / (unsigned)max(len, 1));
     }
 };
-__device__ __forceinline__ int total_cost(const StreamLaunch& a, int lane, int quantum)
-{
-    int total = 0;
-    for (int b0 = 0; b0 < a.B; b0 += 64)
-        total += __builtin_amdgcn_readlane(scan_costs(b0 + lane < a.B ? seq_cost(seq_len(a, b0 + lane), quantum) : 0), 63);
-    return total;
-}
-// Calls piece(b, L, c0, c1) for every piece [c0, c1) of a sequence b in share g, in order.
+// Calls piece(b, L, c0, c1) for every piece [c0, c1) of a sequence b in share g, in order.  Sequences are taken 64 at a time, one a lane.
 template <class Piece>
 __device__ __forceinline__ void for_each_piece(const StreamLaunch& a, int g, int lane, int quantum, Piece piece)
 {
-    const int total = total_cost(a, lane, quantum);
+    int len = lane < a.B ? seq_len(a, lane) : 0;
+    int cost = seq_cost(len, lane, quantum);
+    int end = scan_costs(cost);                          // cost of the sequences up to this one
+    int total = __builtin_amdgcn_readlane(end, 63);
+    for (int b0 = 64; b0 < a.B; b0 += 64)
+        total += __builtin_amdgcn_readlane(scan_costs(b0 + lane < a.B ? seq_cost(seq_len(a, b0 + lane), b0 + lane, quantum) : 0), 63);
     const Shares sh(total, a.groups);
     const int x0 = sh.begin(g), x1 = min(sh.begin(g + 1), total);
     if (x0 >= x1) return;
-    int before = 0;                                      // cost of the sequences before b0
-    for (int b0 = 0; b0 < a.B; b0 += 64) {
-        const int len = b0 + lane < a.B ? seq_len(a, b0 + lane) : 0;
-        const int cost = seq_cost(len, quantum);
-        const int end = before + scan_costs(cost);
-        const int tok = end - cost + kPieceQuanta;       // position of the sequence's first tokens
+    for (int b0 = 0;;) {
+        const int tok = end - cost + piece_cost(b0 + lane);       // position of the sequence's first tokens
         const bool mine = cost > 0 && end > x0 && tok < x1;
         for (unsigned long long todo = __ballot(mine); todo; todo &= todo - 1) {
             const int l = __ffsll((long long)todo) - 1;
@@ -91,9 +87,21 @@ __device__ __forceinline__ void for_each_piece(const StreamLaunch& a, int g, int
             const int c1 = min((min(x1, __builtin_amdgcn_readlane(end, l)) - t) * quantum, L);
             if (c0 < c1) piece(b0 + l, L, c0, c1);
         }
-        before = __builtin_amdgcn_readlane(end, 63);
-        if (before >= x1) break;
+        const int before = __builtin_amdgcn_readlane(end, 63);
+        b0 += 64;
+        if (b0 >= a.B || before >= x1) return;
+        len = b0 + lane < a.B ? seq_len(a, b0 + lane) : 0;
+        cost = seq_cost(len, b0 + lane, quantum);
+        end = before + scan_costs(cost);
     }
+}
+
+// The same number, of which the compiler knows nothing: what rare paths make of it is computed there, and does not take registers from the
+// main loop (a spilled one is loaded back ahead of the loop, and that load waits for all the tiles under way).
+__device__ __forceinline__ int opaque(int lane)
+{
+    asm volatile("" : "+v"(lane));
+    return lane;
 }
 
 // ---- loads
@@ -151,19 +159,36 @@ struct TilePages {
     }
 };
 
-// Loads [E0, E1) of a tile of K or V into `slot`.  Rows past `last_tok` are clamped to it (always a valid address); the softmax masks them.
-template <class G, bool PAGED, bool IS_V>
-__device__ __forceinline__ void load_tile(const RowAddr& ra, const TilePages<G, PAGED>& pages, uint32_t slot, int t0, int last_tok, int lane,
-                                          int e0, int n)
+// Loads [e0, e0 + N) of a tile of K or V into `slot`.  Rows past `last_tok` are clamped to it (always a valid address); the softmax masks them.
+// Where there are none, all that varies from load to load and from tile to tile is uniform and goes into the base; a lane's own offset
+// only depends on the swizzle (f(e RPI + r) = f(e RPI) ^ f(r): fields of bits).
+template <class G, bool PAGED, bool IS_V, int N>
+__device__ __forceinline__ void load_tile(const RowAddr& ra, const TilePages<G, PAGED>& pages, uint32_t slot, int t0, int last_tok, int lane, int e0)
 {
     const char* base = IS_V ? ra.v : ra.k;
     const int r_local = lane / G::CPR, cpos = lane % G::CPR;
+    auto swz = [](int row) { return IS_V ? v_swz<G::QUANT, G::ROWB>(row) : k_swz<G::ROWB>(row); };
+    if (t0 + G::TT - 1 <= last_tok) {
+        const uint32_t row_off = (uint32_t)r_local * ra.tok_bytes;
 #pragma unroll
-    for (int x = 0; x < G::NLD; ++x) {
-        if (x >= n) break;
+        for (int x = 0; x < N; ++x) {
+            const int e = e0 + x;
+            const uint32_t off = row_off + (uint32_t)((cpos ^ swz(r_local)) ^ swz(e * G::RPI)) * 16u;
+            if (PAGED) {
+                const int id = __builtin_amdgcn_readfirstlane(pages.of(e * G::RPI / 16));
+                dma16(base + (int64_t)id * ra.page_bytes + (uint32_t)((t0 + e * G::RPI) & ra.page_mask) * ra.tok_bytes, off, slot + e * 1024);
+            } else {
+                dma16(base + (uint32_t)(t0 + e * G::RPI) * ra.tok_bytes, off, slot + e * 1024);
+            }
+        }
+        return;
+    }
+    lane = opaque(lane);
+#pragma unroll
+    for (int x = 0; x < N; ++x) {
         const int e = e0 + x;
-        const int row = e * G::RPI + r_local;
-        const int c = cpos ^ (IS_V ? v_swz<G::QUANT, G::ROWB>(row) : k_swz<G::ROWB>(row));
+        const int row = e * G::RPI + lane / G::CPR;
+        const int c = lane % G::CPR ^ swz(row);
         const int tok = min(t0 + row, last_tok);
         if (PAGED) {
             const int id = __builtin_amdgcn_readfirstlane(pages.of(e * G::RPI / 16));
@@ -218,10 +243,9 @@ struct WaveState {
     floatx4 acc[G::DB][RB];          // O^T: column 16 db + 4 (lane / 16) + i, row 16 rb + lane % 16
 };
 
-// S^T[token][row] for the tile in `kt`.  In 8 bits a lane reads 16 codes at a time, which feed two steps: step 2p + h of lane group lg holds
-// elements 64 p + 16 lg + 8 h .. + 7 (of K and of Q alike; any order of a sum's terms will do).
+// S^T[token][row] for the tile in `kt`, bf16.
 template <class G, int RB>
-__device__ __forceinline__ void score_tile(floatx4 (&s)[G::TB][RB], const bf16x8 (&qf)[RB][G::KS], const char* kt, const char* sc, int lane)
+__device__ __forceinline__ void score_tile(floatx4 (&s)[G::TB][RB], const bf16x8 (&qf)[RB][G::KS], const char* kt, int lane)
 {
     const int ln = lane & 15, lg = lane >> 4;
 #pragma unroll
@@ -229,40 +253,93 @@ __device__ __forceinline__ void score_tile(floatx4 (&s)[G::TB][RB], const bf16x8
 #pragma unroll
         for (int rb = 0; rb < RB; ++rb) s[tb][rb] = floatx4{0.f, 0.f, 0.f, 0.f};
         const int row = tb * 16 + ln;
-        if constexpr (G::QUANT) {
-            const float scale = scale_value(*reinterpret_cast<const uint8_t*>(sc + row));
 #pragma unroll
-            for (int p = 0; p < G::KS / 2; ++p) {
-                const int c = (p * 4 + lg) ^ k_swz<G::ROWB>(row);
-                const u32x4 raw = *reinterpret_cast<const u32x4*>(kt + row * G::ROWB + c * 16);
+        for (int ks = 0; ks < G::KS; ++ks) {
+            const int c = (ks * 4 + lg) ^ k_swz<G::ROWB>(row);
+            const bf16x8 ka = *reinterpret_cast<const bf16x8*>(kt + row * G::ROWB + c * 16);
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const bf16x8 ka = eight_values(raw[2 * h], raw[2 * h + 1], scale);
-#pragma unroll
-                    for (int rb = 0; rb < RB; ++rb)
-                        s[tb][rb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ka, qf[rb][2 * p + h], s[tb][rb], 0, 0, 0);
-                }
-            }
-        } else {
-#pragma unroll
-            for (int ks = 0; ks < G::KS; ++ks) {
-                const int c = (ks * 4 + lg) ^ k_swz<G::ROWB>(row);
-                const bf16x8 ka = *reinterpret_cast<const bf16x8*>(kt + row * G::ROWB + c * 16);
-#pragma unroll
-                for (int rb = 0; rb < RB; ++rb)
-                    s[tb][rb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ka, qf[rb][ks], s[tb][rb], 0, 0, 0);
-            }
+            for (int rb = 0; rb < RB; ++rb)
+                s[tb][rb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ka, qf[rb][ks], s[tb][rb], 0, 0, 0);
         }
     }
 }
 
-// The scales of V's tokens, four a block: those of this lane group.
+// A tile in 8 bits, out of LDS: this lane's codes of K (16 at a time, which feed two steps of the product: step 2p + h of lane group lg holds
+// elements 64 p + 16 lg + 8 h .. + 7, of K and of Q alike; any order of a sum's terms will do), its token's scales, its columns of V (eight
+// tokens each), the scales of V's tokens (four a block).  K's reads are issued together, and V's, so that the latency of LDS is met twice a tile.
 template <class G>
-__device__ __forceinline__ void value_scales(uint32_t (&vs)[G::TB], const char* sc, int lane)
-{
-    if (!G::QUANT) return;
+struct RawTile {
+    u32x4 k[G::TB][G::KS / 2];
+    i32x2 v[G::TB / 2][G::DB];
+    uint32_t ks[G::TB], vs[G::TB];
+
+    __device__ __forceinline__ void read_k(const char* kt, const char* sc, int lane)
+    {
+        const int ln = lane & 15, lg = lane >> 4;
 #pragma unroll
-    for (int tb = 0; tb < G::TB; ++tb) vs[tb] = *reinterpret_cast<const uint32_t*>(sc + G::TT + tb * 16 + (lane >> 4) * 4);
+        for (int tb = 0; tb < G::TB; ++tb) {
+            const int row = tb * 16 + ln;
+            ks[tb] = *reinterpret_cast<const uint8_t*>(sc + row);
+#pragma unroll
+            for (int p = 0; p < G::KS / 2; ++p)
+                k[tb][p] = *reinterpret_cast<const u32x4*>(kt + row * G::ROWB + ((p * 4 + lg) ^ k_swz<G::ROWB>(row)) * 16);
+            vs[tb] = *reinterpret_cast<const uint32_t*>(sc + G::TT + tb * 16 + lg * 4);
+        }
+    }
+    __device__ __forceinline__ void read_v(char* vt, int lane)
+    {
+        const int ln = lane & 15, lg = lane >> 4;
+#pragma unroll
+        for (int kk = 0; kk < G::TB / 2; ++kk)
+#pragma unroll
+            for (int db = 0; db < G::DB; ++db) {
+                // eight rows of 16 codes: lane i of a group gives the address of row i / 2, half i % 2, and gets column i
+                const int r = ln >> 1, row = kk * 32 + (r >> 2) * 16 + lg * 4 + (r & 3);
+                v[kk][db] = __builtin_amdgcn_ds_read_tr8_b64_v2i32(
+                    (i32x2 __attribute__((address_space(3)))*)(vt + row * G::ROWB + (db ^ v_swz<true, G::ROWB>(row)) * 16 + (ln & 1) * 8));
+            }
+    }
+    template <int RB>
+    __device__ __forceinline__ void scores(floatx4 (&s)[G::TB][RB], const bf16x8 (&qf)[RB][G::KS]) const
+    {
+#pragma unroll
+        for (int tb = 0; tb < G::TB; ++tb) {
+            const float scale = scale_value(ks[tb]);
+#pragma unroll
+            for (int rb = 0; rb < RB; ++rb) s[tb][rb] = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int p = 0; p < G::KS / 2; ++p)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const bf16x8 ka = eight_values(k[tb][p][2 * h], k[tb][p][2 * h + 1], scale);
+#pragma unroll
+                    for (int rb = 0; rb < RB; ++rb)
+                        s[tb][rb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ka, qf[rb][2 * p + h], s[tb][rb], 0, 0, 0);
+                }
+        }
+    }
+    template <int RB>
+    __device__ __forceinline__ void add_values(WaveState<G, RB>& st, const bf16x8 (&pb)[G::TB / 2][RB]) const
+    {
+#pragma unroll
+        for (int kk = 0; kk < G::TB / 2; ++kk)
+#pragma unroll
+            for (int db = 0; db < G::DB; ++db) {
+                const bf16x8 va = eight_values((uint32_t)v[kk][db][0], (uint32_t)v[kk][db][1], 1.0f);
+#pragma unroll
+                for (int rb = 0; rb < RB; ++rb)
+                    st.acc[db][rb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va, pb[kk][rb], st.acc[db][rb], 0, 0, 0);
+            }
+    }
+};
+// The order of what stands before and after stays.
+__device__ __forceinline__ void in_order() { __builtin_amdgcn_sched_barrier(0); }
+// A barrier that waits for nothing: reads of LDS may be under way across it.
+__device__ __forceinline__ void meet()
+{
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
 }
 
 // Mask, online softmax; leaves P^T (in 8 bits: times V's scales) as the B operand of PV: slot j of lane group lg in step kk is token
@@ -273,7 +350,6 @@ template <class G, int RB>
 __device__ __forceinline__ void softmax_tile(WaveState<G, RB>& st, floatx4 (&s)[G::TB][RB], bf16x8 (&pb)[G::TB / 2][RB],
                                              const uint32_t (&vs)[G::TB], int t0, bool masked, const int (&lim)[RB], int end, float c, int lane)
 {
-    const int lg = lane >> 4;
     float vscale[G::TB][4];
     if (G::QUANT) {
 #pragma unroll
@@ -283,6 +359,7 @@ __device__ __forceinline__ void softmax_tile(WaveState<G, RB>& st, floatx4 (&s)[
     }
     if (masked) {
         asm volatile("" : "+s"(t0));                       // a branch, not selects in every tile
+        const int lg = opaque(lane) >> 4;
 #pragma unroll
         for (int tb = 0; tb < G::TB; ++tb)
 #pragma unroll
@@ -298,10 +375,9 @@ __device__ __forceinline__ void softmax_tile(WaveState<G, RB>& st, floatx4 (&s)[
     bool above = false;
 #pragma unroll
     for (int rb = 0; rb < RB; ++rb) {
-        mx[rb] = fmaxf(fmaxf(s[0][rb][0], s[0][rb][1]), fmaxf(s[0][rb][2], s[0][rb][3]));
+        mx[rb] = s[0][rb][0];
 #pragma unroll
-        for (int tb = 1; tb < G::TB; ++tb)
-            mx[rb] = fmaxf(mx[rb], fmaxf(fmaxf(s[tb][rb][0], s[tb][rb][1]), fmaxf(s[tb][rb][2], s[tb][rb][3])));
+        for (int x = 1; x < G::TB * 4; ++x) mx[rb] = __builtin_elementwise_maximum(mx[rb], s[x / 4][rb][x % 4]);   // (a NaN stays one)
         above |= mx[rb] * c > st.m[rb] + kRescaleLog2;
     }
     if (__any(above)) {
@@ -344,7 +420,7 @@ __device__ __forceinline__ uint32_t not_finite(uint32_t w)
     return ((w & 0x7f80u) == 0x7f80u ? 0xffffu : 0u) | ((w & 0x7f800000u) == 0x7f800000u ? 0xffff0000u : 0u);
 }
 
-// O^T[column][row] += sum_token V[token][column] P[row][token].
+// O^T[column][row] += sum_token V[token][column] P[row][token], bf16.
 template <class G, int RB>
 __device__ __forceinline__ void pv_tile(WaveState<G, RB>& st, const bf16x8 (&pb)[G::TB / 2][RB], char* vt, int lane)
 {
@@ -353,26 +429,16 @@ __device__ __forceinline__ void pv_tile(WaveState<G, RB>& st, const bf16x8 (&pb)
     for (int kk = 0; kk < G::TB / 2; ++kk)
 #pragma unroll
         for (int db = 0; db < G::DB; ++db) {
-            bf16x8 va;
-            if constexpr (G::QUANT) {
-                // eight rows of 16 codes: lane i of a group gives the address of row i / 2, half i % 2, and gets column i
-                const int r = ln >> 1, row = kk * 32 + (r >> 2) * 16 + lg * 4 + (r & 3);
-                const int c = db ^ v_swz<true, G::ROWB>(row);
-                const i32x2 w = __builtin_amdgcn_ds_read_tr8_b64_v2i32(
-                    (i32x2 __attribute__((address_space(3)))*)(vt + row * G::ROWB + c * 16 + (ln & 1) * 8));
-                va = eight_values((uint32_t)w[0], (uint32_t)w[1], 1.0f);
-            } else {
-                s16x4 half[2];
+            s16x4 half[2];
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const int row = kk * 32 + h * 16 + lg * 4 + (ln >> 2);
-                    const int c = (db * 2) ^ v_swz<false, G::ROWB>(row);
-                    half[h] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                        (s16x4 __attribute__((address_space(3)))*)(vt + row * G::ROWB + c * 16 + (ln & 3) * 8));
-                }
-                const s16x8 both = __builtin_shufflevector(half[0], half[1], 0, 1, 2, 3, 4, 5, 6, 7);
-                va = __builtin_bit_cast(bf16x8, both);
+            for (int h = 0; h < 2; ++h) {
+                const int row = kk * 32 + h * 16 + lg * 4 + (ln >> 2);
+                const int c = (db * 2) ^ v_swz<false, G::ROWB>(row);
+                half[h] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                    (s16x4 __attribute__((address_space(3)))*)(vt + row * G::ROWB + c * 16 + (ln & 3) * 8));
             }
+            const s16x8 both = __builtin_shufflevector(half[0], half[1], 0, 1, 2, 3, 4, 5, 6, 7);
+            const bf16x8 va = __builtin_bit_cast(bf16x8, both);
 #pragma unroll
             for (int rb = 0; rb < RB; ++rb)
                 st.acc[db][rb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va, pb[kk][rb], st.acc[db][rb], 0, 0, 0);
@@ -386,6 +452,7 @@ template <class G>
 __device__ __forceinline__ bool take_not_finite(char* vt, int lane)
 {
     bool any = false;
+    lane = opaque(lane);
 #pragma unroll 1
     for (int x = 0; x < G::SLOT / 1024; ++x) {
         u32x4* at = reinterpret_cast<u32x4*>(vt + x * 1024 + lane * 16);
@@ -405,7 +472,7 @@ __device__ __forceinline__ bool take_not_finite(char* vt, int lane)
 template <class G, int RB, bool PAGED>
 __device__ __forceinline__ void add_not_finite(WaveState<G, RB>& st, const RowAddr& ra, int begin, int end, const int (&lim)[RB], int lane)
 {
-    const int lg = lane >> 4;
+    const int lg = opaque(lane) >> 4;
 #pragma unroll 1
     for (int t = begin; t < end; ++t) {
         const char* row = ra.v;
