@@ -170,6 +170,11 @@ def _strides(t: torch.Tensor):
                  for i, (n, s) in enumerate(zip(t.shape, t.stride())))
 
 
+def _sizes(*tensors):
+    """What a call's checks go by, for a key."""
+    return [None if t is None else (t.shape, t.stride(), t.dtype, t.device) for t in tensors]
+
+
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 
 
@@ -195,6 +200,7 @@ class Rapid:
         self._ws_args = (None, 0, None, 0)             # address and size of the exchange memory and of the workspace, as a call takes them
         self._ws_accept: Optional[torch.Tensor] = None
         self._ws_shared: list = []                     # workspaces of the quantised and the prefix attention, the last one in use
+        self._ws_shared_args = (None, 0)               # address and size of that one
         self._plans: dict = {}                         # shapes and layouts of calls by their sizes (_planned)
         self._sink: Optional[torch.Tensor] = None
 
@@ -411,18 +417,15 @@ class Rapid:
         return rel, cnt
 
     # ------------------------------------------------------------------ cache in 8 bits, shared prefix
-    def _planned(self, kind: str, scalars, tensors, plan):
-        """What a call of these sizes, strides, types and devices needs besides addresses: plan() checks them and answers, once for
-        each such call (the checks took three times as long as the rest of a small call)."""
-        key = (kind, scalars, tuple([None if t is None else (t.shape, t.stride(), t.dtype, t.device) for t in tensors]))
-        got = self._plans.get(key)
-        if got is None:
-            for t in tensors:
-                self._need(t is None or t.device == self.device, f"a tensor is not on {self.device}")
-            got = plan()
-            if len(self._plans) >= 1024:                       # sizes that change all the time
-                self._plans.clear()
-            self._plans[key] = got
+    def _planned(self, key, plan, *args):
+        """What a call of these sizes, strides, types and devices needs besides addresses: plan(*args) checks them and answers, once for
+        each key, which holds them all (the checks took three times as long as the rest of a small call)."""
+        for t in args:
+            self._need(not isinstance(t, torch.Tensor) or t.device == self.device, f"a tensor is not on {self.device}")
+        got = plan(*args)
+        if len(self._plans) >= 1024:                           # sizes that change all the time
+            self._plans.clear()
+        self._plans[key] = got
         return got
 
     @staticmethod
@@ -475,12 +478,11 @@ class Rapid:
         shape = AttnShape(batch, q_max, hq, hkv, d, ctx_max, gamma, scale, 0, st[1], st[2], st[0], tokens, page_table.shape[1], 0, rows, 0)
         return ctypes.byref(shape), ctypes.byref(QuantLayout(0, ss[1], ss[0]))
 
-    def _shared_workspace(self, nbytes: int) -> torch.Tensor:
+    def _shared_workspace(self, nbytes: int):
         # grows only, and what it has outgrown is kept: a captured graph goes on using the one that it was recorded with
-        if not self._ws_shared or self._ws_shared[-1].numel() < nbytes:
-            have = self._ws_shared[-1].numel() if self._ws_shared else 0
-            self._ws_shared.append(torch.empty(max(nbytes, 2 * have, 256), dtype=torch.uint8, device=self.device))
-        return self._ws_shared[-1]
+        ws = torch.empty(max(nbytes, 2 * self._ws_shared_args[1], 256), dtype=torch.uint8, device=self.device)
+        self._ws_shared.append(ws)
+        self._ws_shared_args = (ws.data_ptr(), ws.numel())
 
     def rapid_kv_append_quant(self, k_codes, v_codes, k_scales, v_scales, k_new, v_new, ctx_lens, gamma: Optional[int] = None, *,
                               gammas=None, page_table=None, max_ctx: Optional[int] = None):
@@ -488,20 +490,22 @@ class Rapid:
         every sequence (ctx_lens counts them).  k_codes/v_codes: float8_e4m3fn or uint8 [B,Lmax,Hkv,d] (any batch/token/head
         strides) or, with page_table, [n_pages,page,Hkv,d]; k_scales/v_scales: float8_e8m0fnu or uint8 [B,Hkv,Lmax] or
         [n_pages,Hkv,page], rows of a multiple of 16."""
-        def plan():
-            self._need(k_new.dim() == 4 and k_new.shape == v_new.shape and k_new.is_contiguous() and v_new.is_contiguous()
-                       and k_new.dtype == torch.bfloat16 and v_new.dtype == torch.bfloat16,
-                       "k_new and v_new: bf16 [B, Qmax, Hkv, d], contiguous")
-            self._need(k_new.shape[2:] == k_codes.shape[2:], "k_new and the cache differ in heads or head_dim")
-            self._check_lengths(k_new.shape[0], ctx_lens, gammas, page_table)
-            return self._quant_shape(*k_new.shape[:3], gamma, k_codes, v_codes, k_scales, v_scales, page_table, max_ctx, 1.0)
-        shape, layout = self._planned("append", (gamma, max_ctx), (k_codes, v_codes, k_scales, v_scales, k_new, v_new, ctx_lens, gammas,
-                                                                   page_table), plan)
+        key = ("append", gamma, max_ctx, *_sizes(k_codes, v_codes, k_scales, v_scales, k_new, v_new, ctx_lens, gammas, page_table))
+        shape, layout = self._plans.get(key) or self._planned(
+            key, self._plan_append, k_codes, v_codes, k_scales, v_scales, k_new, v_new, ctx_lens, gammas, page_table, gamma, max_ctx)
         rc = self.lib.rapid_kv_append_quant(self._ctx, shape, layout, k_new.data_ptr(), v_new.data_ptr(), ctx_lens.data_ptr(),
                                             _dptr(gammas), _dptr(page_table), k_codes.data_ptr(), v_codes.data_ptr(),
                                             k_scales.data_ptr(), v_scales.data_ptr(), _stream_ptr(self.device))
         if rc:
             _check(self.lib, rc, self._ctx)
+
+    def _plan_append(self, k_codes, v_codes, k_scales, v_scales, k_new, v_new, ctx_lens, gammas, page_table, gamma, max_ctx):
+        self._need(k_new.dim() == 4 and k_new.shape == v_new.shape and k_new.is_contiguous() and v_new.is_contiguous()
+                   and k_new.dtype == torch.bfloat16 and v_new.dtype == torch.bfloat16,
+                   "k_new and v_new: bf16 [B, Qmax, Hkv, d], contiguous")
+        self._need(k_new.shape[2:] == k_codes.shape[2:], "k_new and the cache differ in heads or head_dim")
+        self._check_lengths(k_new.shape[0], ctx_lens, gammas, page_table)
+        return self._quant_shape(*k_new.shape[:3], gamma, k_codes, v_codes, k_scales, v_scales, page_table, max_ctx, 1.0)
 
     def rapid_kv_read_quant(self, k_codes, v_codes, k_scales, v_scales, ctx_lens, rows: int, gamma: Optional[int] = None, *,
                             gammas=None, page_table=None, max_ctx: Optional[int] = None, outs=None):
@@ -511,15 +515,9 @@ class Rapid:
             shape = (ctx_lens.numel(), int(rows), *k_codes.shape[2:])
             outs = tuple(torch.empty(shape, dtype=torch.bfloat16, device=self.device) for _ in range(2))
         k_out, v_out = outs
-
-        def plan():
-            batch, (hkv, d) = ctx_lens.numel(), k_codes.shape[2:]
-            self._need(all(t.dtype == torch.bfloat16 and t.shape == (batch, rows, hkv, d) and t.is_contiguous() for t in outs),
-                       "outs: two of bf16 [B, rows, Hkv, d], contiguous")
-            self._check_lengths(batch, ctx_lens, gammas, page_table)
-            return self._quant_shape(batch, int(rows), hkv, gamma, k_codes, v_codes, k_scales, v_scales, page_table, max_ctx, 1.0)
-        shape, layout = self._planned("read", (rows, gamma, max_ctx), (k_codes, v_codes, k_scales, v_scales, k_out, v_out, ctx_lens, gammas,
-                                                                       page_table), plan)
+        key = ("read", rows, gamma, max_ctx, *_sizes(k_codes, v_codes, k_scales, v_scales, k_out, v_out, ctx_lens, gammas, page_table))
+        shape, layout = self._plans.get(key) or self._planned(
+            key, self._plan_read, k_codes, v_codes, k_scales, v_scales, k_out, v_out, ctx_lens, gammas, page_table, rows, gamma, max_ctx)
         rc = self.lib.rapid_kv_read_quant(self._ctx, shape, layout, k_codes.data_ptr(), v_codes.data_ptr(), k_scales.data_ptr(),
                                           v_scales.data_ptr(), ctx_lens.data_ptr(), _dptr(gammas), _dptr(page_table),
                                           k_out.data_ptr(), v_out.data_ptr(), _stream_ptr(self.device))
@@ -527,16 +525,12 @@ class Rapid:
             _check(self.lib, rc, self._ctx)
         return outs
 
-    def _attn_with_workspace(self, call, need, args, tail):
-        """An attention call on the shared workspace, which grows where it is too small: that is the call's last check, nothing has been
-        launched then."""
-        ws = self._ws_shared[-1] if self._ws_shared else None
-        rc = call(*args, _dptr(ws), 0 if ws is None else ws.numel(), tail)
-        if rc == RAPID_EWORKSPACE:
-            ws = self._shared_workspace(need())
-            rc = call(*args, ws.data_ptr(), ws.numel(), tail)
-        if rc:
-            _check(self.lib, rc, self._ctx)
+    def _plan_read(self, k_codes, v_codes, k_scales, v_scales, k_out, v_out, ctx_lens, gammas, page_table, rows, gamma, max_ctx):
+        batch, (hkv, d) = ctx_lens.numel(), k_codes.shape[2:]
+        self._need(all(t.dtype == torch.bfloat16 and t.shape == (batch, rows, hkv, d) and t.is_contiguous() for t in (k_out, v_out)),
+                   "outs: two of bf16 [B, rows, Hkv, d], contiguous")
+        self._check_lengths(batch, ctx_lens, gammas, page_table)
+        return self._quant_shape(batch, int(rows), hkv, gamma, k_codes, v_codes, k_scales, v_scales, page_table, max_ctx, 1.0)
 
     def rapid_verify_attn_quant(self, q, k_codes, v_codes, k_scales, v_scales, ctx_lens, gamma: Optional[int] = None, *, gammas=None,
                                 page_table=None, max_ctx: Optional[int] = None, softmax_scale: Optional[float] = None,
@@ -546,19 +540,26 @@ class Rapid:
         if out is None:
             out = torch.empty_like(q)
 
-        def plan():
-            self._check_attn(q, out, lse_out)
-            self._need(q.shape[3] == k_codes.shape[3], "q and the cache differ in head_dim")
-            self._check_lengths(q.shape[0], ctx_lens, gammas, page_table)
-            return self._quant_shape(*q.shape[:3], gamma, k_codes, v_codes, k_scales, v_scales, page_table, max_ctx, softmax_scale)
-        shape, layout = self._planned("attn", (gamma, max_ctx, softmax_scale),
-                                      (q, k_codes, v_codes, k_scales, v_scales, ctx_lens, gammas, page_table, out, lse_out), plan)
-        self._attn_with_workspace(self.lib.rapid_verify_attn_quant,
-                                  lambda: self.lib.rapid_verify_attn_quant_workspace_bytes(self._ctx, shape),
-                                  (self._ctx, shape, layout, q.data_ptr(), k_codes.data_ptr(), v_codes.data_ptr(),
-                                   k_scales.data_ptr(), v_scales.data_ptr(), ctx_lens.data_ptr(), _dptr(gammas), _dptr(page_table),
-                                   out.data_ptr(), _dptr(lse_out)), _stream_ptr(self.device))
+        key = ("attn", gamma, max_ctx, softmax_scale,
+               *_sizes(q, k_codes, v_codes, k_scales, v_scales, ctx_lens, gammas, page_table, out, lse_out))
+        shape, layout = self._plans.get(key) or self._planned(key, self._plan_attn, q, k_codes, v_codes, k_scales, v_scales, ctx_lens, gammas,
+                                                              page_table, out, lse_out, gamma, max_ctx, softmax_scale)
+        args = (self._ctx, shape, layout, q.data_ptr(), k_codes.data_ptr(), v_codes.data_ptr(), k_scales.data_ptr(),
+                v_scales.data_ptr(), ctx_lens.data_ptr(), _dptr(gammas), _dptr(page_table), out.data_ptr(), _dptr(lse_out))
+        call, stream = self.lib.rapid_verify_attn_quant, _stream_ptr(self.device)
+        rc = call(*args, *self._ws_shared_args, stream)
+        if rc == RAPID_EWORKSPACE:                             # the last check of the call: nothing has been launched
+            self._shared_workspace(self.lib.rapid_verify_attn_quant_workspace_bytes(self._ctx, shape))
+            rc = call(*args, *self._ws_shared_args, stream)
+        if rc:
+            _check(self.lib, rc, self._ctx)
         return out
+
+    def _plan_attn(self, q, k_codes, v_codes, k_scales, v_scales, ctx_lens, gammas, page_table, out, lse_out, gamma, max_ctx, softmax_scale):
+        self._check_attn(q, out, lse_out)
+        self._need(q.shape[3] == k_codes.shape[3], "q and the cache differ in head_dim")
+        self._check_lengths(q.shape[0], ctx_lens, gammas, page_table)
+        return self._quant_shape(*q.shape[:3], gamma, k_codes, v_codes, k_scales, v_scales, page_table, max_ctx, softmax_scale)
 
     def rapid_verify_attn_prefix(self, q, k_cache, v_cache, ctx_lens, prefix_len, gamma: Optional[int] = None, *, k_prefix=None,
                                  v_prefix=None, prefix_table=None, max_prefix: Optional[int] = None, gammas=None, page_table=None,
@@ -569,20 +570,25 @@ class Rapid:
         given).  ctx_lens counts a sequence's own tokens, which k_cache/v_cache hold as for rapid_verify_attn."""
         if out is None:
             out = torch.empty_like(q)
-        shape, prefix = self._planned(
-            "prefix", (gamma, max_prefix, max_ctx, softmax_scale),
-            (q, k_cache, v_cache, ctx_lens, prefix_len, k_prefix, v_prefix, prefix_table, gammas, page_table, out, lse_out),
-            lambda: self._prefix_shape(q, k_cache, v_cache, ctx_lens, prefix_len, gamma, k_prefix, v_prefix, prefix_table, max_prefix,
-                                       gammas, page_table, max_ctx, softmax_scale, out, lse_out))
-        self._attn_with_workspace(self.lib.rapid_verify_attn_prefix,
-                                  lambda: self.lib.rapid_verify_attn_prefix_workspace_bytes(self._ctx, shape, prefix),
-                                  (self._ctx, shape, prefix, q.data_ptr(), _dptr(k_prefix), _dptr(v_prefix), prefix_len.data_ptr(),
-                                   _dptr(prefix_table), k_cache.data_ptr(), v_cache.data_ptr(), ctx_lens.data_ptr(), _dptr(gammas),
-                                   _dptr(page_table), out.data_ptr(), _dptr(lse_out)), _stream_ptr(self.device))
+        key = ("prefix", gamma, max_prefix, max_ctx, softmax_scale,
+               *_sizes(q, k_cache, v_cache, ctx_lens, prefix_len, k_prefix, v_prefix, prefix_table, gammas, page_table, out, lse_out))
+        shape, prefix = self._plans.get(key) or self._planned(
+            key, self._plan_prefix, q, k_cache, v_cache, ctx_lens, prefix_len, k_prefix, v_prefix, prefix_table, gammas, page_table, out,
+            lse_out, gamma, max_prefix, max_ctx, softmax_scale)
+        args = (self._ctx, shape, prefix, q.data_ptr(), _dptr(k_prefix), _dptr(v_prefix), prefix_len.data_ptr(), _dptr(prefix_table),
+                k_cache.data_ptr(), v_cache.data_ptr(), ctx_lens.data_ptr(), _dptr(gammas), _dptr(page_table), out.data_ptr(),
+                _dptr(lse_out))
+        call, stream = self.lib.rapid_verify_attn_prefix, _stream_ptr(self.device)
+        rc = call(*args, *self._ws_shared_args, stream)
+        if rc == RAPID_EWORKSPACE:                             # the last check of the call: nothing has been launched
+            self._shared_workspace(self.lib.rapid_verify_attn_prefix_workspace_bytes(self._ctx, shape, prefix))
+            rc = call(*args, *self._ws_shared_args, stream)
+        if rc:
+            _check(self.lib, rc, self._ctx)
         return out
 
-    def _prefix_shape(self, q, k_cache, v_cache, ctx_lens, prefix_len, gamma, k_prefix, v_prefix, prefix_table, max_prefix, gammas,
-                      page_table, max_ctx, softmax_scale, out, lse_out):
+    def _plan_prefix(self, q, k_cache, v_cache, ctx_lens, prefix_len, k_prefix, v_prefix, prefix_table, gammas, page_table, out, lse_out,
+                     gamma, max_prefix, max_ctx, softmax_scale):
         self._check_attn(q, out, lse_out)
         self._check_lengths(q.shape[0], ctx_lens, gammas, page_table)
         self._need(k_cache.dtype == torch.bfloat16 and v_cache.dtype == torch.bfloat16 and k_cache.dim() == 4
