@@ -27,18 +27,22 @@ struct StreamLaunch {
     int32_t groups, nslots;     // shares of a kv head, groups + B - 1
     int32_t quantum;            // tokens that shares are cut by
     int32_t rot;                // 1: share g of slot x serves head (x + g) mod Hkv, 0: head x
+    int32_t direct;             // 1: short sequences, one workgroup for each and kv head, which writes the result; no partials
     float scale_log2e;
 };
 constexpr int kStreamRows = 96;      // packed rows that the streaming kernel takes
-// Fill the plan (RP .. rot) from the shape and the source's layout.
+// Fill the plan (RP .. direct) from the shape and the source's layout.
 void plan_attn_stream(StreamLaunch& a, int n_cu);
 void plan_attn_prefix(StreamLaunch& a, int n_cu);
-size_t attn_stream_workspace_bytes(const StreamLaunch& a);                       // of either plan
+// Both for one launch: the tokens of a shared prefix (at most kStreamRows rows) and the sequences' own.
+void plan_attn_stream_pair(StreamLaunch& own, StreamLaunch& prefix, int n_cu);
+size_t attn_stream_workspace_bytes(const StreamLaunch& a);                       // of any plan
 void bind_attn_stream(StreamLaunch& a, void* workspace);
 hipError_t configure_attn_stream();
 hipError_t configure_attn_prefix();
-// Write the partials.
+// Write the partials (direct: the result).
 hipError_t launch_attn_stream(const StreamLaunch& a, hipStream_t stream);
+hipError_t launch_attn_stream_pair(const StreamLaunch& own, const StreamLaunch& prefix, hipStream_t stream);
 hipError_t launch_attn_prefix(const StreamLaunch& a, hipStream_t stream);        // a shared prefix with more than kStreamRows rows
 // Joins the partials of `own`, and of a shared prefix where `prefix` has any (prefix.part_o not null).
 hipError_t launch_attn_stream_merge(const StreamLaunch& own, const StreamLaunch& prefix, hipStream_t stream);

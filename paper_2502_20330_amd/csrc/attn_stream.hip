@@ -40,9 +40,20 @@ struct Geo : TileGeo<D, QUANT, QUANT && D == 64 ? 4 : 2> {
     static constexpr int TILES = NP * RING + RP * QROWB;
     static constexpr int MERGE = NP * RP * OROW * 4;
     static constexpr int ML = TILES > MERGE ? TILES : MERGE;      // where the waves' (m, l) lie
-    static constexpr int TAKEN = ML + NW * (TEAMS ? (RB0 > RB1 ? RB0 : RB1) : RB0) * 16 * 8;   // a word for each stream
+    static constexpr int TAKEN = ML + NW * (TEAMS ? (RB0 > RB1 ? RB0 : RB1) : RB0) * 16 * 8 + RP * 4;   // behind the rows' sums: a word for each stream
     static constexpr int LDS = TAKEN + (TEAMS ? NP * 4 : 0);
 };
+
+// Where packed row `row` of (sequence b, kv head h) goes.
+__device__ __forceinline__ int64_t lse_index(const StreamLaunch& a, int b, int h, int row)
+{
+    return ((int64_t)b * a.Hq + h * a.G + row % a.G) * a.Qmax + row / a.G;
+}
+template <int D>
+__device__ __forceinline__ int64_t out_index(const StreamLaunch& a, int b, int h, int row)
+{
+    return (((int64_t)b * a.Qmax + row / a.G) * a.Hq + h * a.G + row % a.G) * D;
+}
 
 // ---- one piece: tokens [c0, c1) of one (sequence, kv head)
 struct Piece {
@@ -50,6 +61,7 @@ struct Piece {
     char *kring, *vring, *sring, *qlds;
     int* taken;                                   // teams: the stream's word for take_not_finite
     uint32_t kring_lds, vring_lds, sring_lds;
+    int b, h;
     int L, Q, R, c0, c1, first, nt, last_tok;     // first, nt: this stream's tiles (tokens c0 + (first + i) TT ..)
     int lane, wave, part, team;
 };
@@ -208,6 +220,7 @@ __device__ __forceinline__ void run_piece(const StreamLaunch& a, const Piece& w,
     }
     __syncthreads();                                     // all rings are dead from here on
     float own[RB];
+    float* sums = mlbuf + G::NW * MLS * 2;               // [RP], direct: the rows' sums
 #pragma unroll
     for (int rb = 0; rb < RB; ++rb) {
         float mw[G::NP], mm = kNoMaximum, ll = 0.f;
@@ -221,8 +234,13 @@ __device__ __forceinline__ void run_piece(const StreamLaunch& a, const Piece& w,
         own[rb] = fast_exp2(st.m[rb] - mm);
         const int row = row0 + rb * 16 + ln;
         if (w.part == 0 && lg == 0 && row < w.R) {
-            a.part_ml[(pbase + row) * 2 + 0] = mm;
-            a.part_ml[(pbase + row) * 2 + 1] = ll;
+            if (a.direct) {
+                sums[row] = ll;
+                if (a.lse_out) a.lse_out[lse_index(a, w.b, w.h, row)] = (mm + log2f(ll)) * 0.6931471805599453f;
+            } else {
+                a.part_ml[(pbase + row) * 2 + 0] = mm;
+                a.part_ml[(pbase + row) * 2 + 1] = ll;
+            }
         }
     }
     constexpr int DH = G::D / G::NH;
@@ -240,7 +258,14 @@ __device__ __forceinline__ void run_piece(const StreamLaunch& a, const Piece& w,
             floatx4 sum = *reinterpret_cast<const floatx4*>(obuf + row * G::OROW + x);
 #pragma unroll
             for (int p = 1; p < G::NP; ++p) sum += *reinterpret_cast<const floatx4*>(obuf + (p * G::RP + row) * G::OROW + x);
-            *reinterpret_cast<floatx4*>(a.part_o + (pbase + row) * G::D + half * DH + x) = sum;
+            if (a.direct) {
+                const float l = sums[row];
+                if (l != 0.f) sum /= l;
+                const bf16x4 o = {(__bf16)sum[0], (__bf16)sum[1], (__bf16)sum[2], (__bf16)sum[3]};
+                *reinterpret_cast<bf16x4*>(a.out + out_index<G::D>(a, w.b, w.h, row) + half * DH + x) = o;
+            } else {
+                *reinterpret_cast<floatx4*>(a.part_o + (pbase + row) * G::D + half * DH + x) = sum;
+            }
         }
         __syncthreads();                                 // before the buffer is written again, or becomes rings
     }
@@ -255,6 +280,8 @@ __device__ __forceinline__ void stream_piece(const StreamLaunch& a, char* smem, 
     w.wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     w.part = w.wave % G::NP;
     w.team = w.wave / G::NP;
+    w.b = b;
+    w.h = h;
     w.L = L;
     w.Q = seq_queries(a, b);
     w.R = w.Q * a.G;
@@ -322,17 +349,46 @@ __device__ __forceinline__ void stream_piece(const StreamLaunch& a, char* smem, 
     }
 }
 
-// Grid: one workgroup per (kv head, share).  Partials: [kv head][g + b], which no two pieces of a head share.
-template <class G, bool PAGED>
-__global__ void __launch_bounds__(G::NW * 64) attn_stream(StreamLaunch a)
+// What rows of a sequence there are none of, and all of one without tokens: zeros (lse: 0, and -infinity for rows that have nothing to attend).
+template <class G>
+__device__ __forceinline__ void write_missing_rows(const StreamLaunch& a, int b, int h, int L)
 {
-    extern __shared__ __attribute__((aligned(1024))) char smem[];
-    const int g = blockIdx.y;
+    const int R = seq_queries(a, b) * a.G, from = L > 0 ? R : 0, rows = a.Qmax * a.G;
+    for (int f = threadIdx.x; f < (rows - from) * (G::D / 8); f += G::NW * 64)
+        *reinterpret_cast<u32x4*>(a.out + out_index<G::D>(a, b, h, from + f / (G::D / 8)) + f % (G::D / 8) * 8) = u32x4{0, 0, 0, 0};
+    if (a.lse_out)
+        for (int row = from + threadIdx.x; row < rows; row += G::NW * 64) a.lse_out[lse_index(a, b, h, row)] = row < R ? -INFINITY : 0.f;
+}
+
+// Grid: one workgroup per (kv head, share).  Partials: [kv head][g + b], which no two pieces of a head share.  Direct: per (kv head, sequence).
+template <class G, bool PAGED>
+__device__ __forceinline__ void stream_share(const StreamLaunch& a, char* smem, int g)
+{
     const int h = __builtin_amdgcn_readfirstlane(a.rot ? (blockIdx.x + g) % a.Hkv : blockIdx.x);     // (base addresses go through scalar registers)
+    if (a.direct) {
+        const int L = __builtin_amdgcn_readfirstlane(seq_len(a, g));
+        write_missing_rows<G>(a, g, h, L);
+        if (L > 0) stream_piece<G, PAGED>(a, smem, g, h, L, 0, L, 0);
+        return;
+    }
     for_each_piece(a, g, threadIdx.x & 63, G::QUANTUM, [&](int b, int L, int c0, int c1) {
         stream_piece<G, PAGED>(a, smem, b, h, L, c0, c1, ((int64_t)h * a.nslots + g + b) * G::RP);
         wait_loads<0>();                                 // the partial's stores are out of the load account
     });
+}
+template <class G, bool PAGED>
+__global__ void __launch_bounds__(G::NW * 64) attn_stream(StreamLaunch a)
+{
+    extern __shared__ __attribute__((aligned(1024))) char smem[];
+    stream_share<G, PAGED>(a, smem, blockIdx.y);
+}
+// Two in one launch: the shares of a prefix, then those of the sequences' own tokens.
+template <class G, bool OWN_PAGED, bool PREFIX_PAGED>
+__global__ void __launch_bounds__(G::NW * 64) attn_stream_pair(StreamLaunch own, StreamLaunch prefix)
+{
+    extern __shared__ __attribute__((aligned(1024))) char smem[];
+    if ((int)blockIdx.y < prefix.groups) stream_share<G, PREFIX_PAGED>(prefix, smem, blockIdx.y);
+    else stream_share<G, OWN_PAGED>(own, smem, blockIdx.y - prefix.groups);
 }
 
 // The partials of one row: `n` of them, from row slot `slot` on, RP slots apart.
@@ -362,33 +418,58 @@ __device__ __forceinline__ Partials find_partials(const StreamLaunch& a, int b, 
     }
     return p;
 }
-// Folds them into the row's state and this thread's column.
-template <int D>
-__device__ __forceinline__ void fold_partials(const StreamLaunch& a, const Partials& p, int d, RowMerge& r, float& num)
-{
-    constexpr int SB = kMergeBlock;
-    for (int s0 = 0; s0 < p.n; s0 += SB) {
-        const int nb = min(SB, p.n - s0), sl = d & (SB - 1);
-        const float* po = a.part_o + (p.slot + (int64_t)s0 * a.RP) * D + d;
-        float o[SB];
+// A block of up to kMergeBlock of them on its way: this thread's column of each, and (maximum, sum) of one.
+struct PartialBlock {
+    float o[kMergeBlock], m, l;
+    template <int D>
+    __device__ __forceinline__ void load(const StreamLaunch& a, int64_t slot, int n, int d)
+    {
+        const float* po = a.part_o + slot * D + d;
 #pragma unroll
-        for (int j = 0; j < SB; ++j) o[j] = j < nb ? po[(int64_t)j * a.RP * D] : 0.f;
-        float ms = -INFINITY, ls = 0.f;
-        if (sl < nb) {
-            const float* ml = a.part_ml + (p.slot + (int64_t)(s0 + sl) * a.RP) * 2;
-            ms = ml[0];
-            ls = ml[1];
+        for (int j = 0; j < kMergeBlock; ++j) o[j] = j < n ? po[(int64_t)j * a.RP * D] : 0.f;
+        const int sl = d & (kMergeBlock - 1);
+        m = -INFINITY;
+        l = 0.f;
+        if (sl < n) {
+            const float* ml = a.part_ml + (slot + (int64_t)sl * a.RP) * 2;
+            m = ml[0];
+            l = ml[1];
         }
+    }
+    // Folds the first n into the row's state and this thread's column; the others may be anything.
+    __device__ __forceinline__ void fold(int n, int d, RowMerge& r, float& num)
+    {
+        const bool there = (d & (kMergeBlock - 1)) < n;
         float resc;
-        const float w = r.block(ms, ls, &resc);
+        const float w = r.block(there ? m : -INFINITY, there ? l : 0.f, &resc);
         float acc0 = 0.f, acc1 = 0.f;
 #pragma unroll
-        for (int j = 0; j < SB; j += 2) {
-            acc0 = fmaf(lane_of(w, j), o[j], acc0);
-            acc1 = fmaf(lane_of(w, j + 1), o[j + 1], acc1);
+        for (int j = 0; j < kMergeBlock; j += 2) {
+            acc0 = fmaf(lane_of(w, j), j < n ? o[j] : 0.f, acc0);
+            acc1 = fmaf(lane_of(w, j + 1), j + 1 < n ? o[j + 1] : 0.f, acc1);
         }
         num = num * resc + (acc0 + acc1);
     }
+};
+template <int D>
+__device__ __forceinline__ void fold_partials(const StreamLaunch& a, int64_t slot, int n, int d, RowMerge& r, float& num)
+{
+    for (int s0 = 0; s0 < n; s0 += kMergeBlock) {
+        PartialBlock x;
+        x.load<D>(a, slot + (int64_t)s0 * a.RP, n - s0, d);
+        x.fold(n - s0, d, r, num);
+    }
+}
+// Those of a single sequence (b = 0), whose first share is share 0 whatever its length: the first block is asked for before the length is known.
+template <int D>
+__device__ __forceinline__ void fold_single(const StreamLaunch& a, int h, int row, int d, RowMerge& r, float& num, bool wanted = true)
+{
+    const int64_t slot = (int64_t)(h * a.tiles + row / a.RP) * a.nslots * a.RP + row % a.RP;
+    PartialBlock x;
+    x.load<D>(a, slot, a.nslots, d);
+    const int n = wanted ? find_partials(a, 0, h, row, d & 63).n : 0;
+    x.fold(n, d, r, num);
+    fold_partials<D>(a, slot + (int64_t)kMergeBlock * a.RP, n - kMergeBlock, d, r, num);
 }
 
 // One workgroup of D threads per (sequence, kv head, packed row): out = sum 2^(m_s - M) O_s / sum 2^(m_s - M) l_s, over the row's partials of the
@@ -397,25 +478,25 @@ template <int D, bool PREFIX>
 __global__ void __launch_bounds__(D) attn_stream_merge(StreamLaunch a, StreamLaunch prefix)
 {
     const int row = blockIdx.x, h = blockIdx.y, b = blockIdx.z;
-    const int d = threadIdx.x, lane = d & 63;
-    const int R = seq_queries(a, b) * a.G;
-    const int qi = row / a.G, hq = h * a.G + row % a.G;
-    uint16_t* dst = a.out + (((int64_t)b * a.Qmax + qi) * a.Hq + hq) * D + d;
-    if (row >= R) {                                       // query rows this sequence does not have
+    const int d = threadIdx.x;
+    uint16_t* dst = a.out + out_index<D>(a, b, h, row) + d;
+    if (row >= seq_queries(a, b) * a.G) {                 // query rows this sequence does not have
         *dst = 0;
-        if (a.lse_out && d == 0) a.lse_out[((int64_t)b * a.Hq + hq) * a.Qmax + qi] = 0.f;
+        if (a.lse_out && d == 0) a.lse_out[lse_index(a, b, h, row)] = 0.f;
         return;
     }
     RowMerge r;
     float num = 0.f;
-    const Partials own = find_partials(a, b, h, row, lane);
-    if (own.n) {                                          // else a sequence without tokens
-        if (PREFIX) fold_partials<D>(prefix, find_partials(prefix, 0, h, b * a.Qmax * a.G + row, lane), d, r, num);
-        fold_partials<D>(a, own, d, r, num);
+    if (PREFIX) fold_single<D>(prefix, h, b * a.Qmax * a.G + row, d, r, num, seq_len(a, b) > 0);     // (a sequence without tokens has no rows)
+    if (a.B == 1) {
+        fold_single<D>(a, h, row, d, r, num);
+    } else {
+        const Partials own = find_partials(a, b, h, row, d & 63);
+        fold_partials<D>(a, own.slot, own.n, d, r, num);
     }
     const __bf16 o = (__bf16)(r.den == 0.f ? 0.f : num / r.den);
     *dst = __builtin_bit_cast(uint16_t, o);
-    if (a.lse_out && d == 0) a.lse_out[((int64_t)b * a.Hq + hq) * a.Qmax + qi] = (r.M + log2f(r.den)) * 0.6931471805599453f;
+    if (a.lse_out && d == 0) a.lse_out[lse_index(a, b, h, row)] = (r.M + log2f(r.den)) * 0.6931471805599453f;
 }
 
 // Calls f(Geo, paged) for the kernel that a shape takes; row blocks 1..6.
@@ -449,37 +530,72 @@ hipError_t configure_attn_stream()
                 const hipError_t e = with_geo(D, quant, rb, [](auto geo) {
                     using G = decltype(geo);
                     static_assert(G::LDS <= 160 * 1024, "LDS of a compute unit");
-                    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(attn_stream<G, false>),
-                                                             hipFuncAttributeMaxDynamicSharedMemorySize, G::LDS);
-                    if (e != hipSuccess) return e;
-                    return hipFuncSetAttribute(reinterpret_cast<const void*>(attn_stream<G, true>),
-                                               hipFuncAttributeMaxDynamicSharedMemorySize, G::LDS);
+                    auto raise = [](auto fn) {
+                        return hipFuncSetAttribute(reinterpret_cast<const void*>(fn), hipFuncAttributeMaxDynamicSharedMemorySize, G::LDS);
+                    };
+                    hipError_t e = raise(attn_stream<G, false>);
+                    if (e == hipSuccess) e = raise(attn_stream<G, true>);
+                    if constexpr (!G::QUANT) {
+                        if (e == hipSuccess) e = raise(attn_stream_pair<G, false, false>);
+                        if (e == hipSuccess) e = raise(attn_stream_pair<G, true, false>);
+                        if (e == hipSuccess) e = raise(attn_stream_pair<G, true, true>);
+                    }
+                    return e;
                 });
                 if (e != hipSuccess) return e;
             }
     return hipSuccess;
 }
 
-void plan_attn_stream(StreamLaunch& a, int n_cu)
+namespace {
+
+// One workgroup for each sequence and kv head, which writes the result, spares a launch and the partials, and gives up sharing out the tokens.  Up to two
+// quanta there is little to share (us a call, one sequence, 8 kv heads of 128, 4 and 36 rows: 512 tokens 8.4 and 12.3 instead of 11.1 and 14.0;
+// 1024 tokens 10.8 and 16.6 instead of 11.0 and 14.4), and up to eight it pays where the sequences occupy at least half of the compute units anyhow, in one
+// round (16 sequences, 20 rows: 512 tokens 11.4 instead of 18, 1024 14.3 instead of 20, 2048 19.7 instead of 24.5).
+constexpr int kDirectQuanta = 2, kDirectBatchQuanta = 8;
+
+void plan_shares(StreamLaunch& a, int rb, int groups)
 {
-    const int rb = (a.Qmax * a.G + 15) / 16;
     a.RP = rb * 16;
     a.tiles = 1;
-    a.groups = n_cu > a.Hkv ? n_cu / a.Hkv : 1;          // a workgroup takes a compute unit's LDS
-    // no more shares than the longest possible batch has quanta
     (void)with_geo(a.D, a.own.ks != nullptr, rb, [&](auto geo) {
         a.quantum = decltype(geo)::QUANTUM;
         return hipSuccess;
     });
+    // no more shares than the longest possible batch has quanta
     const int64_t most = (int64_t)a.B * (((int64_t)a.max_ctx + a.quantum - 1) / a.quantum + kPieceQuanta);
+    a.groups = groups < 1 ? 1 : groups;
     if (a.groups > most) a.groups = (int)most;
     a.nslots = a.groups + a.B - 1;
     // heads whose rows are contiguous are spread over the dies, heads inside a token's row run side by side
     a.rot = a.own.hstride > a.own.tstride && a.Hkv > 1;
 }
 
+}  // namespace
+
+// A workgroup takes a compute unit's LDS.
+void plan_attn_stream(StreamLaunch& a, int n_cu)
+{
+    plan_shares(a, (a.Qmax * a.G + 15) / 16, n_cu / a.Hkv);
+    const int64_t units = (int64_t)a.B * a.Hkv;
+    const int quanta = 2 * units >= n_cu && units <= n_cu ? kDirectBatchQuanta : kDirectQuanta;
+    a.direct = a.max_ctx <= quanta * a.quantum;
+}
+
+void plan_attn_stream_pair(StreamLaunch& own, StreamLaunch& prefix, int n_cu)
+{
+    const int rb = (prefix.Qmax * prefix.G + 15) / 16, each = n_cu / own.Hkv;
+    const int64_t tokens = (int64_t)own.B * own.max_ctx;
+    int mine = (int)(each * tokens / (tokens + prefix.max_ctx));       // of the compute units, by what there may be to read
+    if (mine < 1) mine = 1;
+    plan_shares(own, rb, mine);
+    plan_shares(prefix, rb, each - own.groups);
+}
+
 size_t attn_stream_workspace_bytes(const StreamLaunch& a)
 {
+    if (a.direct) return 256;
     const size_t rows = (size_t)a.Hkv * a.tiles * a.nslots * a.RP;
     return (rows * a.D * 4 + 255) / 256 * 256 + (rows * 8 + 255) / 256 * 256;
 }
@@ -496,8 +612,22 @@ hipError_t launch_attn_stream(const StreamLaunch& a, hipStream_t stream)
     return with_geo(a.D, a.own.ks != nullptr, a.RP / 16, [&](auto geo) {
         using G = decltype(geo);
         auto fn = a.own.page_table ? attn_stream<G, true> : attn_stream<G, false>;
-        hipLaunchKernelGGL(fn, dim3(a.Hkv, a.groups), dim3(G::NW * 64), G::LDS, stream, a);
+        hipLaunchKernelGGL(fn, dim3(a.Hkv, a.direct ? a.B : a.groups), dim3(G::NW * 64), G::LDS, stream, a);
         return hipGetLastError();
+    });
+}
+
+hipError_t launch_attn_stream_pair(const StreamLaunch& own, const StreamLaunch& prefix, hipStream_t stream)
+{
+    return with_geo(own.D, false, own.RP / 16, [&](auto geo) {
+        using G = decltype(geo);
+        if constexpr (!G::QUANT) {
+            auto fn = prefix.own.page_table ? attn_stream_pair<G, true, true>
+                                            : own.own.page_table ? attn_stream_pair<G, true, false> : attn_stream_pair<G, false, false>;
+            hipLaunchKernelGGL(fn, dim3(own.Hkv, own.groups + prefix.groups), dim3(G::NW * 64), G::LDS, stream, own, prefix);
+            return hipGetLastError();
+        }
+        return hipErrorInvalidValue;
     });
 }
 

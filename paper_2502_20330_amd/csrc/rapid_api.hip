@@ -304,8 +304,8 @@ int check_prefix_place(const rapid_attn_shape* s, const rapid_prefix_layout* p, 
     return p->token_stride * 2 * p->max_prefix < (int64_t)1 << 32 ? RAPID_OK : RAPID_EUNSUPPORTED;
 }
 
-// The streaming kernel's plan for a shape.
-StreamLaunch stream_launch(const rapid_ctx* ctx, const rapid_attn_shape* s, const AttnSource& own)
+// A call's shape for the kernels that divide the batch's tokens by themselves.
+StreamLaunch stream_shape(const rapid_attn_shape* s, const AttnSource& own)
 {
     StreamLaunch a{};
     a.own = own;
@@ -318,28 +318,44 @@ StreamLaunch stream_launch(const rapid_ctx* ctx, const rapid_attn_shape* s, cons
     a.gamma = s->gamma;
     a.max_ctx = s->max_ctx;
     a.scale_log2e = s->softmax_scale * 1.4426950408889634f;
-    plan_attn_stream(a, ctx && ctx->n_cu > 0 ? ctx->n_cu : 256);
     return a;
 }
-// And for the rows of all its sequences over the shared prefix at `source`.
-StreamLaunch prefix_launch(const rapid_ctx* ctx, const rapid_attn_shape* s, int max_prefix, const AttnSource& source)
+int compute_units(const rapid_ctx* ctx) { return ctx && ctx->n_cu > 0 ? ctx->n_cu : 256; }
+StreamLaunch plan_quant(const rapid_ctx* ctx, const rapid_attn_shape* s, const AttnSource& own)
 {
-    StreamLaunch a{};
-    a.own = source;
-    a.shared = 1;
-    a.B = 1;
-    a.Qmax = s->batch * s->q_max;
-    a.Hq = s->n_q_heads;
-    a.Hkv = s->n_kv_heads;
-    a.G = a.Hq / a.Hkv;
-    a.D = s->head_dim;
-    a.gamma = a.Qmax - 1;
-    a.max_ctx = max_prefix;
-    a.scale_log2e = s->softmax_scale * 1.4426950408889634f;
-    const int n_cu = ctx && ctx->n_cu > 0 ? ctx->n_cu : 256;
-    if (a.Qmax * a.G > kStreamRows) plan_attn_prefix(a, n_cu);
-    else plan_attn_stream(a, n_cu);
+    StreamLaunch a = stream_shape(s, own);
+    plan_attn_stream(a, compute_units(ctx));
     return a;
+}
+// The sequences' own tokens, and the shared prefix with the rows of all of them.
+struct PrefixPlan {
+    StreamLaunch own, prefix;
+    size_t own_bytes, bytes;    // of the workspace
+    bool pair;                  // both in one launch
+};
+PrefixPlan plan_prefix(const rapid_ctx* ctx, const rapid_attn_shape* s, int max_prefix, const AttnSource& own, const AttnSource& prefix)
+{
+    PrefixPlan p{stream_shape(s, own), stream_shape(s, prefix), 0, 0, false};
+    const int n_cu = compute_units(ctx);
+    p.prefix.shared = 1;
+    p.prefix.B = 1;
+    p.prefix.Qmax = s->batch * s->q_max;
+    p.prefix.gamma = p.prefix.Qmax - 1;
+    p.prefix.max_ctx = max_prefix;
+    const bool few = p.prefix.Qmax * p.prefix.G <= kStreamRows;
+    p.pair = max_prefix > 0 && few;
+    if (p.pair) {
+        plan_attn_stream_pair(p.own, p.prefix, n_cu);
+    } else {
+        plan_attn_stream(p.own, n_cu);
+        if (max_prefix > 0) {
+            p.own.direct = 0;
+            plan_attn_prefix(p.prefix, n_cu);
+        }
+    }
+    p.own_bytes = attn_stream_workspace_bytes(p.own);
+    p.bytes = p.own_bytes + (max_prefix > 0 ? attn_stream_workspace_bytes(p.prefix) : 0);
+    return p;
 }
 
 }  // namespace
@@ -857,7 +873,7 @@ size_t rapid_verify_attn_quant_workspace_bytes(const rapid_ctx* ctx, const rapid
     if (check_quant_shape(shape, true) != RAPID_OK) return 0;
     AttnSource own{};
     own.ks = own.vs = reinterpret_cast<const uint8_t*>(1);      // a cache in 8 bits; nothing is read
-    return attn_stream_workspace_bytes(stream_launch(ctx, shape, own));
+    return attn_stream_workspace_bytes(plan_quant(ctx, shape, own));
 }
 
 int rapid_verify_attn_quant(rapid_ctx* ctx, const rapid_attn_shape* shape, const rapid_quant_layout* layout, const void* q,
@@ -879,7 +895,7 @@ int rapid_verify_attn_quant(rapid_ctx* ctx, const rapid_attn_shape* shape, const
     own.sbstride = layout->scale_batch_stride;
     own.shstride = layout->scale_head_stride;
     own.spstride = layout->scale_page_stride;
-    StreamLaunch a = stream_launch(ctx, shape, own);
+    StreamLaunch a = plan_quant(ctx, shape, own);
     if (!workspace || !aligned(workspace, 256) || workspace_bytes < attn_stream_workspace_bytes(a)) return RAPID_EWORKSPACE;
     bind_attn_stream(a, workspace);
     a.q = static_cast<const uint16_t*>(q);
@@ -890,7 +906,7 @@ int rapid_verify_attn_quant(rapid_ctx* ctx, const rapid_attn_shape* shape, const
     DeviceScope dev(ctx->device);
     if (dev.err != hipSuccess) return hip_fail(ctx, dev.err);
     hipError_t e = launch_attn_stream(a, static_cast<hipStream_t>(stream));
-    if (e == hipSuccess) e = launch_attn_stream_merge(a, StreamLaunch{}, static_cast<hipStream_t>(stream));
+    if (e == hipSuccess && !a.direct) e = launch_attn_stream_merge(a, StreamLaunch{}, static_cast<hipStream_t>(stream));
     if (e != hipSuccess) return hip_fail(ctx, e);
     return RAPID_OK;
 }
@@ -898,8 +914,7 @@ int rapid_verify_attn_quant(rapid_ctx* ctx, const rapid_attn_shape* shape, const
 size_t rapid_verify_attn_prefix_workspace_bytes(const rapid_ctx* ctx, const rapid_attn_shape* shape, const rapid_prefix_layout* prefix)
 {
     if (check_prefix_shape(shape, prefix) != RAPID_OK) return 0;
-    const size_t own = attn_stream_workspace_bytes(stream_launch(ctx, shape, AttnSource{}));
-    return prefix->max_prefix ? own + attn_stream_workspace_bytes(prefix_launch(ctx, shape, prefix->max_prefix, AttnSource{})) : own;
+    return plan_prefix(ctx, shape, prefix->max_prefix, AttnSource{}, AttnSource{}).bytes;
 }
 
 int rapid_verify_attn_prefix(rapid_ctx* ctx, const rapid_attn_shape* shape, const rapid_prefix_layout* prefix, const void* q,
@@ -918,41 +933,41 @@ int rapid_verify_attn_prefix(rapid_ctx* ctx, const rapid_attn_shape* shape, cons
     if (rc != RAPID_OK) return rc;
     if (!aligned(q, 16) || !aligned(k_cache, 16) || !aligned(v_cache, 16) || !aligned(k_prefix, 16) || !aligned(v_prefix, 16) ||
         !aligned(out, 16)) return RAPID_EALIGN;
-    StreamLaunch a = stream_launch(ctx, shape, source_of(shape, k_cache, v_cache, page_table));
-    StreamLaunch p{};
-    if (prefix->max_prefix) {
-        AttnSource source{};
-        if (prefix_table) {
-            source = source_of(shape, k_cache, v_cache, prefix_table);
-            source.max_pages = prefix->max_pages;
-        } else {
-            source.k = k_prefix;
-            source.v = v_prefix;
-            source.tstride = prefix->token_stride;
-            source.hstride = prefix->head_stride;
-        }
-        p = prefix_launch(ctx, shape, prefix->max_prefix, source);
+    AttnSource source{};
+    if (prefix_table) {
+        source = source_of(shape, k_cache, v_cache, prefix_table);
+        source.max_pages = prefix->max_pages;
+    } else {
+        source.k = k_prefix;
+        source.v = v_prefix;
+        source.tstride = prefix->token_stride;
+        source.hstride = prefix->head_stride;
     }
-    const size_t own_bytes = attn_stream_workspace_bytes(a), need = own_bytes + (prefix->max_prefix ? attn_stream_workspace_bytes(p) : 0);
-    if (!workspace || !aligned(workspace, 256) || workspace_bytes < need) return RAPID_EWORKSPACE;
+    PrefixPlan p = plan_prefix(ctx, shape, prefix->max_prefix, source_of(shape, k_cache, v_cache, page_table), source);
+    if (!workspace || !aligned(workspace, 256) || workspace_bytes < p.bytes) return RAPID_EWORKSPACE;
+    StreamLaunch& a = p.own;
     bind_attn_stream(a, workspace);
     a.q = static_cast<const uint16_t*>(q);
     a.out = static_cast<uint16_t*>(out);
     a.lse_out = lse_out;
     a.ctx_lens = ctx_lens;
     a.gammas = gammas;
+    if (prefix->max_prefix) {
+        bind_attn_stream(p.prefix, static_cast<char*>(workspace) + p.own_bytes);
+        p.prefix.q = a.q;
+        p.prefix.ctx_lens = prefix_len;
+    }
     hipStream_t st = static_cast<hipStream_t>(stream);
     DeviceScope dev(ctx->device);
     if (dev.err != hipSuccess) return hip_fail(ctx, dev.err);
     hipError_t e = hipSuccess;
-    if (prefix->max_prefix) {
-        bind_attn_stream(p, static_cast<char*>(workspace) + own_bytes);
-        p.q = a.q;
-        p.ctx_lens = prefix_len;
-        e = p.Qmax * p.G > kStreamRows ? launch_attn_prefix(p, st) : launch_attn_stream(p, st);
+    if (p.pair) {
+        e = launch_attn_stream_pair(a, p.prefix, st);
+    } else {
+        if (prefix->max_prefix) e = launch_attn_prefix(p.prefix, st);
+        if (e == hipSuccess) e = launch_attn_stream(a, st);
     }
-    if (e == hipSuccess) e = launch_attn_stream(a, st);
-    if (e == hipSuccess) e = launch_attn_stream_merge(a, p, st);
+    if (e == hipSuccess && !a.direct) e = launch_attn_stream_merge(a, p.prefix, st);
     if (e != hipSuccess) return hip_fail(ctx, e);
     return RAPID_OK;
 }
