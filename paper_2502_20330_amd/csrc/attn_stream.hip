@@ -382,13 +382,14 @@ __global__ void __launch_bounds__(G::NW * 64) attn_stream(StreamLaunch a)
     extern __shared__ __attribute__((aligned(1024))) char smem[];
     stream_share<G, PAGED>(a, smem, blockIdx.y);
 }
-// Two in one launch: the shares of a prefix, then those of the sequences' own tokens.
-template <class G, bool OWN_PAGED, bool PREFIX_PAGED>
+// bf16: two in one launch, the shares of a prefix (or none), then those of the sequences' own tokens; both paged or neither.
+template <class G, bool PAGED>
 __global__ void __launch_bounds__(G::NW * 64) attn_stream_pair(StreamLaunch own, StreamLaunch prefix)
 {
     extern __shared__ __attribute__((aligned(1024))) char smem[];
-    if ((int)blockIdx.y < prefix.groups) stream_share<G, PREFIX_PAGED>(prefix, smem, blockIdx.y);
-    else stream_share<G, OWN_PAGED>(own, smem, blockIdx.y - prefix.groups);
+    const bool first = (int)blockIdx.y < prefix.groups;
+    const StreamLaunch a = first ? prefix : own;
+    stream_share<G, PAGED>(a, smem, first ? blockIdx.y : blockIdx.y - prefix.groups);
 }
 
 // The partials of one row: `n` of them, from row slot `slot` on, RP slots apart.
@@ -533,14 +534,13 @@ hipError_t configure_attn_stream()
                     auto raise = [](auto fn) {
                         return hipFuncSetAttribute(reinterpret_cast<const void*>(fn), hipFuncAttributeMaxDynamicSharedMemorySize, G::LDS);
                     };
-                    hipError_t e = raise(attn_stream<G, false>);
-                    if (e == hipSuccess) e = raise(attn_stream<G, true>);
-                    if constexpr (!G::QUANT) {
-                        if (e == hipSuccess) e = raise(attn_stream_pair<G, false, false>);
-                        if (e == hipSuccess) e = raise(attn_stream_pair<G, true, false>);
-                        if (e == hipSuccess) e = raise(attn_stream_pair<G, true, true>);
+                    if constexpr (G::QUANT) {
+                        const hipError_t e = raise(attn_stream<G, false>);
+                        return e == hipSuccess ? raise(attn_stream<G, true>) : e;
+                    } else {
+                        const hipError_t e = raise(attn_stream_pair<G, false>);
+                        return e == hipSuccess ? raise(attn_stream_pair<G, true>) : e;
                     }
-                    return e;
                 });
                 if (e != hipSuccess) return e;
             }
@@ -611,19 +611,28 @@ hipError_t launch_attn_stream(const StreamLaunch& a, hipStream_t stream)
 {
     return with_geo(a.D, a.own.ks != nullptr, a.RP / 16, [&](auto geo) {
         using G = decltype(geo);
-        auto fn = a.own.page_table ? attn_stream<G, true> : attn_stream<G, false>;
-        hipLaunchKernelGGL(fn, dim3(a.Hkv, a.direct ? a.B : a.groups), dim3(G::NW * 64), G::LDS, stream, a);
+        const dim3 grid(a.Hkv, a.direct ? a.B : a.groups), block(G::NW * 64);
+        if constexpr (G::QUANT) {
+            auto fn = a.own.page_table ? attn_stream<G, true> : attn_stream<G, false>;
+            hipLaunchKernelGGL(fn, grid, block, G::LDS, stream, a);
+        } else {
+            auto fn = a.own.page_table ? attn_stream_pair<G, true> : attn_stream_pair<G, false>;
+            hipLaunchKernelGGL(fn, grid, block, G::LDS, stream, a, StreamLaunch{});
+        }
         return hipGetLastError();
     });
 }
 
 hipError_t launch_attn_stream_pair(const StreamLaunch& own, const StreamLaunch& prefix, hipStream_t stream)
 {
+    if (!prefix.own.page_table != !own.own.page_table) {               // (rare: a prefix of its own beside paged sequences)
+        const hipError_t e = launch_attn_stream(prefix, stream);
+        return e == hipSuccess ? launch_attn_stream(own, stream) : e;
+    }
     return with_geo(own.D, false, own.RP / 16, [&](auto geo) {
         using G = decltype(geo);
         if constexpr (!G::QUANT) {
-            auto fn = prefix.own.page_table ? attn_stream_pair<G, true, true>
-                                            : own.own.page_table ? attn_stream_pair<G, true, false> : attn_stream_pair<G, false, false>;
+            auto fn = own.own.page_table ? attn_stream_pair<G, true> : attn_stream_pair<G, false>;
             hipLaunchKernelGGL(fn, dim3(own.Hkv, own.groups + prefix.groups), dim3(G::NW * 64), G::LDS, stream, own, prefix);
             return hipGetLastError();
         }
