@@ -387,7 +387,7 @@ int rapid_kv_commit_pages(rapid_ctx* ctx, const rapid_attn_shape* shape, const i
  *     code[c] = x_c * 2^-k, clamped to [-448, 448] and rounded to e4m3 (nearest, ties to even);  NaN where x_c is NaN or infinite
  * Scales are powers of two, so that x_c * 2^-k has no rounding of its own, the stored value is a bf16 number, and rows read back and written again
  * keep their values.  Where the row's largest lies between 2^-91 and 448 * 2^119, elements within 2^13 of it are at most 2^-4 of themselves off,
- * smaller ones 2^-17 of the largest.
+ * smaller ones 2^-17 of the largest.  Scale bytes are thus 27 .. 246; what a token with another one stands for is not defined.
  *
  * The codes are addressed as rapid_attn_shape says, its strides in elements, here bytes: multiples of 16.
  * The scale byte of (b, token j, kv head h) lies at
@@ -418,6 +418,8 @@ typedef struct rapid_quant_layout {
  * exist and lse_out, computed on the stored values with fp32 accumulation; weights are rounded to bf16 before the second product.  A NaN
  * in a token's K or V reaches the rows that attend this token and no others.
  *   chunk_tokens and ctx_sum_hint are not used: the kernel divides the tokens of the batch by itself
+ *   sums are formed before they are divided: 2^8 times the sum of a column's |v| has to stay within fp32's range
+ *   batch * max_ctx is at most 2^35, max_ctx 2^30
  *   workspace   >= rapid_verify_attn_quant_workspace_bytes(), 256-byte aligned, any content
  */
 int rapid_kv_append_quant(rapid_ctx* ctx, const rapid_attn_shape* shape, const rapid_quant_layout* layout,
@@ -446,7 +448,8 @@ int rapid_verify_attn_quant(rapid_ctx* ctx, const rapid_attn_shape* shape, const
  *                 of 8); NULL where prefix_table is given, or where max_prefix is 0
  *   prefix_table  int32 [prefix->max_pages] or NULL; with it the prefix lies in pages of k_cache / v_cache (page_size > 0), addressed like the sequences'
  *                 own (its strides above are not used), and ids are clamped in the same way
- *   k_cache, v_cache, ctx_lens, gammas, page_table, out, lse_out   as for rapid_verify_attn (chunk_tokens and ctx_sum_hint are not used)
+ *   k_cache, v_cache, ctx_lens, gammas, page_table, out, lse_out   as for rapid_verify_attn (chunk_tokens and ctx_sum_hint are not used); the
+ *                 bounds of batch * max_ctx and of the values as for rapid_verify_attn_quant, and max_prefix is at most 2^30
  *   workspace     >= rapid_verify_attn_prefix_workspace_bytes(), 256-byte aligned, any content
  */
 typedef struct rapid_prefix_layout {

@@ -13,7 +13,7 @@ typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 namespace {
 
 constexpr float kRescaleLog2 = 8.0f;   // the running maximum only moves when a tile exceeds it by this (log2 units)
-constexpr float kNoMaximum = -1e30f;   // a row that has met no score yet: finite, so that differences are numbers; every score exceeds it
+constexpr float kNoMaximum = -3e38f;   // a row that has met no score yet: finite, so that differences are no NaN; below every score that is
 constexpr int kPieceQuanta = 2;        // what a sequence costs a workgroup besides its tokens, in quanta
 
 template <int D_, bool QUANT_, int TB_>

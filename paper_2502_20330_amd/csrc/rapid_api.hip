@@ -239,6 +239,12 @@ int page_shift_of(const rapid_attn_shape* s)
     return s->page_size ? sh : -1;
 }
 
+// Positions, also of loads ahead of the last token, and shares of the batch's tokens, cut by at least 32, are counted in 32 bits.
+int check_tokens(int64_t batch, int64_t max_tokens)
+{
+    return max_tokens <= 1 << 30 && batch * (max_tokens / 32 + 4) < (int64_t)1 << 31 ? RAPID_OK : RAPID_EUNSUPPORTED;
+}
+
 // Shapes of the calls on a cache in 8 bits; strides are bytes.  `attn`: the packed rows of an attention call.
 int check_quant_shape(const rapid_attn_shape* s, bool attn)
 {
@@ -262,8 +268,8 @@ int check_quant_shape(const rapid_attn_shape* s, bool attn)
     if (s->kv_token_stride < s->head_dim || s->kv_token_stride % 16 || s->kv_head_stride % 16) return RAPID_EALIGN;
     // rows of one (sequence or page, head) are addressed with 32-bit byte offsets
     const int64_t span_tokens = s->page_size ? s->page_size : s->max_ctx;
-    if (s->kv_token_stride * span_tokens >= (int64_t)1 << 32) return RAPID_EUNSUPPORTED;
-    return RAPID_OK;
+    if (s->kv_token_stride > (((int64_t)1 << 32) - 1) / span_tokens) return RAPID_EUNSUPPORTED;
+    return attn ? check_tokens(s->batch, s->max_ctx) : RAPID_OK;
 }
 int check_quant_layout(const rapid_attn_shape* s, const rapid_quant_layout* l)
 {
@@ -294,14 +300,15 @@ int check_prefix_shape(const rapid_attn_shape* s, const rapid_prefix_layout* p)
     const int rc = check_attn_shape(s);
     if (rc != RAPID_OK) return rc;
     if (!p || p->max_prefix < 0 || p->max_pages < 0) return RAPID_EINVAL;
-    return RAPID_OK;
+    return check_tokens(1, p->max_prefix) == RAPID_OK ? check_tokens(s->batch, s->max_ctx) : RAPID_EUNSUPPORTED;
 }
 // How the prefix lies: in pages of the sequences' pool, or by strides of its own.
 int check_prefix_place(const rapid_attn_shape* s, const rapid_prefix_layout* p, bool paged)
 {
     if (paged) return s->page_size != 0 && (int64_t)p->max_pages * s->page_size >= p->max_prefix ? RAPID_OK : RAPID_EINVAL;
+    if (p->max_prefix == 0) return RAPID_OK;              // there is none
     if (p->token_stride < s->head_dim || p->token_stride % 8 || p->head_stride % 8) return RAPID_EALIGN;
-    return p->token_stride * 2 * p->max_prefix < (int64_t)1 << 32 ? RAPID_OK : RAPID_EUNSUPPORTED;
+    return p->token_stride <= (((int64_t)1 << 31) - 1) / p->max_prefix ? RAPID_OK : RAPID_EUNSUPPORTED;
 }
 
 // A call's shape for the kernels that divide the batch's tokens by themselves.

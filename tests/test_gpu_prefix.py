@@ -139,6 +139,60 @@ def test_what_is_not_finite_reaches_who_attends_it_and_nobody_else(bad, d):
     assert not torch.isfinite(out[:, :, :2, 9]).any()
 
 
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+@pytest.mark.parametrize("prefix", [1, 31, 70, 333])
+@pytest.mark.parametrize("B,Q", [(2, 5), (9, 12), (5, 7)])
+def test_what_is_not_finite_at_the_end_of_the_prefix(bad, prefix, B, Q):
+    """Its last token, in the tile that goes on behind the end: every row attends it."""
+    rng = np.random.default_rng(prefix + B)
+    for n in "vk":
+        batch = Batch(rng, prefix, [Q + b for b in range(B)], 1, 128, prefix_cap=prefix + 40)
+        batch.shared[n][-1, 0, 9] = bad
+        batch.store()
+        out = batch.check(rng, [Q - 1] * B, Q, 8)
+        assert not torch.isfinite(out if n == "k" and bad != bad else out[..., 9]).any() or (n == "k" and bad == bad)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("B,Q,hq,hkv", [(9, 12, 8, 1), (30, 3, 8, 2), (20, 2, 16, 4), (40, 2, 4, 1)])
+def test_many_rows_of_a_ragged_batch(d, B, Q, hq, hkv):
+    """More rows than the streaming kernel takes, sequences without tokens or rows among them, paged; then with no prefix at all under the same bound."""
+    rng = np.random.default_rng(B + d)
+    lens = [int(x) for x in rng.integers(0, 40, B)]
+    lens[1], gammas = 0, [int(x) for x in rng.integers(0, Q, B)]
+    Batch(rng, 523, lens, hkv, d, 16, cap=64, prefix_cap=700).check(rng, gammas, Q, hq, "head")
+    Batch(rng, 0, lens, hkv, d, 16, cap=64, prefix_cap=700).check(rng, gammas, Q, hq, "head")
+
+
+def test_an_empty_prefix_array_is_no_prefix():
+    rng = np.random.default_rng(18)
+    lens, gammas = [300, 0, 7], [2, 0, 1]
+    batch = Batch(rng, 0, lens, 2, 64)
+    q = qu.bf16(rng, (3, 3, 4, 64))
+    (k, v, n, length), _ = batch.args("token")
+    empty = torch.empty((0, 2, 64), dtype=torch.bfloat16, device="cuda")
+    lse = torch.empty((3, 4, 3), device="cuda")
+    out = rapid().rapid_verify_attn_prefix(q.cuda(), k, v, n, length, k_prefix=empty, v_prefix=empty, gammas=i32(gammas), lse_out=lse)
+    batch.compare(q, out, lse, gammas)
+
+
+@pytest.mark.parametrize("B", [2, 40])
+def test_scores_far_below_zero(B):
+    """All of a row's scores are the same number near -1e32: its weights are equal."""
+    rng = np.random.default_rng(19)
+    d, P, n = 64, 200, 20
+    batch = Batch(rng, P, [n] * B, 1, d)
+    for x in [batch.shared["k"], *batch.own["k"]]:
+        x.fill_(-2.0 ** 50)
+    batch.store()
+    args, kw = batch.args("token")
+    out = rapid().rapid_verify_attn_prefix(torch.full((B, 1, 4, d), 2.0 ** 54, dtype=torch.bfloat16, device="cuda"), *args, **kw)
+    for b in (0, B - 1):
+        v = torch.cat([batch.shared["v"], batch.own["v"][b]])[:, 0].double().numpy()
+        tol = 2 * (P + n) * 2.0 ** -24 * np.abs(v).mean(0) + 2.0 ** -8 * np.abs(v.mean(0))     # weights of 1; sums, and the rounding of the result
+        qu.close(out[b, 0, 2], v.mean(0), tol)
+
+
 def test_the_prefix_is_as_if_each_sequence_held_it():
     """The same tokens as one sequence each through rapid_verify_attn: results of the two agree to their roundings."""
     rng = np.random.default_rng(13)

@@ -307,6 +307,109 @@ def test_captured_and_replayed_with_eager_calls_between():
         assert all(torch.equal(a.view(torch.uint8), b.view(torch.uint8)) for a, b in zip(state[:4], check[:4]))
 
 
+@pytest.mark.parametrize("d,page", [(64, 0), (64, 16), (128, 0), (128, 64)])
+def test_rows_by_the_thousand(d, page):
+    """So many rows that a thread takes several: whole blocks of them and a rest, fewer rows than there is room for, fewer tokens than rows."""
+    rng = np.random.default_rng(70 + d + page)
+    hkv = 8
+    Q = (1 << 21) // (2 * hkv * 2 * (d // 8)) + 37
+    lens, gammas = [Q + 5, Q - 50], [Q - 60, Q - 1]
+    cache = qu.QuantCache(rng, [0, 0], hkv, d, page, cap=Q + 6)
+    new = {n: awkward_rows(rng, (2, Q, hkv, d)) for n in "kv"}
+    kc, vc, ks, vs, table = cache.dev()
+    more = dict(gammas=i32(gammas), page_table=table, max_ctx=Q + 6)
+    rapid().rapid_kv_append_quant(kc, vc, ks, vs, new["k"].cuda(), new["v"].cuda(), i32(lens), **more)
+    outs = rapid().rapid_kv_read_quant(kc, vc, ks, vs, i32(lens), Q, **more)
+    for n, c, s, out in (("k", kc, ks, outs[0]), ("v", vc, vs, outs[1])):
+        want = np.zeros((2, Q, hkv, d), np.float32)
+        for b, (length, g) in enumerate(zip(lens, gammas)):
+            i = np.arange(max(0, g + 1 - length), g + 1)
+            codes, scales = qu.quantise(new[n][b, i].double().numpy())
+            cache.put(n, b, length - g - 1 + i, codes, scales)
+            want[b, i] = qu.values(codes, scales)
+        assert np.array_equal(c.view(torch.uint8).cpu().numpy(), cache.codes[n])
+        assert np.array_equal(s.view(torch.uint8).cpu().numpy(), cache.scales[n])
+        assert np.array_equal(out.float().cpu().numpy(), want, equal_nan=True)
+
+
+@pytest.mark.parametrize("d,page,hq,Q", [(128, 0, 8, 1), (64, 16, 16, 5), (128, 16, 16, 14), (64, 0, 16, 20), (128, 0, 16, 24)])
+def test_batches_of_short_sequences(d, page, hq, Q):
+    """A workgroup for each sequence and kv head: lengths from none to the bound, fewer tokens than rows, rows that a sequence does not have."""
+    rng = np.random.default_rng(80 + Q + d)
+    lens = [0, 1, 3, 1000, 1024, 16, 0, 127, 128, 129, 31, 33] + [int(x) for x in rng.integers(0, 300, 20)]
+    gammas = [int(x) for x in rng.integers(0, Q, len(lens))]
+    cache = qu.QuantCache(rng, lens, 4, d, page, cap=1024)
+    r, t = cache.at(3, np.array([997]))
+    cache.codes["v"][r, t, 1, 2] = 0x7F                    # for the last rows alone, if there are so many
+    run_attention(cache, lens, gammas, Q, hq, "token")
+
+
+def test_tens_of_thousands_of_sequences():
+    rng = np.random.default_rng(90)
+    B, d = 32767, 64
+    r = rapid()
+    codes = [torch.zeros((B, 16, 1, d), dtype=torch.uint8, device="cuda") for _ in range(2)]
+    scales = [torch.zeros((B, 1, 16), dtype=torch.uint8, device="cuda") for _ in range(2)]
+    new = [qu.bf16(rng, (B, 2, 1, d)) for _ in range(2)]
+    n = torch.full((B,), 2, dtype=torch.int32, device="cuda")
+    r.rapid_kv_append_quant(*codes, *scales, *(x.cuda() for x in new), n)
+    back = r.rapid_kv_read_quant(*codes, *scales, n, 2)
+    vals = [qu.values(*qu.quantise(x.double().numpy())) for x in new]
+    for got, want in zip(back, vals):
+        assert np.array_equal(got.float().cpu().numpy(), want.astype(np.float32))
+    q = qu.bf16(rng, (B, 1, 1, d))
+    out = r.rapid_verify_attn_quant(q.cuda(), *codes, *scales, n)
+    some = [0, 1, 255, 256, 16383, 16384, 32766]
+    qu.check_attention(q[some], out[some], None, lambda b, h: (vals[0][some[b]][:, 0], vals[1][some[b]][:, 0], 0), [0] * 7, d ** -0.5, [2] * 7)
+
+
+@pytest.mark.parametrize("n", [100, 3000])
+def test_scores_far_below_zero(n):
+    """All of a row's scores are the same number near -1e32: its weights are equal."""
+    rng = np.random.default_rng(91)
+    d = 64
+    cache = qu.QuantCache(rng, [n], 1, d)
+    cache.put("k", 0, np.arange(n), *qu.quantise(np.full((n, 1, d), -2.0 ** 50)))
+    kc, vc, ks, vs, _ = cache.dev()
+    q = torch.full((1, 1, 4, d), 2.0 ** 54, dtype=torch.bfloat16, device="cuda")
+    out = rapid().rapid_verify_attn_quant(q, kc, vc, ks, vs, i32([n]))
+    v = cache.tokens("v", 0)[:, 0]
+    tol = n * 2.0 ** -24 * np.abs(v).mean(0) + 2.0 ** -8 * np.abs(v.mean(0))       # weights of 1; the sum, and the rounding of the result
+    qu.close(out[0, 0, 3], v.mean(0), tol)
+
+
+def test_two_graphs_of_one_object_in_turn():
+    """Both use the object's workspace; one after the other on a stream they do not disturb each other, nor eager calls between."""
+    from paper_2502_20330_amd import binding
+    rng = np.random.default_rng(92)
+    r, d = binding.Rapid(0), 128
+    calls, graphs, outs = [], [], []
+    for lens, Q in (([2000, 300], 4), ([5000], 9)):
+        cache = qu.QuantCache(rng, lens, 2, d)
+        args = (qu.bf16(rng, (len(lens), Q, 8, d)).cuda(), *cache.dev()[:4], i32(lens))
+        calls.append(args)
+        outs.append(torch.empty_like(args[0]))
+    want = [rapid().rapid_verify_attn_quant(*args) for args in calls]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        for args, out in zip(calls, outs):
+            r.rapid_verify_attn_quant(*args, out=out)
+    torch.cuda.current_stream().wait_stream(side)
+    for args, out in zip(calls, outs):
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            r.rapid_verify_attn_quant(*args, out=out)
+    for turn in range(4):
+        for out in outs:
+            out.zero_()
+        for g in graphs if turn % 2 else graphs[::-1]:
+            g.replay()
+            eager = r.rapid_verify_attn_quant(*calls[turn % 2])
+        torch.cuda.synchronize()
+        assert torch.equal(outs[0], want[0]) and torch.equal(outs[1], want[1]) and torch.equal(eager, want[turn % 2])
+
+
 def test_on_another_stream():
     rng = np.random.default_rng(51)
     cache = qu.QuantCache(rng, [3000], 2, 128)

@@ -115,6 +115,23 @@ def test_what_the_prefix_call_refuses():
     assert binding.load_library().rapid_verify_attn_prefix_workspace_bytes(None, shape(head_dim=32), lay(1, 0, 256, 128)) == 0
 
 
+def test_bounds_of_the_positions():
+    lib, lay = binding.load_library(), binding.PrefixLayout
+    wide = dict(PAGED, max_pages=1 << 27)
+    for kw in (dict(wide, max_ctx=(1 << 30) + 1), dict(wide, max_ctx=1 << 30, batch=64), dict(kv_token_stride=1 << 62)):
+        assert quant_call("attn", shape(**kw)) == EUNSUPPORTED
+    assert quant_call("attn", shape(**dict(wide, max_ctx=1 << 30)), ws=None) == EWORKSPACE
+    assert quant_call("append", shape(kv_token_stride=1 << 62)) == EUNSUPPORTED
+    for kw in (dict(wide, max_ctx=(1 << 30) + 1), dict(wide, max_ctx=1 << 30, batch=64)):
+        assert prefix_call(shape(**kw)) == EUNSUPPORTED
+    assert prefix_call(shape(**PAGED), lay((1 << 30) + 1, 1 << 27, 0, 0), kp=None, vp=None, pt=P) == EUNSUPPORTED
+    assert prefix_call(shape(), lay(500, 0, 1 << 62, 128)) == EUNSUPPORTED
+
+
+def test_no_prefix_needs_no_layout():
+    assert prefix_call(shape(), binding.PrefixLayout(0, 0, 0, 0), kp=None, vp=None, ws=None) == EWORKSPACE
+
+
 def test_the_format_of_the_tests_is_torch_s_e4m3():
     codes = np.arange(256, dtype=np.uint8)
     want = torch.from_numpy(codes).view(torch.float8_e4m3fn).double().numpy()
