@@ -219,7 +219,7 @@ __device__ __forceinline__ void prefix_piece(const StreamLaunch& a, char* smem, 
     __syncthreads();                                     // all rings are dead from here on
     if (*taken_word != 0) {
         const int it = max(0, (max(first_masked_t0 - c0, 0) + G::TT - 1) / G::TT - first);
-        add_not_finite<G, RB, PAGED>(st, addr, tile_t0(it), min(c1, tile_t0(nt)), lim, lane);
+        add_not_finite<G, RB, PAGED>(st, addr, tile_t0(it), min(c1, tile_t0(nt)), G::TT, lim, lane);
     }
 #pragma unroll
     for (int rb = 0; rb < RB; ++rb) st.l[rb] = sum_over_groups(st.l[rb]);

@@ -62,7 +62,7 @@ struct Piece {
     int* taken;                                   // teams: the stream's word for take_not_finite
     uint32_t kring_lds, vring_lds, sring_lds;
     int b, h;
-    int L, Q, R, c0, c1, first, nt, last_tok;     // first, nt: this stream's tiles (tokens c0 + (first + i) TT ..)
+    int L, Q, R, c0, c1, nt, last_tok;            // nt: this stream's tiles (tokens c0 + (part + it NP) TT ..)
     int lane, wave, part, team;
 };
 
@@ -72,7 +72,7 @@ __device__ __forceinline__ void run_piece(const StreamLaunch& a, const Piece& w,
 {
     constexpr int MLS = (G::TEAMS && G::RB1 > G::RB0 ? G::RB1 : G::RB0) * 16;
     const int lane = w.lane, ln = lane & 15, lg = lane >> 4;
-    auto tile_t0 = [&](int it) { return w.c0 + (w.first + it) * G::TT; };
+    auto tile_t0 = [&](int it) { return w.c0 + (w.part + it * G::NP) * G::TT; };
 
     bf16x8 qf[RB][G::KS];
     int lim[RB];                                         // last token that a row attends in this piece
@@ -181,7 +181,7 @@ __device__ __forceinline__ void run_piece(const StreamLaunch& a, const Piece& w,
             pages.find(w.addr, t_next, w.last_tok);
             wait_loads<BEHIND>();                               // own half of K(it)
             __syncthreads();                                    // A
-            load_tile<G, PAGED, true, H>(w.addr, vpages, w.vring_lds + before * G::SLOT, t_next - G::TT, w.last_tok, lane, w.team * H);
+            load_tile<G, PAGED, true, H>(w.addr, vpages, w.vring_lds + before * G::SLOT, t_next - G::QUANTUM, w.last_tok, lane, w.team * H);
             score_tile<G, RB>(s, qf, kt, lane);
             softmax_tile<G, RB>(st, s, pb, no_scales, t0, t0 >= first_masked_t0, lim, w.c1, c, lane);
 
@@ -202,8 +202,8 @@ __device__ __forceinline__ void run_piece(const StreamLaunch& a, const Piece& w,
         taken = *w.taken != 0;
     }
     if (taken) {
-        const int it = max(0, (max(first_masked_t0 - w.c0, 0) + G::TT - 1) / G::TT - w.first);
-        add_not_finite<G, RB, PAGED>(st, w.addr, tile_t0(it), min(w.c1, tile_t0(w.nt)), lim, lane);
+        const int it = (max(first_masked_t0 - tile_t0(0), 0) + G::QUANTUM - 1) / G::QUANTUM;
+        add_not_finite<G, RB, PAGED>(st, w.addr, tile_t0(it), w.c1, G::QUANTUM, lim, lane);
     }
 #pragma unroll
     for (int rb = 0; rb < RB; ++rb) st.l[rb] = sum_over_groups(st.l[rb]);
@@ -288,11 +288,11 @@ __device__ __forceinline__ void stream_piece(const StreamLaunch& a, char* smem, 
     w.c0 = c0;
     w.c1 = c1;
     const int ntile = (c1 - c0 + G::TT - 1) / G::TT;
-    const int each = (ntile + G::NP - 1) / G::NP;        // tiles of a stream; contiguous
-    w.first = w.part * each;
-    // teams meet at barriers, so there every stream runs as many tiles; those past its end are masked
-    w.nt = G::TEAMS ? each : max(0, min(each, ntile - w.first));
-    w.last_tok = min(c1, c0 + (w.first + each) * G::TT) - 1;
+    // The streams take the tiles in turn, so that what a workgroup reads at a time lies together.  (A contiguous range for each, beginning powers of two
+    // apart: 128K tokens at 4 rows 48.4 us instead of 46.2, at 36 rows 61 instead of 59, at 72 rows 75 instead of 72.5.)
+    // Teams meet at barriers, so there every stream runs as many tiles; those past the end are masked.
+    w.nt = (ntile + G::NP - 1 - (G::TEAMS ? 0 : w.part)) / G::NP;
+    w.last_tok = c1 - 1;
     w.addr = make_row_addr<G, PAGED>(a.own, b, h);
     const int ring = w.part * G::RING;
     const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)smem;
@@ -317,7 +317,7 @@ __device__ __forceinline__ void stream_piece(const StreamLaunch& a, char* smem, 
             dma16_keep(reinterpret_cast<const char*>(a.q), off, lds + G::NP * G::RING + e * 1024);
         }
     }
-    auto tile_t0 = [&](int it) { return c0 + (w.first + it) * G::TT; };
+    auto tile_t0 = [&](int it) { return c0 + (w.part + it * G::NP) * G::TT; };
     TilePages<G, PAGED> pages;
     constexpr int H = G::TEAMS ? G::NLD / 2 : G::NLD;
     const int e0 = G::TEAMS ? w.team * H : 0;

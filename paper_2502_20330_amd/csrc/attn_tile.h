@@ -471,11 +471,11 @@ __device__ __forceinline__ bool take_not_finite(char* vt, int lane)
     return __any(any);
 }
 template <class G, int RB, bool PAGED>
-__device__ __forceinline__ void add_not_finite(WaveState<G, RB>& st, const RowAddr& ra, int begin, int end, const int (&lim)[RB], int lane)
-{
+__device__ __forceinline__ void add_not_finite(WaveState<G, RB>& st, const RowAddr& ra, int begin, int end, int step, const int (&lim)[RB], int lane)
+{                                                        // tiles of a stream, `step` tokens apart, from token `begin` on
     const int lg = opaque(lane) >> 4;
 #pragma unroll 1
-    for (int t = begin; t < end; ++t) {
+    for (int t = begin, left = G::TT; t < end; ++t) {
         const char* row = ra.v;
         if (PAGED) row += (int64_t)min(max(ra.pages[t >> ra.page_shift], 0), ra.page_hi) * ra.page_bytes;
         row += (uint32_t)(PAGED ? t & ra.page_mask : t) * ra.tok_bytes;
@@ -499,6 +499,10 @@ __device__ __forceinline__ void add_not_finite(WaveState<G, RB>& st, const RowAd
 #pragma unroll
                 for (int rb = 0; rb < RB; ++rb)
                     if (bits[i] && t <= lim[rb]) st.acc[db][rb][i] += __uint_as_float(bits[i]);
+        }
+        if (--left == 0) {
+            left = G::TT;
+            t += step - G::TT;
         }
     }
 }
