@@ -398,11 +398,12 @@ struct Partials {
     int64_t slot = 0;
 };
 // Those of packed row `row` of sequence b, head h.
-__device__ __forceinline__ Partials find_partials(const StreamLaunch& a, int b, int h, int row, int lane)
-{
+__device__ __forceinline__ Partials find_partials(const StreamLaunch& a, int b, int h, int row, int lane, int len)
+{                                                        // len: of sequence `lane`, 0 where there is none
     int before = 0, total = 0, cost = 0;
     for (int b0 = 0; b0 < a.B; b0 += 64) {
-        const int mine = b0 + lane < a.B ? seq_cost(seq_len(a, b0 + lane), b0 + lane, a.quantum) : 0;
+        if (b0) len = b0 + lane < a.B ? seq_len(a, b0 + lane) : 0;
+        const int mine = seq_cost(len, b0 + lane, a.quantum);
         const int end = total + scan_costs(mine);
         if (b >= b0 && b < b0 + 64) {
             cost = __builtin_amdgcn_readlane(mine, b - b0);
@@ -461,16 +462,10 @@ __device__ __forceinline__ void fold_partials(const StreamLaunch& a, int64_t slo
         x.fold(n - s0, d, r, num);
     }
 }
-// Those of a single sequence (b = 0), whose first share is share 0 whatever its length: the first block is asked for before the length is known.
-template <int D>
-__device__ __forceinline__ void fold_single(const StreamLaunch& a, int h, int row, int d, RowMerge& r, float& num, bool wanted = true)
+// Where a single sequence's begin (b = 0), whose first share is share 0 whatever its length.
+__device__ __forceinline__ int64_t first_slot(const StreamLaunch& a, int h, int row)
 {
-    const int64_t slot = (int64_t)(h * a.tiles + row / a.RP) * a.nslots * a.RP + row % a.RP;
-    PartialBlock x;
-    x.load<D>(a, slot, a.nslots, d);
-    const int n = wanted ? find_partials(a, 0, h, row, d & 63).n : 0;
-    x.fold(n, d, r, num);
-    fold_partials<D>(a, slot + (int64_t)kMergeBlock * a.RP, n - kMergeBlock, d, r, num);
+    return (int64_t)(h * a.tiles + row / a.RP) * a.nslots * a.RP + row % a.RP;
 }
 
 // One workgroup of D threads per (sequence, kv head, packed row): out = sum 2^(m_s - M) O_s / sum 2^(m_s - M) l_s, over the row's partials of the
@@ -486,15 +481,33 @@ __global__ void __launch_bounds__(D) attn_stream_merge(StreamLaunch a, StreamLau
         if (a.lse_out && d == 0) a.lse_out[lse_index(a, b, h, row)] = 0.f;
         return;
     }
+    // All that can be asked for is asked for at once: the lengths, the first block of a single sequence (the prefix is one) before its length is known, the
+    // other's as soon as the lengths are there.
+    const int lane = d & 63;
+    const int len = lane < a.B ? seq_len(a, lane) : 0, prefix_len = PREFIX && lane == 0 ? seq_len(prefix, 0) : 0;
+    const bool there = seq_len(a, b) > 0;                 // (a sequence without tokens has no rows, behind a prefix either)
+    const int prefix_row = b * a.Qmax * a.G + row;
+    PartialBlock x, y;
+    const int64_t x_slot = PREFIX ? first_slot(prefix, h, prefix_row) : 0;
+    if (PREFIX) x.load<D>(prefix, x_slot, prefix.nslots, d);
+    Partials own;
+    if (a.B == 1) {
+        own.slot = first_slot(a, h, row);
+        y.load<D>(a, own.slot, a.nslots, d);
+        own.n = find_partials(a, 0, h, row, lane, len).n;
+    } else {
+        own = find_partials(a, b, h, row, lane, len);
+        y.load<D>(a, own.slot, own.n, d);
+    }
     RowMerge r;
     float num = 0.f;
-    if (PREFIX) fold_single<D>(prefix, h, b * a.Qmax * a.G + row, d, r, num, seq_len(a, b) > 0);     // (a sequence without tokens has no rows)
-    if (a.B == 1) {
-        fold_single<D>(a, h, row, d, r, num);
-    } else {
-        const Partials own = find_partials(a, b, h, row, d & 63);
-        fold_partials<D>(a, own.slot, own.n, d, r, num);
+    if (PREFIX) {
+        const int n = there ? find_partials(prefix, 0, h, prefix_row, lane, prefix_len).n : 0;
+        x.fold(n, d, r, num);
+        fold_partials<D>(prefix, x_slot + (int64_t)kMergeBlock * prefix.RP, n - kMergeBlock, d, r, num);
     }
+    y.fold(own.n, d, r, num);
+    fold_partials<D>(a, own.slot + (int64_t)kMergeBlock * a.RP, own.n - kMergeBlock, d, r, num);
     const __bf16 o = (__bf16)(r.den == 0.f ? 0.f : num / r.den);
     *dst = __builtin_bit_cast(uint16_t, o);
     if (a.lse_out && d == 0) a.lse_out[lse_index(a, b, h, row)] = (r.M + log2f(r.den)) * 0.6931471805599453f;
