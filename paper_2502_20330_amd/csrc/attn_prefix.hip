@@ -8,6 +8,8 @@
 //    and the slots of the ones before are free.
 //  * Rows beyond that go to other workgroups, which read the same tokens at about the same time on the same die (blockIdx modulo 8), so that its L2
 //    serves all but one of them.
+// Measured (8 kv heads of 128): 131000 tokens, 320 rows 183 to 198 us (550 to 600 TFLOP/s), 32K tokens, 288 rows 57.  A tile of 384 rows takes 2735 cycles, 1536 of
+// them matrix instructions, at 1.96 GHz, where the power limit holds the clock; the exponentials and conversions run beside them in part only.
 #include "attn_tile.h"
 
 namespace {
