@@ -199,8 +199,8 @@ class Rapid:
         self._ws_exchange: Optional[torch.Tensor] = None
         self._ws_args = (None, 0, None, 0)             # address and size of the exchange memory and of the workspace, as a call takes them
         self._ws_accept: Optional[torch.Tensor] = None
-        self._ws_shared: list = []                     # workspaces of the quantised and the prefix attention, the last one in use
-        self._ws_shared_args = (None, 0)               # address and size of that one
+        self._ws_streams: dict = {}                    # address and size of the quantised and the prefix attention's workspace, by stream
+        self._ws_kept: list = []                       # those, and the ones they have outgrown
         self._plans: dict = {}                         # shapes and layouts of calls by their sizes (_planned)
         self._sink: Optional[torch.Tensor] = None
 
@@ -478,11 +478,15 @@ class Rapid:
         shape = AttnShape(batch, q_max, hq, hkv, d, ctx_max, gamma, scale, 0, st[1], st[2], st[0], tokens, page_table.shape[1], 0, rows, 0)
         return ctypes.byref(shape), ctypes.byref(QuantLayout(0, ss[1], ss[0]))
 
-    def _shared_workspace(self, nbytes: int):
-        # grows only, and what it has outgrown is kept: a captured graph goes on using the one that it was recorded with
-        ws = torch.empty(max(nbytes, 2 * self._ws_shared_args[1], 256), dtype=torch.uint8, device=self.device)
-        self._ws_shared.append(ws)
-        self._ws_shared_args = (ws.data_ptr(), ws.numel())
+    _NO_WORKSPACE = (None, 0)
+
+    def _stream_workspace(self, stream: int, nbytes: int):
+        # one for each stream, so that calls on two may overlap.  It grows only, and what it has outgrown is kept: a captured graph goes on using the
+        # one that it was recorded with
+        ws = torch.empty(max(nbytes, 2 * self._ws_streams.get(stream, self._NO_WORKSPACE)[1], 256), dtype=torch.uint8, device=self.device)
+        self._ws_kept.append(ws)
+        self._ws_streams[stream] = (ws.data_ptr(), ws.numel())
+        return self._ws_streams[stream]
 
     def rapid_kv_append_quant(self, k_codes, v_codes, k_scales, v_scales, k_new, v_new, ctx_lens, gamma: Optional[int] = None, *,
                               gammas=None, page_table=None, max_ctx: Optional[int] = None):
@@ -536,7 +540,8 @@ class Rapid:
                                 page_table=None, max_ctx: Optional[int] = None, softmax_scale: Optional[float] = None,
                                 out=None, lse_out=None):
         """:meth:`rapid_verify_attn` on a cache in 8 bits (layout: :meth:`rapid_kv_append_quant`): q bf16 [B,Qmax,Hq,d]; returns
-        out bf16 [B,Qmax,Hq,d] and fills lse_out fp32 [B,Hq,Qmax] if given.  One position (Qmax = 1) is a decode step."""
+        out bf16 [B,Qmax,Hq,d] and fills lse_out fp32 [B,Hq,Qmax] if given.  One position (Qmax = 1) is a decode step.
+        Calls on different streams may overlap; graphs captured on one stream use one workspace and may not."""
         if out is None:
             out = torch.empty_like(q)
 
@@ -547,10 +552,10 @@ class Rapid:
         args = (self._ctx, shape, layout, q.data_ptr(), k_codes.data_ptr(), v_codes.data_ptr(), k_scales.data_ptr(),
                 v_scales.data_ptr(), ctx_lens.data_ptr(), _dptr(gammas), _dptr(page_table), out.data_ptr(), _dptr(lse_out))
         call, stream = self.lib.rapid_verify_attn_quant, _stream_ptr(self.device)
-        rc = call(*args, *self._ws_shared_args, stream)
+        rc = call(*args, *self._ws_streams.get(stream, self._NO_WORKSPACE), stream)
         if rc == RAPID_EWORKSPACE:                             # the last check of the call: nothing has been launched
-            self._shared_workspace(self.lib.rapid_verify_attn_quant_workspace_bytes(self._ctx, shape))
-            rc = call(*args, *self._ws_shared_args, stream)
+            need = self.lib.rapid_verify_attn_quant_workspace_bytes(self._ctx, shape)
+            rc = call(*args, *self._stream_workspace(stream, need), stream)
         if rc:
             _check(self.lib, rc, self._ctx)
         return out
@@ -567,7 +572,8 @@ class Rapid:
         """:meth:`rapid_verify_attn` for a batch whose sequences follow one shared prefix, which is read once.  prefix_len int32
         [1] (device); the prefix is k_prefix/v_prefix bf16 [P,Hkv,d] (any token/head strides) or, with page_table, pages of
         k_cache/v_cache that prefix_table int32 [max_pages] names; max_prefix bounds prefix_len on the host (default: what is
-        given).  ctx_lens counts a sequence's own tokens, which k_cache/v_cache hold as for rapid_verify_attn."""
+        given).  ctx_lens counts a sequence's own tokens, which k_cache/v_cache hold as for rapid_verify_attn.  Streams
+        and graphs as for :meth:`rapid_verify_attn_quant`."""
         if out is None:
             out = torch.empty_like(q)
         key = ("prefix", gamma, max_prefix, max_ctx, softmax_scale,
@@ -579,10 +585,10 @@ class Rapid:
                 k_cache.data_ptr(), v_cache.data_ptr(), ctx_lens.data_ptr(), _dptr(gammas), _dptr(page_table), out.data_ptr(),
                 _dptr(lse_out))
         call, stream = self.lib.rapid_verify_attn_prefix, _stream_ptr(self.device)
-        rc = call(*args, *self._ws_shared_args, stream)
+        rc = call(*args, *self._ws_streams.get(stream, self._NO_WORKSPACE), stream)
         if rc == RAPID_EWORKSPACE:                             # the last check of the call: nothing has been launched
-            self._shared_workspace(self.lib.rapid_verify_attn_prefix_workspace_bytes(self._ctx, shape, prefix))
-            rc = call(*args, *self._ws_shared_args, stream)
+            need = self.lib.rapid_verify_attn_prefix_workspace_bytes(self._ctx, shape, prefix)
+            rc = call(*args, *self._stream_workspace(stream, need), stream)
         if rc:
             _check(self.lib, rc, self._ctx)
         return out

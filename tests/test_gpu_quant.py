@@ -425,6 +425,25 @@ def test_on_another_stream():
     assert all(torch.equal(rapid().rapid_verify_attn_quant(q, *dev[:4], i32([3000])), want) for _ in range(3))   # the same bits every time
 
 
+def test_calls_on_two_streams_at_once():
+    """Of one object, without waiting for one another."""
+    rng = np.random.default_rng(52)
+    streams, calls = [torch.cuda.Stream() for _ in range(2)], []
+    for lens, Q in (([20000], 9), ([3000, 900], 4)):
+        cache = qu.QuantCache(rng, lens, 2, 128)
+        calls.append((qu.bf16(rng, (len(lens), Q, 8, 128)).cuda(), *cache.dev()[:4], i32(lens)))
+    want = [rapid().rapid_verify_attn_quant(*c) for c in calls]
+    torch.cuda.synchronize()
+    got = [[], []]
+    for _ in range(20):
+        for i in range(2):
+            with torch.cuda.stream(streams[i]):
+                got[i].append(rapid().rapid_verify_attn_quant(*calls[i]))
+    torch.cuda.synchronize()
+    for i in range(2):
+        assert all(torch.equal(x, want[i]) for x in got[i])
+
+
 def test_refusals_of_the_binding():
     from paper_2502_20330_amd import binding
     rng = np.random.default_rng(61)
