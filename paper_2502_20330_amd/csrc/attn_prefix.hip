@@ -2,7 +2,7 @@
 //
 // All rows of the batch, R = B (gamma_max + 1) G per kv head, attend the same P tokens, without a mask: the prefix is one "sequence"
 // with R rows.  Reading it costs 4 d bytes per token and kv head, computing 4 R d multiply-adds and R exponentials, so that from about a hundred rows on the
-// matrix cores and the exponentials bound it and no longer the memory.  Up to 96 rows the streaming kernel (attn_stream.hip) does it; this one takes more:
+// matrix cores and the exponentials bound it and no longer the memory.  Up to 96 rows, and where all of it is little work, the streaming kernel (attn_stream.hip) does it; this one takes more:
 //  * A workgroup has eight waves, T of which share a stream of token tiles (8 / T streams) and hold one to three blocks of 16 rows each, 128 to 384 rows
 //    together.  Tiles go HBM -> LDS once a workgroup; S of them lie in a ring, and the waves meet every S / 4 tiles: then the next ones have landed
 //    and the slots of the ones before are free.
@@ -374,8 +374,11 @@ void plan_attn_prefix(StreamLaunch& a, int n_cu)
     });
     const int64_t units = (int64_t)a.Hkv * a.tiles;
     a.groups = n_cu > units ? (int)(n_cu / units) : 1;
-    const int64_t most = ((int64_t)a.max_ctx + a.quantum - 1) / a.quantum + kPieceQuanta;
+    const int64_t most = ((int64_t)a.max_ctx + a.quantum - 1) / a.quantum;
     if (a.groups > most) a.groups = (int)most;
+    // A share more divides the tiles further, and is one more partial of every row to write and read: the sum of the two is least where
+    // groups^2 is about 2 max_ctx / units (4 kv heads, 266 rows, 2000 tokens: 64 shares 35 us, 31 of them 31; more tokens want them all).
+    while (a.groups > 1 && (int64_t)a.groups * a.groups * units > (int64_t)2 * a.max_ctx) --a.groups;
     a.nslots = a.groups;
     a.rot = 0;
 }

@@ -23,7 +23,7 @@ struct StreamLaunch {
     float* part_ml;             // [Hkv][tiles][nslots][RP][2] (maximum in log2 units, sum)
     int32_t B, Qmax, Hq, Hkv, G, D, gamma, max_ctx;
     int32_t shared;             // 1: a shared prefix: one sequence (ctx_lens: its length) with the rows of the batch, which all attend all of it
-    int32_t RP, tiles;          // packed rows of a slot (a multiple of 16), row tiles (1 but for attn_prefix)
+    int32_t RP, tiles;          // packed rows of a slot (a multiple of 16), row tiles (1 but for a prefix)
     int32_t groups, nslots;     // shares of a kv head, groups + B - 1
     int32_t quantum;            // tokens that shares are cut by
     int32_t rot;                // 1: share g of slot x serves head (x + g) mod Hkv, 0: head x
@@ -34,7 +34,7 @@ constexpr int kStreamRows = 96;      // packed rows that the streaming kernel ta
 // Fill the plan (RP .. direct) from the shape and the source's layout.
 void plan_attn_stream(StreamLaunch& a, int n_cu);
 void plan_attn_prefix(StreamLaunch& a, int n_cu);
-// Both for one launch: the tokens of a shared prefix (at most kStreamRows rows) and the sequences' own.
+// Both for one launch: the tokens of a shared prefix, its rows in tiles of at most kStreamRows, and the sequences' own.
 void plan_attn_stream_pair(StreamLaunch& own, StreamLaunch& prefix, int n_cu);
 size_t attn_stream_workspace_bytes(const StreamLaunch& a);                       // of any plan
 void bind_attn_stream(StreamLaunch& a, void* workspace);
@@ -43,6 +43,6 @@ hipError_t configure_attn_prefix();
 // Write the partials (direct: the result).
 hipError_t launch_attn_stream(const StreamLaunch& a, hipStream_t stream);
 hipError_t launch_attn_stream_pair(const StreamLaunch& own, const StreamLaunch& prefix, hipStream_t stream);
-hipError_t launch_attn_prefix(const StreamLaunch& a, hipStream_t stream);        // a shared prefix with more than kStreamRows rows
+hipError_t launch_attn_prefix(const StreamLaunch& a, hipStream_t stream);
 // Joins the partials of `own`, and of a shared prefix where `prefix` has any (prefix.part_o not null).
 hipError_t launch_attn_stream_merge(const StreamLaunch& own, const StreamLaunch& prefix, hipStream_t stream);

@@ -275,8 +275,8 @@ __device__ __forceinline__ void run_piece(const StreamLaunch& a, const Piece& w,
 }
 
 template <class G, bool PAGED>
-__device__ __forceinline__ void stream_piece(const StreamLaunch& a, char* smem, int b, int h, int L, int c0, int c1, int64_t pbase)
-{
+__device__ __forceinline__ void stream_piece(const StreamLaunch& a, char* smem, int b, int h, int L, int c0, int c1, int64_t pbase, int r0)
+{                                                        // r0: the first of the packed rows (of a shared prefix, there may be more than RP)
     Piece w;
     const int tid = opaque(threadIdx.x);
     w.lane = tid & 63;
@@ -287,7 +287,7 @@ __device__ __forceinline__ void stream_piece(const StreamLaunch& a, char* smem, 
     w.h = h;
     w.L = L;
     w.Q = seq_queries(a, b);
-    w.R = w.Q * a.G;
+    w.R = min(w.Q * a.G - r0, G::RP);
     w.c0 = c0;
     w.c1 = c1;
     const int ntile = (c1 - c0 + G::TT - 1) / G::TT;
@@ -314,7 +314,7 @@ __device__ __forceinline__ void stream_piece(const StreamLaunch& a, char* smem, 
         const int last_row = a.Qmax * a.G - 1;
         for (int e = w.wave; e < G::RP / G::QRPI; e += G::NW) {
             const int row = e * G::QRPI + w.lane / G::QCPR;
-            const int rr = min(row, last_row);
+            const int rr = min(r0 + row, last_row);
             const int ch = (w.lane % G::QCPR) ^ k_swz<G::QROWB>(row);
             const uint32_t off = (uint32_t)(((((int64_t)b * a.Qmax + rr / a.G) * a.Hq + h * a.G + rr % a.G) * G::D) * 2) + ch * 16;
             dma16_keep(reinterpret_cast<const char*>(a.q), off, lds + G::NP * G::RING + e * 1024);
@@ -365,17 +365,17 @@ __device__ __forceinline__ void write_missing_rows(const StreamLaunch& a, int b,
 
 // Grid: one workgroup per (kv head, share).  Partials: [kv head][g + b], which no two pieces of a head share.  Direct: per (kv head, sequence).
 template <class G, bool PAGED>
-__device__ __forceinline__ void stream_share(const StreamLaunch& a, char* smem, int g)
+__device__ __forceinline__ void stream_share(const StreamLaunch& a, char* smem, int g, int rt = 0)
 {
     const int h = __builtin_amdgcn_readfirstlane(a.rot ? (blockIdx.x + g) % a.Hkv : blockIdx.x);     // (base addresses go through scalar registers)
     if (a.direct) {
         const int L = __builtin_amdgcn_readfirstlane(seq_len(a, g));
         write_missing_rows<G>(a, g, h, L);
-        if (L > 0) stream_piece<G, PAGED>(a, smem, g, h, L, 0, L, 0);
+        if (L > 0) stream_piece<G, PAGED>(a, smem, g, h, L, 0, L, 0, 0);
         return;
     }
     for_each_piece(a, g, threadIdx.x & 63, G::QUANTUM, [&](int b, int L, int c0, int c1) {
-        stream_piece<G, PAGED>(a, smem, b, h, L, c0, c1, ((int64_t)h * a.nslots + g + b) * G::RP);
+        stream_piece<G, PAGED>(a, smem, b, h, L, c0, c1, ((int64_t)(h * a.tiles + rt) * a.nslots + g + b) * G::RP, rt * G::RP);
         wait_loads<0>();                                 // the partial's stores are out of the load account
     });
 }
@@ -390,9 +390,11 @@ template <class G, bool PAGED>
 __global__ void __launch_bounds__(G::NW * 64) attn_stream_pair(StreamLaunch own, StreamLaunch prefix)
 {
     extern __shared__ __attribute__((aligned(1024))) char smem[];
-    const bool first = (int)blockIdx.y < prefix.groups;
+    const int y = __builtin_amdgcn_readfirstlane(blockIdx.y), shares = prefix.groups * prefix.tiles;
+    const bool first = y < shares;
     const StreamLaunch a = first ? prefix : own;
-    stream_share<G, PAGED>(a, smem, first ? blockIdx.y : blockIdx.y - prefix.groups);
+    const int g = first ? y : y - shares;
+    stream_share<G, PAGED>(a, smem, g / a.tiles, g % a.tiles);
 }
 
 // The partials of one row: `n` of them, from row slot `slot` on, RP slots apart.
@@ -599,14 +601,20 @@ void plan_attn_stream(StreamLaunch& a, int n_cu)
     a.direct = a.max_ctx <= quanta * a.quantum;
 }
 
+// A sequence costs its own part about as much as 512 tokens, besides those that it has (19 short ones beside 2000 tokens of prefix, 4 kv heads: 19 us, 40 without).
+constexpr int kPieceTokens = 512;
+
 void plan_attn_stream_pair(StreamLaunch& own, StreamLaunch& prefix, int n_cu)
 {
-    const int rb = (prefix.Qmax * prefix.G + 15) / 16, each = n_cu / own.Hkv;
-    const int64_t tokens = (int64_t)own.B * own.max_ctx;
-    int mine = (int)(each * tokens / (tokens + prefix.max_ctx));       // of the compute units, by what there may be to read
+    const int rows = prefix.Qmax * prefix.G, own_rows = own.Qmax * own.G, each = n_cu / own.Hkv;
+    const int rb = rows <= kStreamRows ? (rows + 15) / 16 : own_rows <= 48 ? 3 : (own_rows + 15) / 16;
+    const int tiles = (rows + rb * 16 - 1) / (rb * 16);
+    const int64_t tokens = (int64_t)own.B * (own.max_ctx + kPieceTokens);
+    int mine = (int)(each * tokens / (tokens + (int64_t)tiles * prefix.max_ctx));       // of the compute units, by what there may be to read
     if (mine < 1) mine = 1;
     plan_shares(own, rb, mine);
-    plan_shares(prefix, rb, each - own.groups);
+    plan_shares(prefix, rb, (each - own.groups) / tiles);
+    prefix.tiles = tiles;
 }
 
 size_t attn_stream_workspace_bytes(const StreamLaunch& a)
@@ -627,7 +635,7 @@ hipError_t launch_attn_stream(const StreamLaunch& a, hipStream_t stream)
 {
     return with_geo(a.D, a.own.ks != nullptr, a.RP / 16, [&](auto geo) {
         using G = decltype(geo);
-        const dim3 grid(a.Hkv, a.direct ? a.B : a.groups), block(G::NW * 64);
+        const dim3 grid(a.Hkv, a.direct ? a.B : a.groups * a.tiles), block(G::NW * 64);
         if constexpr (G::QUANT) {
             auto fn = a.own.page_table ? attn_stream<G, true> : attn_stream<G, false>;
             hipLaunchKernelGGL(fn, grid, block, G::LDS, stream, a);
@@ -649,7 +657,7 @@ hipError_t launch_attn_stream_pair(const StreamLaunch& own, const StreamLaunch& 
         using G = decltype(geo);
         if constexpr (!G::QUANT) {
             auto fn = own.own.page_table ? attn_stream_pair<G, true> : attn_stream_pair<G, false>;
-            hipLaunchKernelGGL(fn, dim3(own.Hkv, own.groups + prefix.groups), dim3(G::NW * 64), G::LDS, stream, own, prefix);
+            hipLaunchKernelGGL(fn, dim3(own.Hkv, own.groups + prefix.groups * prefix.tiles), dim3(G::NW * 64), G::LDS, stream, own, prefix);
             return hipGetLastError();
         }
         return hipErrorInvalidValue;

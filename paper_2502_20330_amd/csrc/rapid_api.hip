@@ -340,17 +340,22 @@ struct PrefixPlan {
     size_t own_bytes, bytes;    // of the workspace
     bool pair;                  // both in one launch
 };
+// One launch for both, whose prefix part takes the rows 48 to 96 at a time: up to kStreamRows rows, and beyond while there is so little of it, rows times
+// tokens of all kv heads a compute unit, that what each launch costs weighs more than a kernel that reads the prefix once for up to 384 rows.  (8 kv heads,
+// 288 rows, sequences of up to 1500 tokens: 2000 tokens 27.5 us instead of 45, 8000 37 instead of 53, 16000 57 and 61; 440 rows of 64, 4000 tokens 28 and 33,
+// 8000 tokens 42 and 38.5.)
+constexpr int64_t kPairWork = 96 << 10;
 PrefixPlan plan_prefix(const rapid_ctx* ctx, const rapid_attn_shape* s, int max_prefix, const AttnSource& own, const AttnSource& prefix)
 {
     PrefixPlan p{stream_shape(s, own), stream_shape(s, prefix), 0, 0, false};
-    const int n_cu = compute_units(ctx);
+    const int64_t n_cu = compute_units(ctx);
     p.prefix.shared = 1;
     p.prefix.B = 1;
     p.prefix.Qmax = s->batch * s->q_max;
     p.prefix.gamma = p.prefix.Qmax - 1;
     p.prefix.max_ctx = max_prefix;
-    const bool few = p.prefix.Qmax * p.prefix.G <= kStreamRows;
-    p.pair = max_prefix > 0 && few;
+    const int rows = p.prefix.Qmax * p.prefix.G;
+    p.pair = max_prefix > 0 && (rows <= kStreamRows || (rows < 1 << 20 && (int64_t)rows * max_prefix * s->n_kv_heads <= kPairWork * n_cu));
     if (p.pair) {
         plan_attn_stream_pair(p.own, p.prefix, n_cu);
     } else {

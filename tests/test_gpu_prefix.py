@@ -164,6 +164,27 @@ def test_many_rows_of_a_ragged_batch(d, B, Q, hq, hkv):
     Batch(rng, 0, lens, hkv, d, 16, cap=64, prefix_cap=700).check(rng, gammas, Q, hq, "head")
 
 
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("B,page", [(98, 0), (99, 16), (100, 0), (102, 16), (104, 64)])
+def test_thousands_of_rows(d, B, page):
+    """6272 to 6656 rows: tiles of 128, 192, 320, 384 and 256; sequences here and there are compared.  Then a token of the last tile is not finite."""
+    rng = np.random.default_rng(B + d)
+    Q, hq, some = 8, 8, [0, 1, 2, B // 2, B - 1]
+    lens, gammas = [int(x) for x in rng.integers(0, 40, B)], [int(x) for x in rng.integers(0, Q, B)]
+    lens[1], lens[2], gammas[2] = 0, 3, Q - 1
+    batch = Batch(rng, 4201, lens, 1, d, page, cap=48, prefix_cap=4230)
+    q, lse = qu.bf16(rng, (B, Q, hq, d)), torch.empty((B, hq, Q), device="cuda")
+    for bad in (None, float("nan"), float("inf")):
+        if bad is not None:
+            batch.shared["v"][-1, 0, 9] = bad
+            batch.store()
+        args, kw = batch.args("head")
+        out = rapid().rapid_verify_attn_prefix(q.cuda(), *args, gammas=i32(gammas), lse_out=lse, **kw)
+        whole = {n: [torch.cat([batch.shared[n], batch.own[n][b]]).double().numpy() for b in some] for n in "kv"}
+        qu.check_attention(q[some], out[some], lse[some], lambda b, h: (whole["k"][b][:, 0], whole["v"][b][:, 0], batch.P),
+                           [gammas[b] for b in some], d ** -0.5, [lens[b] for b in some])
+
+
 def test_an_empty_prefix_array_is_no_prefix():
     rng = np.random.default_rng(18)
     lens, gammas = [300, 0, 7], [2, 0, 1]
