@@ -15,8 +15,8 @@
 //    conversion: in the S^T = K Q^T form a lane holds one token's row.  A value's scale cannot (there a lane holds one column of eight
 //    tokens) and is multiplied into the token's weight instead, in 32 bits, before the weight's own rounding to bf16.
 //  * ds_read_b64_tr_b8 delivers V^T, eight tokens of one column, straight from LDS.
-// Measured, 8 kv heads of 128 and 128K tokens (271 MB, 39 us at the rate of a pure read): 4 rows 46 us, 36 rows 55 to 59, 72 rows 70 to 75; eight sequences
-// of 16K to 128K, 16-token pages, 36 rows (1291 MB, 186 us): 219.  Of the 55 us, 5 pass until the first tiles are there, 4.5 in the epilogue and 6.5
+// Measured, 8 kv heads of 128 and 128K tokens (271 MB, 39 us at the rate of a pure read): 4 rows 46 us, 36 rows 53 to 59, 72 rows 70 to 75; eight sequences
+// of 16K to 128K, 16-token pages, 36 rows (1291 MB, 186 us): 216 to 220.  Of the 55 us, 5 pass until the first tiles are there, 4.5 in the epilogue and 6.5
 // between the kernel's end and the merge's; from 36 rows on the matrix and softmax work is as long as the reads.
 #include "attn_exchange.h"
 #include "attn_stream.h"
