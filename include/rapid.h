@@ -418,7 +418,8 @@ typedef struct rapid_quant_layout {
  * exist and lse_out, computed on the stored values with fp32 accumulation; weights are rounded to bf16 before the second product.  A NaN
  * in a token's K or V reaches the rows that attend this token and no others.
  *   chunk_tokens and ctx_sum_hint are not used: the kernel divides the tokens of the batch by itself
- *   sums are formed before they are divided: 2^8 times the sum of a column's |v| has to stay within fp32's range
+ *   sums are formed before they are divided: 2^9 times the sum of a column's |v| has to stay within fp32's range, and so do scores (times
+ *               softmax_scale log2 e); weights are as exact as 32-bit scores allow however far from zero these lie
  *   batch * max_ctx is at most 2^35, max_ctx 2^30
  *   workspace   >= rapid_verify_attn_quant_workspace_bytes(), 256-byte aligned, any content
  */

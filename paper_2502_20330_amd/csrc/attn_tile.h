@@ -13,7 +13,8 @@ typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 namespace {
 
 constexpr float kRescaleLog2 = 8.0f;   // the running maximum only moves when a tile exceeds it by this (log2 units)
-constexpr float kNoMaximum = -3e38f;   // a row that has met no score yet: finite, so that differences are no NaN; below every score that is
+constexpr float kNoMaximum = -3.402823466e38f;   // a row that has met no score yet: finite, so that differences are no NaN; no score is below it
+constexpr float kFar = 8388608.f;      // 2^23: from here on a reference is far from zero (softmax_tile)
 constexpr int kPieceQuanta = 2;        // what a sequence costs a workgroup besides its tokens, in quanta
 
 template <int D_, bool QUANT_, int TB_>
@@ -241,6 +242,7 @@ template <class G, int RB>
 struct WaveState {
     float m[RB];                     // reference maximum per query row, log2 units (score * scale * log2 e); kNoMaximum at first
     float l[RB];                     // running sum, this lane group's tokens only
+    bool far = false;                // a reference is far from zero (of the wave's rows: uniform)
     floatx4 acc[G::DB][RB];          // O^T: column 16 db + 4 (lane / 16) + i, row 16 rb + lane % 16
 };
 
@@ -343,6 +345,14 @@ __device__ __forceinline__ void meet()
     asm volatile("" ::: "memory");
 }
 
+// s c - m with the product rounded first.
+__device__ __forceinline__ float rounded_exponent(float s, float c, float m)
+{
+#pragma clang fp contract(off)
+    const float y = s * c;
+    return y - m;
+}
+
 // Mask, online softmax; leaves P^T (in 8 bits: times V's scales) as the B operand of PV: slot j of lane group lg in step kk is token
 // 32 kk + 16 (j / 4) + 4 lg + j % 4, what this lane holds in s[2 kk + j / 4][.][j % 4].
 // The reference maximum only moves when a score exceeds it by kRescaleLog2; until then p = 2^(s - ref) <= 2^kRescaleLog2, exact in the final
@@ -379,20 +389,36 @@ __device__ __forceinline__ void softmax_tile(WaveState<G, RB>& st, floatx4 (&s)[
         mx[rb] = s[0][rb][0];
 #pragma unroll
         for (int x = 1; x < G::TB * 4; ++x) mx[rb] = __builtin_elementwise_maximum(mx[rb], s[x / 4][rb][x % 4]);   // (a NaN stays one)
-        above |= mx[rb] * c > st.m[rb] + kRescaleLog2;
+        above |= rounded_exponent(mx[rb], c, st.m[rb]) > kRescaleLog2;
     }
     if (__any(above)) {
+        bool far = false;
 #pragma unroll
         for (int rb = 0; rb < RB; ++rb) {
-            const float top = max_over_groups(mx[rb]) * c;
-            const float m_new = top > st.m[rb] + kRescaleLog2 ? top : st.m[rb];
+            const float top = max_over_groups(mx[rb]);
+            const float m_new = rounded_exponent(top, c, st.m[rb]) > kRescaleLog2 ? top * c : st.m[rb];
             const float alpha = fast_exp2(st.m[rb] - m_new);
             st.m[rb] = m_new;
+            far |= fabsf(m_new) >= kFar && m_new > kNoMaximum;
             st.l[rb] *= alpha;
 #pragma unroll
             for (int db = 0; db < G::DB; ++db)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) st.acc[db][rb][i] *= alpha;
+        }
+        st.far = __any(far);
+    }
+    float ref[RB];
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb) ref[rb] = st.m[rb];
+    if (st.far) {
+        const float inv = 1.f / c;
+#pragma unroll
+        for (int rb = 0; rb < RB; ++rb) {
+            if (fabsf(ref[rb]) < kFar) continue;
+#pragma unroll
+            for (int x = 0; x < G::TB * 4; ++x) s[x / 4][rb][x % 4] = rounded_exponent(s[x / 4][rb][x % 4], c, ref[rb]) * inv;
+            ref[rb] = 0.f;
         }
     }
 #pragma unroll
@@ -402,7 +428,7 @@ __device__ __forceinline__ void softmax_tile(WaveState<G, RB>& st, floatx4 (&s)[
         for (int tb = 0; tb < G::TB; ++tb)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const float p = fast_exp2(fmaf(s[tb][rb][i], c, -st.m[rb]));
+                const float p = fast_exp2(fmaf(s[tb][rb][i], c, -ref[rb]));
                 sum += p;
                 pb[tb / 2][rb][(tb & 1) * 4 + i] = (__bf16)(G::QUANT ? p * vscale[tb][i] : p);
             }
