@@ -310,7 +310,8 @@ __global__ void __launch_bounds__(G::NW * 64) attn_prefix(StreamLaunch a)
     u = __builtin_amdgcn_readfirstlane(u);
     rt = __builtin_amdgcn_readfirstlane(rt);
     const int g = u / a.Hkv, h = __builtin_amdgcn_readfirstlane(u % a.Hkv);
-    for_each_piece(a, __builtin_amdgcn_readfirstlane(g), threadIdx.x & 63, G::QUANTUM, [&](int, int, int c0, int c1) {
+    const int lane = threadIdx.x & 63;
+    for_each_piece(a, __builtin_amdgcn_readfirstlane(g), lane, lane == 0 ? seq_len(a, 0) : 0, G::QUANTUM, [&](int, int, int c0, int c1) {
         const int64_t pbase = ((int64_t)(h * a.tiles + rt) * a.nslots + g) * G::RP;
         const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
         // (the two arms run the same barriers)

@@ -25,6 +25,7 @@ struct StreamLaunch {
     int32_t shared;             // 1: a shared prefix: one sequence (ctx_lens: its length) with the rows of the batch, which all attend all of it
     int32_t RP, tiles;          // packed rows of a slot (a multiple of 16), row tiles (1 but for a prefix)
     int32_t groups, nslots;     // shares of a kv head, groups + B - 1
+    int32_t units;              // two in one launch: workgroups of a kv head, which they divide by their lengths; groups is then the most.  0: groups as they are
     int32_t quantum;            // tokens that shares are cut by
     int32_t rot;                // 1: share g of slot x serves head (x + g) mod Hkv, 0: head x
     int32_t direct;             // 1: short sequences, one workgroup for each and kv head, which writes the result; no partials
@@ -34,7 +35,8 @@ constexpr int kStreamRows = 96;      // packed rows that the streaming kernel ta
 // Fill the plan (RP .. direct) from the shape and the source's layout.
 void plan_attn_stream(StreamLaunch& a, int n_cu);
 void plan_attn_prefix(StreamLaunch& a, int n_cu);
-// Both for one launch: the tokens of a shared prefix, its rows in tiles of at most kStreamRows, and the sequences' own.
+// Both for one launch: the tokens of a shared prefix, its rows in tiles of at most kStreamRows, and the sequences' own.  Where the two lie differently
+// (one paged, the other not), for two launches in turn.
 void plan_attn_stream_pair(StreamLaunch& own, StreamLaunch& prefix, int n_cu);
 size_t attn_stream_workspace_bytes(const StreamLaunch& a);                       // of any plan
 void bind_attn_stream(StreamLaunch& a, void* workspace);

@@ -365,8 +365,8 @@ __device__ __forceinline__ void write_missing_rows(const StreamLaunch& a, int b,
 
 // Grid: one workgroup per (kv head, share).  Partials: [kv head][g + b], which no two pieces of a head share.  Direct: per (kv head, sequence).
 template <class G, bool PAGED>
-__device__ __forceinline__ void stream_share(const StreamLaunch& a, char* smem, int g, int rt = 0)
-{
+__device__ __forceinline__ void stream_share(const StreamLaunch& a, char* smem, int g, int len, int rt = 0)
+{                                                        // len: of sequence `lane`, 0 where there is none
     const int h = __builtin_amdgcn_readfirstlane(a.rot ? (blockIdx.x + g) % a.Hkv : blockIdx.x);     // (base addresses go through scalar registers)
     if (a.direct) {
         const int L = __builtin_amdgcn_readfirstlane(seq_len(a, g));
@@ -374,27 +374,71 @@ __device__ __forceinline__ void stream_share(const StreamLaunch& a, char* smem, 
         if (L > 0) stream_piece<G, PAGED>(a, smem, g, h, L, 0, L, 0, 0);
         return;
     }
-    for_each_piece(a, g, threadIdx.x & 63, G::QUANTUM, [&](int b, int L, int c0, int c1) {
+    for_each_piece(a, g, threadIdx.x & 63, len, G::QUANTUM, [&](int b, int L, int c0, int c1) {
         stream_piece<G, PAGED>(a, smem, b, h, L, c0, c1, ((int64_t)(h * a.tiles + rt) * a.nslots + g + b) * G::RP, rt * G::RP);
         wait_loads<0>();                                 // the partial's stores are out of the load account
     });
+}
+__device__ __forceinline__ int first_len(const StreamLaunch& a)
+{
+    const int lane = threadIdx.x & 63;
+    return !a.direct && lane < a.B ? seq_len(a, lane) : 0;
 }
 template <class G, bool PAGED>
 __global__ void __launch_bounds__(G::NW * 64) attn_stream(StreamLaunch a)
 {
     extern __shared__ __attribute__((aligned(1024))) char smem[];
-    stream_share<G, PAGED>(a, smem, blockIdx.y);
+    stream_share<G, PAGED>(a, smem, blockIdx.y, first_len(a));
+}
+
+// How a prefix and the sequences' own tokens divide the `units` workgroups of a kv head: by what there is to read, of the prefix once for each row tile.
+// It goes by the lengths, which are device data, and by no bound of them, that a caller may set as far above them as a cache's capacity (4 sequences of
+// 300 tokens in caches of 128K, 32K of prefix: 174 us by the bounds, 30 by the lengths).  A sequence costs its own part about as much as 512 tokens, besides
+// those that it has (19 short ones beside 2000 tokens of prefix, 4 kv heads: 19 us, 40 without).
+constexpr int kPieceTokens = 512;
+// The most that the own part takes: the prefix has a workgroup for each row tile, beyond the units where the tiles are many.
+__host__ __device__ constexpr int most_own_units(int units, int tiles)
+{
+    const int left = units - tiles, half = units / 2;
+    return left > half ? left : half > 1 ? half : 1;
+}
+struct PairGroups { int own, prefix; };          // shares of a kv head
+// What the own tokens cost, in units of 32 tokens, that do not pass 32 bits: of the 64 sequences whose lengths the lanes hold.
+__device__ __forceinline__ int pair_cost(int len)
+{
+    return __builtin_amdgcn_readlane(scan_costs((len + 16) >> 5), 63) + __popcll(__ballot(len > 0)) * (kPieceTokens / 32);
+}
+__device__ __forceinline__ PairGroups pair_groups(const StreamLaunch& own, const StreamLaunch& prefix, int own_cost, int prefix_len)
+{
+    if (own.units == 0) return {own.groups, prefix.groups};
+    const float mine = (float)own_cost, other = (float)(prefix.tiles * ((prefix_len + 16) >> 5));
+    // (the merge must find what the shares were: both take the hardware's reciprocal, whose last bits do not matter)
+    int g = (int)((float)own.units * mine * __builtin_amdgcn_rcpf(fmaxf(mine + other, 1.f)));
+    g = __builtin_amdgcn_readfirstlane(max(1, min(g, most_own_units(own.units, prefix.tiles))));
+    const int left = max(own.units - g, 0), each = prefix.tiles == 1 ? left : (int)((unsigned)left / (unsigned)prefix.tiles);
+    return {min(g, own.groups), min(max(1, each), prefix.groups)};
 }
 // bf16: two in one launch, the shares of a prefix (or none), then those of the sequences' own tokens; both paged or neither.
 template <class G, bool PAGED>
 __global__ void __launch_bounds__(G::NW * 64) attn_stream_pair(StreamLaunch own, StreamLaunch prefix)
 {
     extern __shared__ __attribute__((aligned(1024))) char smem[];
-    const int y = __builtin_amdgcn_readfirstlane(blockIdx.y), shares = prefix.groups * prefix.tiles;
+    const int y = __builtin_amdgcn_readfirstlane(blockIdx.y);
+    PairGroups groups{own.groups, prefix.groups};
+    int len = first_len(own), P = 0;
+    if (own.units) {
+        P = seq_len(prefix, 0);
+        int cost = pair_cost(len);
+        for (int b = 64 + (threadIdx.x & 63); b - (int)(threadIdx.x & 63) < own.B; b += 64) cost += pair_cost(b < own.B ? seq_len(own, b) : 0);
+        groups = pair_groups(own, prefix, cost, P);
+    }
+    const int shares = groups.prefix * prefix.tiles;
     const bool first = y < shares;
-    const StreamLaunch a = first ? prefix : own;
+    StreamLaunch a = first ? prefix : own;
+    a.groups = first ? groups.prefix : groups.own;
+    if (first) len = (threadIdx.x & 63) == 0 ? P : 0;
     const int g = first ? y : y - shares;
-    stream_share<G, PAGED>(a, smem, g / a.tiles, g % a.tiles);
+    stream_share<G, PAGED>(a, smem, g / a.tiles, len, g % a.tiles);
 }
 
 // The partials of one row: `n` of them, from row slot `slot` on, RP slots apart.
@@ -402,24 +446,34 @@ struct Partials {
     int n = 0;
     int64_t slot = 0;
 };
-// Those of packed row `row` of sequence b, head h.
-__device__ __forceinline__ Partials find_partials(const StreamLaunch& a, int b, int h, int row, int lane, int len)
+// Where a sequence stands among the batch's quanta.
+struct Place {
+    int before = 0, cost = 0, total = 0, pair = 0;       // pair: cost of all of them as pair_cost() counts it
+};
+template <bool PAIR>
+__device__ __forceinline__ Place find_place(const StreamLaunch& a, int b, int lane, int len)
 {                                                        // len: of sequence `lane`, 0 where there is none
-    int before = 0, total = 0, cost = 0;
+    Place p;
     for (int b0 = 0; b0 < a.B; b0 += 64) {
         if (b0) len = b0 + lane < a.B ? seq_len(a, b0 + lane) : 0;
         const int mine = seq_cost(len, b0 + lane, a.quantum);
-        const int end = total + scan_costs(mine);
+        const int end = p.total + scan_costs(mine);
         if (b >= b0 && b < b0 + 64) {
-            cost = __builtin_amdgcn_readlane(mine, b - b0);
-            before = __builtin_amdgcn_readlane(end, b - b0) - cost;
+            p.cost = __builtin_amdgcn_readlane(mine, b - b0);
+            p.before = __builtin_amdgcn_readlane(end, b - b0) - p.cost;
         }
-        total = __builtin_amdgcn_readlane(end, 63);
+        p.total = __builtin_amdgcn_readlane(end, 63);
+        if (PAIR) p.pair += pair_cost(len);
     }
+    return p;
+}
+// The partials of packed row `row` of sequence b, head h, of `groups` shares.
+__device__ __forceinline__ Partials find_partials(const StreamLaunch& a, const Place& at, int groups, int b, int h, int row)
+{
     Partials p;
-    if (cost > 0) {
-        const Shares sh(total, a.groups);
-        const int g0 = sh.owner(before + piece_cost(b)), g1 = sh.owner(before + cost - 1);
+    if (at.cost > 0) {
+        const Shares sh(at.total, groups);
+        const int g0 = sh.owner(at.before + piece_cost(b)), g1 = sh.owner(at.before + at.cost - 1);
         p.n = g1 - g0 + 1;
         p.slot = ((int64_t)(h * a.tiles + row / a.RP) * a.nslots + g0 + b) * a.RP + row % a.RP;
     }
@@ -489,25 +543,22 @@ __global__ void __launch_bounds__(D) attn_stream_merge(StreamLaunch a, StreamLau
     // All that can be asked for is asked for at once: the lengths, the first block of a single sequence (the prefix is one) before its length is known, the
     // other's as soon as the lengths are there.
     const int lane = d & 63;
-    const int len = lane < a.B ? seq_len(a, lane) : 0, prefix_len = PREFIX && lane == 0 ? seq_len(prefix, 0) : 0;
+    const int len = lane < a.B ? seq_len(a, lane) : 0, prefix_len = PREFIX ? seq_len(prefix, 0) : 0;
     const bool there = seq_len(a, b) > 0;                 // (a sequence without tokens has no rows, behind a prefix either)
     const int prefix_row = b * a.Qmax * a.G + row;
     PartialBlock x, y;
     const int64_t x_slot = PREFIX ? first_slot(prefix, h, prefix_row) : 0;
     if (PREFIX) x.load<D>(prefix, x_slot, prefix.nslots, d);
-    Partials own;
-    if (a.B == 1) {
-        own.slot = first_slot(a, h, row);
-        y.load<D>(a, own.slot, a.nslots, d);
-        own.n = find_partials(a, 0, h, row, lane, len).n;
-    } else {
-        own = find_partials(a, b, h, row, lane, len);
-        y.load<D>(a, own.slot, own.n, d);
-    }
+    if (a.B == 1) y.load<D>(a, first_slot(a, h, row), a.nslots, d);
+    const Place at = find_place<PREFIX>(a, b, lane, len);
+    PairGroups groups{a.groups, 0};
+    if (PREFIX) groups = pair_groups(a, prefix, at.pair, prefix_len);
+    const Partials own = find_partials(a, at, groups.own, b, h, row);
+    if (a.B != 1) y.load<D>(a, own.slot, own.n, d);
     RowMerge r;
     float num = 0.f;
     if (PREFIX) {
-        const int n = there ? find_partials(prefix, 0, h, prefix_row, lane, prefix_len).n : 0;
+        const int quanta = (prefix_len + prefix.quantum - 1) / prefix.quantum, n = there ? min(groups.prefix, quanta) : 0;   // a share each
         x.fold(n, d, r, num);
         fold_partials<D>(prefix, x_slot + (int64_t)kMergeBlock * prefix.RP, n - kMergeBlock, d, r, num);
     }
@@ -601,20 +652,15 @@ void plan_attn_stream(StreamLaunch& a, int n_cu)
     a.direct = a.max_ctx <= quanta * a.quantum;
 }
 
-// A sequence costs its own part about as much as 512 tokens, besides those that it has (19 short ones beside 2000 tokens of prefix, 4 kv heads: 19 us, 40 without).
-constexpr int kPieceTokens = 512;
-
 void plan_attn_stream_pair(StreamLaunch& own, StreamLaunch& prefix, int n_cu)
 {
-    const int rows = prefix.Qmax * prefix.G, own_rows = own.Qmax * own.G, each = n_cu / own.Hkv;
+    const int rows = prefix.Qmax * prefix.G, own_rows = own.Qmax * own.G, each = n_cu > own.Hkv ? n_cu / own.Hkv : 1;
     const int rb = rows <= kStreamRows ? (rows + 15) / 16 : own_rows <= 48 ? 3 : (own_rows + 15) / 16;
     const int tiles = (rows + rb * 16 - 1) / (rb * 16);
-    const int64_t tokens = (int64_t)own.B * (own.max_ctx + kPieceTokens);
-    int mine = (int)(each * tokens / (tokens + (int64_t)tiles * prefix.max_ctx));       // of the compute units, by what there may be to read
-    if (mine < 1) mine = 1;
-    plan_shares(own, rb, mine);
-    plan_shares(prefix, rb, (each - own.groups) / tiles);
+    plan_shares(own, rb, each);
+    plan_shares(prefix, rb, each / tiles);
     prefix.tiles = tiles;
+    own.units = !prefix.own.page_table == !own.own.page_table ? each : 0;
 }
 
 size_t attn_stream_workspace_bytes(const StreamLaunch& a)
@@ -649,7 +695,7 @@ hipError_t launch_attn_stream(const StreamLaunch& a, hipStream_t stream)
 
 hipError_t launch_attn_stream_pair(const StreamLaunch& own, const StreamLaunch& prefix, hipStream_t stream)
 {
-    if (!prefix.own.page_table != !own.own.page_table) {               // (rare: a prefix of its own beside paged sequences)
+    if (own.units == 0) {                                               // (rare: a prefix of its own beside paged sequences)
         const hipError_t e = launch_attn_stream(prefix, stream);
         return e == hipSuccess ? launch_attn_stream(own, stream) : e;
     }
@@ -657,7 +703,9 @@ hipError_t launch_attn_stream_pair(const StreamLaunch& own, const StreamLaunch& 
         using G = decltype(geo);
         if constexpr (!G::QUANT) {
             auto fn = own.own.page_table ? attn_stream_pair<G, true> : attn_stream_pair<G, false>;
-            hipLaunchKernelGGL(fn, dim3(own.Hkv, own.groups + prefix.groups * prefix.tiles), dim3(G::NW * 64), G::LDS, stream, own, prefix);
+            const int with_tiles = most_own_units(own.units, prefix.tiles) + prefix.tiles;
+            const int shares = with_tiles > own.units ? with_tiles : own.units;
+            hipLaunchKernelGGL(fn, dim3(own.Hkv, shares), dim3(G::NW * 64), G::LDS, stream, own, prefix);
             return hipGetLastError();
         }
         return hipErrorInvalidValue;

@@ -68,9 +68,8 @@ struct Shares {
 };
 // Calls piece(b, L, c0, c1) for every piece [c0, c1) of a sequence b in share g, in order.  Sequences are taken 64 at a time, one a lane.
 template <class Piece>
-__device__ __forceinline__ void for_each_piece(const StreamLaunch& a, int g, int lane, int quantum, Piece piece)
-{
-    int len = lane < a.B ? seq_len(a, lane) : 0;
+__device__ __forceinline__ void for_each_piece(const StreamLaunch& a, int g, int lane, int len, int quantum, Piece piece)
+{                                                        // len: of sequence `lane`, 0 where there is none
     int cost = seq_cost(len, lane, quantum);
     int end = scan_costs(cost);                          // cost of the sequences up to this one
     int total = __builtin_amdgcn_readlane(end, 63);
