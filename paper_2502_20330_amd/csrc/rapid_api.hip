@@ -73,7 +73,7 @@ int check_attn_shape(const rapid_attn_shape* s)
     if (s->kv_token_stride < s->head_dim || s->kv_token_stride % 8 || s->kv_head_stride % 8) return RAPID_EALIGN;
     // rows of one (sequence, head) are addressed with 32-bit byte offsets
     const int64_t span_tokens = s->page_size ? s->page_size : s->max_ctx;
-    if (s->kv_token_stride * 2 * span_tokens >= (int64_t)1 << 32) return RAPID_EUNSUPPORTED;
+    if (s->kv_token_stride > (((int64_t)1 << 31) - 1) / span_tokens) return RAPID_EUNSUPPORTED;
     // and so are the rows of q
     if ((int64_t)s->batch * s->q_max * s->n_q_heads * s->head_dim * 2 >= (int64_t)1 << 32) return RAPID_EUNSUPPORTED;
     return RAPID_OK;
