@@ -200,7 +200,7 @@ class Rapid:
         self._ws_args = (None, 0, None, 0)             # address and size of the exchange memory and of the workspace, as a call takes them
         self._ws_accept: Optional[torch.Tensor] = None
         self._ws_streams: dict = {}                    # address and size of the quantised and the prefix attention's workspace, by stream
-        self._ws_kept: list = []                       # those, and the ones they have outgrown
+        self._ws_kept: dict = {}                       # and the tensors
         self._plans: dict = {}                         # shapes and layouts of calls by their sizes (_planned)
         self._sink: Optional[torch.Tensor] = None
 
@@ -480,13 +480,24 @@ class Rapid:
 
     _NO_WORKSPACE = (None, 0)
 
-    def _stream_workspace(self, stream: int, nbytes: int):
-        # one for each stream, so that calls on two may overlap.  It grows only, and what it has outgrown is kept: a captured graph goes on using the
-        # one that it was recorded with
+    def _capturing(self) -> bool:
+        if torch.cuda.current_device() == self.device.index:
+            return torch.cuda.is_current_stream_capturing()
+        with torch.cuda.device(self.device):
+            return torch.cuda.is_current_stream_capturing()
+
+    def _stream_workspace(self, stream: int):
+        # Address and size.  Eager calls of a stream share a workspace, so that calls on two may overlap; a captured call begins with none.
+        # (The default stream is never captured.)
+        return self._NO_WORKSPACE if stream and self._capturing() else self._ws_streams.get(stream, self._NO_WORKSPACE)
+
+    def _new_workspace(self, stream: int, nbytes: int) -> torch.Tensor:
+        # a captured call takes memory of its graph's, like any temporary tensor of a capture; a stream's own grows only
+        if stream and self._capturing():
+            return torch.empty(max(nbytes, 256), dtype=torch.uint8, device=self.device)
         ws = torch.empty(max(nbytes, 2 * self._ws_streams.get(stream, self._NO_WORKSPACE)[1], 256), dtype=torch.uint8, device=self.device)
-        self._ws_kept.append(ws)
-        self._ws_streams[stream] = (ws.data_ptr(), ws.numel())
-        return self._ws_streams[stream]
+        self._ws_kept[stream], self._ws_streams[stream] = ws, (ws.data_ptr(), ws.numel())
+        return ws
 
     def rapid_kv_append_quant(self, k_codes, v_codes, k_scales, v_scales, k_new, v_new, ctx_lens, gamma: Optional[int] = None, *,
                               gammas=None, page_table=None, max_ctx: Optional[int] = None):
@@ -541,7 +552,7 @@ class Rapid:
                                 out=None, lse_out=None):
         """:meth:`rapid_verify_attn` on a cache in 8 bits (layout: :meth:`rapid_kv_append_quant`): q bf16 [B,Qmax,Hq,d]; returns
         out bf16 [B,Qmax,Hq,d] and fills lse_out fp32 [B,Hq,Qmax] if given.  One position (Qmax = 1) is a decode step.
-        Calls on different streams may overlap; graphs captured on one stream use one workspace and may not."""
+        Calls on different streams may overlap, and graphs (captured by torch.cuda.graph) may overlap with them and one another."""
         if out is None:
             out = torch.empty_like(q)
 
@@ -552,10 +563,10 @@ class Rapid:
         args = (self._ctx, shape, layout, q.data_ptr(), k_codes.data_ptr(), v_codes.data_ptr(), k_scales.data_ptr(),
                 v_scales.data_ptr(), ctx_lens.data_ptr(), _dptr(gammas), _dptr(page_table), out.data_ptr(), _dptr(lse_out))
         call, stream = self.lib.rapid_verify_attn_quant, _stream_ptr(self.device)
-        rc = call(*args, *self._ws_streams.get(stream, self._NO_WORKSPACE), stream)
+        rc = call(*args, *self._stream_workspace(stream), stream)
         if rc == RAPID_EWORKSPACE:                             # the last check of the call: nothing has been launched
-            need = self.lib.rapid_verify_attn_quant_workspace_bytes(self._ctx, shape)
-            rc = call(*args, *self._stream_workspace(stream, need), stream)
+            ws = self._new_workspace(stream, self.lib.rapid_verify_attn_quant_workspace_bytes(self._ctx, shape))
+            rc = call(*args, ws.data_ptr(), ws.numel(), stream)
         if rc:
             _check(self.lib, rc, self._ctx)
         return out
@@ -585,10 +596,10 @@ class Rapid:
                 k_cache.data_ptr(), v_cache.data_ptr(), ctx_lens.data_ptr(), _dptr(gammas), _dptr(page_table), out.data_ptr(),
                 _dptr(lse_out))
         call, stream = self.lib.rapid_verify_attn_prefix, _stream_ptr(self.device)
-        rc = call(*args, *self._ws_streams.get(stream, self._NO_WORKSPACE), stream)
+        rc = call(*args, *self._stream_workspace(stream), stream)
         if rc == RAPID_EWORKSPACE:                             # the last check of the call: nothing has been launched
-            need = self.lib.rapid_verify_attn_prefix_workspace_bytes(self._ctx, shape, prefix)
-            rc = call(*args, *self._stream_workspace(stream, need), stream)
+            ws = self._new_workspace(stream, self.lib.rapid_verify_attn_prefix_workspace_bytes(self._ctx, shape, prefix))
+            rc = call(*args, ws.data_ptr(), ws.numel(), stream)
         if rc:
             _check(self.lib, rc, self._ctx)
         return out
