@@ -419,7 +419,9 @@ class Rapid:
     # ------------------------------------------------------------------ cache in 8 bits, shared prefix
     def _planned(self, key, plan, *args):
         """What a call of these sizes, strides, types and devices needs besides addresses: plan(*args) checks them and answers, once for
-        each key, which holds them all (the checks took three times as long as the rest of a small call)."""
+        each key, which holds them all (the checks took three times as long as the rest of a small call).  Numbers are the host's: a tensor in a
+        key would stand for itself and not for its value."""
+        self._need(not any(isinstance(x, torch.Tensor) for x in key), "sizes and the scale are numbers, not tensors")
         for t in args:
             self._need(not isinstance(t, torch.Tensor) or t.device == self.device, f"a tensor is not on {self.device}")
         got = plan(*args)
