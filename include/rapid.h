@@ -146,6 +146,8 @@ size_t rapid_verify_attn_workspace_bytes(const rapid_ctx* ctx, const rapid_attn_
  * them).  Query row i (0 <= i < Q) of head h attends keys 0 .. L-Q+i:
  *     out[b,i,h,:] = softmax_j(softmax_scale * <q[b,i,h,:], k[b,j,h/G,:]>) . v[b,j,h/G,:]
  * computed with fp32 accumulation from bf16 inputs, result rounded to bf16.
+ * Scores, times softmax_scale log2 e, lie within 2^24 of zero (farther out their
+ * rounding moves the weights, and can leave a row without any).
  * Rows i >= Q are written as zeros.  Rotary embedding etc. are the caller's.
  *
  *   q          bf16 [B, Qmax, Hq, d], contiguous
@@ -442,8 +444,8 @@ int rapid_verify_attn_quant(rapid_ctx* ctx, const rapid_attn_shape* shape, const
  * context): the prefix is kept once and read once for all of the batch's rows.  With P = prefix_len[0] and the rest as for rapid_verify_attn,
  * sequence b's own tokens follow the prefix, ctx_lens[b] counts them alone, and row i of head h attends the prefix and its own keys 0 .. L-Q+i:
  *     out[b,i,h,:] = softmax over (prefix keys, own keys) . (their values);  lse_out likewise over both
- * Rows i >= Q, and all rows of a sequence with ctx_lens[b] = 0, are written as zeros, their lse_out as 0 and as -infinity.  A NaN or infinity in
- * a token's K or V reaches the rows that attend this token and no others.
+ * Sums are fp32, weights are rounded to bf16 before the second product.  Rows i >= Q, and all rows of a sequence with ctx_lens[b] = 0, are written
+ * as zeros, their lse_out as 0 and as -infinity.  A NaN or infinity in a token's K or V reaches the rows that attend this token and no others.
  *   prefix_len    int32 [1], device data, 0 <= prefix_len[0] <= max_prefix (clamped to that range)
  *   k_prefix, v_prefix   bf16, 16-byte aligned, element (token j, kv head h, c) at j*token_stride + h*head_stride + c (in elements, multiples
  *                 of 8); NULL where prefix_table is given, or where max_prefix is 0
@@ -454,7 +456,8 @@ int rapid_verify_attn_quant(rapid_ctx* ctx, const rapid_attn_shape* shape, const
  *   workspace     >= rapid_verify_attn_prefix_workspace_bytes(), 256-byte aligned, any content
  */
 typedef struct rapid_prefix_layout {
-    int32_t max_prefix;       /* upper bound of prefix_len[0], >= 0; sizes the grid and the workspace */
+    int32_t max_prefix;       /* upper bound of prefix_len[0], >= 0; sizes the grid and the workspace, and beyond 96 rows of the batch a kv head */
+                              /* chooses the kernel: a bound near the length is then worth giving                                              */
     int32_t max_pages;        /* length of prefix_table                                             */
     int64_t token_stride;
     int64_t head_stride;

@@ -2,14 +2,16 @@
 //
 // All rows of the batch, R = B (gamma_max + 1) G per kv head, attend the same P tokens, without a mask: the prefix is one "sequence"
 // with R rows.  Reading it costs 4 d bytes per token and kv head, computing 4 R d multiply-adds and R exponentials, so that from about a hundred rows on the
-// matrix cores and the exponentials bound it and no longer the memory.  Up to 96 rows, and where all of it is little work, the streaming kernel (attn_stream.hip) does it; this one takes more:
+// matrix cores and the exponentials bound it and no longer the memory.  Up to 96 rows, and where all of it is little work, the streaming kernel (attn_stream.hip) does it; this one takes more.
+// The rows are packed as q holds them: those past a sequence's drafts, and the last tile's padding, are computed like the others and read by nobody.
 //  * A workgroup has eight waves, T of which share a stream of token tiles (8 / T streams) and hold one to three blocks of 16 rows each, 128 to 384 rows
 //    together.  Tiles go HBM -> LDS once a workgroup; S of them lie in a ring, and the waves meet every S / 4 tiles: then the next ones have landed
 //    and the slots of the ones before are free.
 //  * Rows beyond that go to other workgroups, which read the same tokens at about the same time on the same die (blockIdx modulo 8), so that its L2
 //    serves all but one of them.
-// Measured (8 kv heads of 128): 131000 tokens, 320 rows 183 to 198 us (550 to 600 TFLOP/s), 32K tokens, 288 rows 57.  A tile of 384 rows takes 2735 cycles, 1536 of
-// them matrix instructions, at 1.96 GHz, where the power limit holds the clock; the exponentials and conversions run beside them in part only.
+// Measured (8 kv heads of 128): 131000 tokens, 320 rows 187 to 207 us (830 to 920 TFLOP/s of what is computed; 228 of the rows exist in that case: 590 to
+// 650), 32K tokens, 288 rows 58.  By counters the matrix cores are busy in 43 % of the compute units' cycles there, 1284 of about 3000 a tile of 32 tokens; 304 vector
+// instructions of a SIMD's two waves a tile, exponentials and conversions, run beside them in part only.
 #include "attn_tile.h"
 
 namespace {

@@ -98,7 +98,8 @@ __device__ __forceinline__ void for_each_piece(const StreamLaunch& a, int g, int
 }
 
 // The same number, of which the compiler knows nothing: what rare paths make of it is computed there, and does not take registers from the
-// main loop (a spilled one is loaded back ahead of the loop, and that load waits for all the tiles under way).
+// main loop (a spilled one is loaded back ahead of the loop, and that load waits for all the tiles under way).  Three blocks of 16 rows a wave use all
+// there are: a few kernels keep 12 bytes in scratch, written ahead of the loop or read behind it.
 __device__ __forceinline__ int opaque(int lane)
 {
     asm volatile("" : "+v"(lane));
@@ -352,8 +353,10 @@ __device__ __forceinline__ float rounded_exponent(float s, float c, float m)
     return y - m;
 }
 
-// Mask, online softmax; leaves P^T (in 8 bits: times V's scales) as the B operand of PV: slot j of lane group lg in step kk is token
+// Mask, online softmax; leaves P^T (in 8 bits: times V's scales), rounded to bf16 as the matrix cores take it, as the B operand of PV: slot j of lane group lg in step kk is token
 // 32 kk + 16 (j / 4) + 4 lg + j % 4, what this lane holds in s[2 kk + j / 4][.][j % 4].
+// That is the one rounding of a weight, by at most half a step, 2^-8 of it; an operand of more bits would take a second product.  Against 64 bits a result, with its
+// own rounding, is up to 1.4 times as far off as one of 32-bit weights.  The sum of the weights takes them unrounded.
 // The reference maximum only moves when a score exceeds it by kRescaleLog2; until then p = 2^(s - ref) <= 2^kRescaleLog2, exact in the final
 // ratio.  So a tile's own maxima are only looked at lane by lane, and brought together over the lanes of a row when one of them asks for it.
 template <class G, int RB>
