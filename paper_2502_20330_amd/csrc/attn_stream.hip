@@ -393,7 +393,7 @@ __global__ void __launch_bounds__(G::NW * 64) attn_stream(StreamLaunch a)
 
 // How a prefix and the sequences' own tokens divide the `units` workgroups of a kv head: by what there is to read, of the prefix once for each row tile.
 // It goes by the lengths, which are device data, and by no bound of them, that a caller may set as far above them as a cache's capacity (4 sequences of
-// 300 tokens in caches of 128K, 32K of prefix: 174 us by the bounds, 30 by the lengths).  A sequence costs its own part about as much as 512 tokens, besides
+// 300 tokens in caches of 128K, 32K of prefix: 174 us by the bounds, 30 by the lengths; looking at all lengths first costs every call about 0.5 us).  A sequence costs its own part about as much as 512 tokens, besides
 // those that it has (19 short ones beside 2000 tokens of prefix, 4 kv heads: 19 us, 40 without).
 constexpr int kPieceTokens = 512;
 // The most that the own part takes: the prefix has a workgroup for each row tile, beyond the units where the tiles are many.
@@ -403,20 +403,19 @@ __host__ __device__ constexpr int most_own_units(int units, int tiles)
     return left > half ? left : half > 1 ? half : 1;
 }
 struct PairGroups { int own, prefix; };          // shares of a kv head
-// What the own tokens cost, in units of 32 tokens, that do not pass 32 bits: of the 64 sequences whose lengths the lanes hold.
-__device__ __forceinline__ int pair_cost(int len)
+// quanta: the sum of the own tokens' seq_cost(), of n sequences that have any.
+__device__ __forceinline__ PairGroups pair_groups(const StreamLaunch& own, const StreamLaunch& prefix, int quanta, int n, int prefix_len)
 {
-    return __builtin_amdgcn_readlane(scan_costs((len + 16) >> 5), 63) + __popcll(__ballot(len > 0)) * (kPieceTokens / 32);
-}
-__device__ __forceinline__ PairGroups pair_groups(const StreamLaunch& own, const StreamLaunch& prefix, int own_cost, int prefix_len)
-{
+#pragma clang fp contract(off)
+    // The merge must find what the shares were: the same operations on both sides, whose last bits do not matter.  In half quanta; a sequence's last one is half full.
     if (own.units == 0) return {own.groups, prefix.groups};
-    const float mine = (float)own_cost, other = (float)(prefix.tiles * ((prefix_len + 16) >> 5));
-    // (the merge must find what the shares were: both take the hardware's reciprocal, whose last bits do not matter)
+    const float mine = (float)(2 * quanta + n * (2 * kPieceTokens / own.quantum - 2 * kPieceQuanta - 1));
+    const float other = (float)prefix.tiles * (float)prefix_len * __builtin_amdgcn_rcpf((float)(own.quantum / 2));
     int g = (int)((float)own.units * mine * __builtin_amdgcn_rcpf(fmaxf(mine + other, 1.f)));
     g = __builtin_amdgcn_readfirstlane(max(1, min(g, most_own_units(own.units, prefix.tiles))));
-    const int left = max(own.units - g, 0), each = prefix.tiles == 1 ? left : (int)((unsigned)left / (unsigned)prefix.tiles);
-    return {min(g, own.groups), min(max(1, each), prefix.groups)};
+    const int left = max(own.units - g, 0), each = max(1, prefix.tiles == 1 ? left : (int)((unsigned)left / (unsigned)prefix.tiles));
+    g = max(g, own.units - each * prefix.tiles);                 // what the row tiles leave over
+    return {min(g, own.groups), min(each, prefix.groups)};
 }
 // bf16: two in one launch, the shares of a prefix (or none), then those of the sequences' own tokens; both paged or neither.
 template <class G, bool PAGED>
@@ -428,9 +427,14 @@ __global__ void __launch_bounds__(G::NW * 64) attn_stream_pair(StreamLaunch own,
     int len = first_len(own), P = 0;
     if (own.units) {
         P = seq_len(prefix, 0);
-        int cost = pair_cost(len);
-        for (int b = 64 + (threadIdx.x & 63); b - (int)(threadIdx.x & 63) < own.B; b += 64) cost += pair_cost(b < own.B ? seq_len(own, b) : 0);
-        groups = pair_groups(own, prefix, cost, P);
+        int quanta = 0, n = 0;
+        for (int b0 = 0, l = len; b0 < own.B; b0 += 64) {
+            const int b = b0 + (threadIdx.x & 63);
+            if (b0) l = b < own.B ? seq_len(own, b) : 0;
+            quanta += __builtin_amdgcn_readlane(scan_costs(seq_cost(l, b, G::QUANTUM)), 63);
+            n += __popcll(__ballot(l > 0));
+        }
+        groups = pair_groups(own, prefix, quanta, n, P);
     }
     const int shares = groups.prefix * prefix.tiles;
     const bool first = y < shares;
@@ -448,9 +452,8 @@ struct Partials {
 };
 // Where a sequence stands among the batch's quanta.
 struct Place {
-    int before = 0, cost = 0, total = 0, pair = 0;       // pair: cost of all of them as pair_cost() counts it
+    int before = 0, cost = 0, total = 0, n = 0;          // n: sequences that have tokens
 };
-template <bool PAIR>
 __device__ __forceinline__ Place find_place(const StreamLaunch& a, int b, int lane, int len)
 {                                                        // len: of sequence `lane`, 0 where there is none
     Place p;
@@ -463,7 +466,7 @@ __device__ __forceinline__ Place find_place(const StreamLaunch& a, int b, int la
             p.before = __builtin_amdgcn_readlane(end, b - b0) - p.cost;
         }
         p.total = __builtin_amdgcn_readlane(end, 63);
-        if (PAIR) p.pair += pair_cost(len);
+        p.n += __popcll(__ballot(len > 0));
     }
     return p;
 }
@@ -550,9 +553,9 @@ __global__ void __launch_bounds__(D) attn_stream_merge(StreamLaunch a, StreamLau
     const int64_t x_slot = PREFIX ? first_slot(prefix, h, prefix_row) : 0;
     if (PREFIX) x.load<D>(prefix, x_slot, prefix.nslots, d);
     if (a.B == 1) y.load<D>(a, first_slot(a, h, row), a.nslots, d);
-    const Place at = find_place<PREFIX>(a, b, lane, len);
+    const Place at = find_place(a, b, lane, len);
     PairGroups groups{a.groups, 0};
-    if (PREFIX) groups = pair_groups(a, prefix, at.pair, prefix_len);
+    if (PREFIX) groups = pair_groups(a, prefix, at.total, at.n, prefix_len);
     const Partials own = find_partials(a, at, groups.own, b, h, row);
     if (a.B != 1) y.load<D>(a, own.slot, own.n, d);
     RowMerge r;
