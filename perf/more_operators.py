@@ -6,9 +6,9 @@ Four operators around a draft:
           (rapid_kv_append_rope, and rapid_kv_append_rope_quant into a cache in 8 bits)
   window  attention that sees the last `window` tokens and the first `sinks` ones, from one position to a whole prompt
           (rapid_verify_attn_window)
-  codes   rows of bf16 values become 8-bit integers with a scale for each row (rapid_quant_rows_int8)
+  codes   rows of bf16 values become 8-bit integers with a scale for each row (rapid_quant_rows)
   head    logits of the drafted rows from an output embedding that is kept that way, with the row statistics of the accept
-          pass (rapid_lm_head_int8)
+          pass (rapid_lm_head_quant)
 
 A row x of 8-bit integers: code[c] = 127 x[c] / max |x| to the nearest whole number, ties to even; the scale is max |x| / 127 in 32
 bits.  Codes are kept in rows of a multiple of 256, zeros behind the last one.
@@ -393,9 +393,9 @@ def run(s):
         return _results(s)
     r = _handle()
     if op == "codes":
-        r.rapid_quant_rows_int8(s["x"], codes=s["codes"], scales=s["scales"])
+        r.rapid_quant_rows(s["x"], codes=s["codes"], scales=s["scales"])
     elif op == "head":
-        r.rapid_lm_head_int8(s["h"], s["codes"], s["scales"], want_stats=case["stats"], logits=s["logits"], stats=s["stats"])
+        r.rapid_lm_head_quant(s["h"], s["codes"], s["scales"], want_stats=case["stats"], logits=s["logits"], stats=s["stats"])
     elif op == "window":
         r.rapid_verify_attn_window(s["q"], s["k"], s["v"], s["lens"], case["window"], sinks=case["sinks"], gammas=s["gammas"],
                                    page_table=s["table"], max_ctx=case["ctx"], out=s["out"], lse_out=s["lse"])
