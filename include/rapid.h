@@ -18,6 +18,9 @@
  * (cache bookkeeping of a validation round), rapid_retrieve (the RAG drafter's
  * chunk selection, Sec. 2.2) and rapid_hbm_read_probe (a measurement aid).
  *
+ * The drafter's side: rapid_kv_append_rope (rotary positions on the way into the cache), rapid_verify_attn_window (attention with
+ * a sliding window), rapid_lm_head_quant (an output embedding in 8-bit integers).
+ *
  * Two ways to read less of the cache: a cache in 8 bits (rapid_kv_append_quant,
  * rapid_verify_attn_quant, rapid_kv_read_quant), and one copy of a prefix that the
  * sequences of a batch share (rapid_verify_attn_prefix).
@@ -305,6 +308,37 @@ int rapid_lm_head(rapid_ctx* ctx, int n_rows, int hidden, int vocab,
                   float* logits, int64_t logits_row_stride, float* stats, void* stream);
 
 /*
+ * Rows of bf16 values as 8-bit integers, a scale for each row: with m = max |x_c| of a row
+ *     codes[r][c] = 127 x_c / m to the nearest whole number, ties to even;   scales[r] = m / 127 (fp32)
+ * A row of zeros has codes 0 and the scale 0, a row with a NaN or an infinity codes 0 and the scale NaN.
+ *   rows, cols    rows < 2^31, cols a multiple of 8, at most 2^17
+ *   x             bf16, row r at x + r * row_stride elements (a multiple of 8, at least cols), 16-byte aligned
+ *   codes         int8 [rows, pitch], 16-byte aligned; pitch is cols rounded up to a multiple of 256, and zeros fill the rows
+ *   scales        fp32 [rows]
+ */
+int rapid_quant_rows(rapid_ctx* ctx, int64_t rows, int cols, const void* x, int64_t row_stride, void* codes, float* scales,
+                     void* stream);
+
+/*
+ * rapid_lm_head on an output embedding in 8-bit integers (rapid_quant_rows of it): the rows of h are brought to codes in the same way, and
+ *     logits[r][v] = s_h[r] * w_scales[v] * sum_k c_h[r][k] * w_codes[v][k]
+ * The sum is exact; at most three roundings of 2^-24 follow.  Half of the bytes of bf16 weights.  Made for a drafter: whatever its distribution
+ * is, rapid_accept takes it into account, as long as the drafts were drawn from these very logits.  A row of h with a NaN or an infinity
+ * has logits that are NaN, and so does an entry whose scale is NaN.
+ *   n_rows 1..96, hidden a multiple of 8 and at most 2^17, vocab >= 16
+ *   h             bf16 [n_rows, hidden], contiguous, 16-byte aligned
+ *   w_codes       int8 [vocab, pitch] (pitch: hidden rounded up to a multiple of 256; what lies behind hidden has no effect), 16-byte aligned
+ *   w_scales      fp32 [vocab]
+ *   temperature, logits, logits_row_stride, stats   as for rapid_lm_head, with the same chunks
+ *   workspace     >= rapid_lm_head_quant_workspace_bytes(), 256-byte aligned, any content
+ */
+size_t rapid_lm_head_quant_workspace_bytes(const rapid_ctx* ctx, int n_rows, int hidden);   /* 0 on bad sizes */
+int rapid_lm_head_quant(rapid_ctx* ctx, int n_rows, int hidden, int vocab,
+                        const void* h, const void* w_codes, const float* w_scales, float temperature,
+                        float* logits, int64_t logits_row_stride, float* stats,
+                        void* workspace, size_t workspace_bytes, void* stream);
+
+/*
  * rapid_accept with the (max, sum exp) statistics of the rows supplied by the caller
  * instead of being formed from the logits by a first pass (same results up to the
  * rounding order of the fp32 sums inside a chunk):
@@ -438,6 +472,41 @@ int rapid_verify_attn_quant(rapid_ctx* ctx, const rapid_attn_shape* shape, const
                             const void* k_codes, const void* v_codes, const void* k_scales, const void* v_scales,
                             const int32_t* ctx_lens, const int32_t* gammas, const int32_t* page_table,
                             void* out, float* lse_out, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * rapid_kv_append_rope: rapid_kv_append with the rotary position embedding on the way.  Row i (0 <= i <= gamma_b) of k_new, rotated, and
+ * of v_new becomes token ctx_lens[b] - (gamma_b+1) + i of sequence b's cache, and row i of q_new, rotated, becomes row i of q_out.  With
+ * t = pos * inv_freq[c] the pair (x, y) of elements that belongs to c < rotary_dim / 2 turns into
+ *     amplitude * (x cos t - y sin t),  amplitude * (y cos t + x sin t)
+ * computed in fp32 from an angle that is reduced in 64 bits, and rounded to bf16 once; elements from rotary_dim on are copied.
+ * Rows i > gamma_b, rows whose token would be negative, and all other elements are left untouched.
+ *   q_new         bf16 or NULL (then q_out is NULL too): keys and values alone.  Row (b, i) at (b * q_max + i) * q_stride, heads side by side, 16-byte
+ *                 aligned; k_new and v_new likewise with their strides, so that all three may be slices of one projection's output
+ *   inv_freq      fp32 [rotary_dim / 2], the model's frequencies with whatever scaling it applies to them
+ *   positions     int32 [B, q_max] or NULL: a row's position is then its token, ctx_lens[b] - (gamma_b+1) + i (behind a shared prefix, say,
+ *                 or in chunks that keep their places in a document, it is not)
+ *   q_out         bf16 [B, q_max, Hq, d], contiguous; may be q_new where that is contiguous too
+ *   shape         as for rapid_verify_attn; q_max may be anything up to max_ctx (a whole prompt), softmax_scale is > 0 and not used otherwise
+ *
+ * rapid_kv_append_rope_quant: the same into a cache in 8 bits: what is quantised is the rotated row in bf16, so that the cache is what
+ * rapid_kv_append_quant leaves of such rows.  Shape and layout as for that call.
+ */
+typedef struct rapid_rope {
+    int32_t rotary_dim;       /* elements of a head that are rotated: a multiple of 16, at most head_dim       */
+    int32_t interleaved;      /* 0: c is paired with c + rotary_dim / 2;  1: 2c with 2c + 1                    */
+    float   amplitude;        /* factor on cos and sin, finite (1 unless the model's scaling has one)          */
+    int64_t q_stride;         /* elements from one row to the next: a multiple of 8, at least heads * head_dim */
+    int64_t k_stride;
+    int64_t v_stride;
+} rapid_rope;
+int rapid_kv_append_rope(rapid_ctx* ctx, const rapid_attn_shape* shape, const rapid_rope* rope,
+                         const void* q_new, const void* k_new, const void* v_new, const float* inv_freq, const int32_t* positions,
+                         const int32_t* ctx_lens, const int32_t* gammas, const int32_t* page_table,
+                         void* q_out, void* k_cache, void* v_cache, void* stream);
+int rapid_kv_append_rope_quant(rapid_ctx* ctx, const rapid_attn_shape* shape, const rapid_quant_layout* layout, const rapid_rope* rope,
+                               const void* q_new, const void* k_new, const void* v_new, const float* inv_freq, const int32_t* positions,
+                               const int32_t* ctx_lens, const int32_t* gammas, const int32_t* page_table,
+                               void* q_out, void* k_codes, void* v_codes, void* k_scales, void* v_scales, void* stream);
 
 /*
  * Verification attention of a batch whose sequences share one prefix (several requests, or several drafts, about one long

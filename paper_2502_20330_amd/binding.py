@@ -27,6 +27,8 @@ EXPORTS = ["rapid_create", "rapid_destroy", "rapid_strerror", "rapid_last_hip_er
            "rapid_kv_commit_pages",
            "rapid_kv_append_quant", "rapid_kv_read_quant", "rapid_verify_attn_quant", "rapid_verify_attn_quant_workspace_bytes",
            "rapid_verify_attn_prefix", "rapid_verify_attn_prefix_workspace_bytes",
+           "rapid_kv_append_rope", "rapid_kv_append_rope_quant", "rapid_quant_rows", "rapid_lm_head_quant",
+           "rapid_lm_head_quant_workspace_bytes",
            "rapid_retrieve", "rapid_hbm_read_probe"]
 
 
@@ -58,6 +60,12 @@ class PrefixLayout(ctypes.Structure):
     """Mirror of ``rapid_prefix_layout`` in include/rapid.h."""
     _fields_ = [("max_prefix", ctypes.c_int32), ("max_pages", ctypes.c_int32), ("token_stride", ctypes.c_int64),
                 ("head_stride", ctypes.c_int64)]
+
+
+class Rope(ctypes.Structure):
+    """Mirror of ``rapid_rope`` in include/rapid.h."""
+    _fields_ = [("rotary_dim", ctypes.c_int32), ("interleaved", ctypes.c_int32), ("amplitude", ctypes.c_float),
+                ("q_stride", ctypes.c_int64), ("k_stride", ctypes.c_int64), ("v_stride", ctypes.c_int64)]
 
 
 _lib = None
@@ -140,6 +148,19 @@ def load_library() -> ctypes.CDLL:
     lib.rapid_verify_attn_prefix.argtypes = [vp, shape_p, prefix_p, vp, vp, vp, i32p, i32p, vp, vp, i32p, i32p, i32p, vp, f32p,
                                              vp, ctypes.c_size_t, vp]
     lib.rapid_verify_attn_prefix.restype = ctypes.c_int
+    rope_p = ctypes.POINTER(Rope)
+    lib.rapid_kv_append_rope.argtypes = [vp, shape_p, rope_p, vp, vp, vp, f32p, i32p, i32p, i32p, i32p, vp, vp, vp, vp]
+    lib.rapid_kv_append_rope.restype = ctypes.c_int
+    lib.rapid_kv_append_rope_quant.argtypes = [vp, shape_p, quant_p, rope_p, vp, vp, vp, f32p, i32p, i32p, i32p, i32p, vp, vp, vp, vp, vp,
+                                               vp]
+    lib.rapid_kv_append_rope_quant.restype = ctypes.c_int
+    lib.rapid_quant_rows.argtypes = [vp, ctypes.c_int64, ctypes.c_int, vp, ctypes.c_int64, vp, f32p, vp]
+    lib.rapid_quant_rows.restype = ctypes.c_int
+    lib.rapid_lm_head_quant_workspace_bytes.argtypes = [vp, ctypes.c_int, ctypes.c_int]
+    lib.rapid_lm_head_quant_workspace_bytes.restype = ctypes.c_size_t
+    lib.rapid_lm_head_quant.argtypes = [vp, ctypes.c_int, ctypes.c_int, ctypes.c_int, vp, vp, f32p, ctypes.c_float, f32p, ctypes.c_int64,
+                                        f32p, vp, ctypes.c_size_t, vp]
+    lib.rapid_lm_head_quant.restype = ctypes.c_int
     lib.rapid_retrieve.argtypes = [ctypes.c_void_p, ctypes.c_int, ctypes.c_int, f32p, f32p, ctypes.c_int, ctypes.c_float,
                                    f32p, i32p, i32p, vp]
     lib.rapid_retrieve.restype = ctypes.c_int
@@ -615,16 +636,9 @@ class Rapid:
                    "k_cache and v_cache: bf16 [B or pages, tokens, Hkv, d], d contiguous, the same sizes and strides")
         self._need(k_cache.shape[3] == q.shape[3], "q and the cache differ in head_dim")
         self._need(prefix_len.dtype == torch.int32 and prefix_len.numel() == 1, "prefix_len: int32 [1]")
-        (rows, tokens, hkv, d), st = k_cache.shape, _strides(k_cache)
-        gamma = q.shape[1] - 1 if gamma is None else int(gamma)
+        tokens, hkv, d = k_cache.shape[1:]
         scale = d ** -0.5 if softmax_scale is None else float(softmax_scale)
-        if page_table is None:
-            ctx_max = tokens if max_ctx is None else int(max_ctx)
-            self._need(rows == q.shape[0] and ctx_max <= tokens, "the cache holds fewer sequences or tokens than the call names")
-            shape = AttnShape(*q.shape[:3], hkv, d, ctx_max, gamma, scale, st[0], st[1], st[2], 0, 0, 0, 0, 0, 0)
-        else:
-            ctx_max = page_table.shape[1] * tokens if max_ctx is None else int(max_ctx)
-            shape = AttnShape(*q.shape[:3], hkv, d, ctx_max, gamma, scale, 0, st[1], st[2], st[0], tokens, page_table.shape[1], 0, rows, 0)
+        shape = self._cache_shape(*q.shape[:3], k_cache, gamma, page_table, max_ctx, scale)
         if prefix_table is not None:
             self._need(page_table is not None and k_prefix is None and v_prefix is None,
                        "prefix_table names pages of a paged cache, in the place of k_prefix and v_prefix")
@@ -640,6 +654,94 @@ class Rapid:
         n = k_prefix.shape[0]
         self._need(max_prefix is None or max_prefix <= n, "the prefix holds fewer tokens than max_prefix")
         return ctypes.byref(shape), ctypes.byref(PrefixLayout(n if max_prefix is None else int(max_prefix), 0, sp[1], sp[2]))
+
+    # ------------------------------------------------------------------ append with rotary positions
+    def rapid_kv_append_rope(self, k_cache, v_cache, k_new, v_new, inv_freq, ctx_lens, gamma: Optional[int] = None, *, q_new=None,
+                             q_out=None, positions=None, interleaved: bool = False, amplitude: float = 1.0, gammas=None, page_table=None,
+                             max_ctx: Optional[int] = None):
+        """:meth:`rapid_kv_append` with the rotary positions on the way: rows 0..gamma_b of k_new (rotated) and v_new become the last
+        gamma_b+1 tokens of every sequence; the same rows of q_new, rotated, are written to q_out, which is returned (bf16
+        [B,Qmax,Hq,d]; made here where q_new is given and q_out is not; may be q_new).  q_new/k_new/v_new: bf16 [B,Qmax,heads,d],
+        heads side by side, rows any distance apart, so that they may be slices of one projection's output.  inv_freq: fp32
+        [rotary_dim/2]; positions: int32 [B,Qmax], by default a row's token.  Cache layout as for rapid_verify_attn."""
+        if q_out is None and q_new is not None:
+            q_out = torch.empty(q_new.shape, dtype=torch.bfloat16, device=self.device)
+        key = ("rope", gamma, max_ctx, interleaved, amplitude,
+               *_sizes(k_cache, v_cache, k_new, v_new, inv_freq, ctx_lens, q_new, q_out, positions, gammas, page_table))
+        shape, rope = self._plans.get(key) or self._planned(
+            key, self._plan_rope, k_cache, v_cache, None, None, k_new, v_new, inv_freq, ctx_lens, q_new, q_out, positions, gammas, page_table,
+            gamma, max_ctx, interleaved, amplitude)
+        rc = self.lib.rapid_kv_append_rope(self._ctx, shape, rope, _dptr(q_new), k_new.data_ptr(), v_new.data_ptr(), inv_freq.data_ptr(),
+                                           _dptr(positions), ctx_lens.data_ptr(), _dptr(gammas), _dptr(page_table), _dptr(q_out),
+                                           k_cache.data_ptr(), v_cache.data_ptr(), _stream_ptr(self.device))
+        if rc:
+            _check(self.lib, rc, self._ctx)
+        return q_out
+
+    def rapid_kv_append_rope_quant(self, k_codes, v_codes, k_scales, v_scales, k_new, v_new, inv_freq, ctx_lens,
+                                   gamma: Optional[int] = None, *, q_new=None, q_out=None, positions=None, interleaved: bool = False,
+                                   amplitude: float = 1.0, gammas=None, page_table=None, max_ctx: Optional[int] = None):
+        """:meth:`rapid_kv_append_rope` into a cache in 8 bits (layout: :meth:`rapid_kv_append_quant`)."""
+        if q_out is None and q_new is not None:
+            q_out = torch.empty(q_new.shape, dtype=torch.bfloat16, device=self.device)
+        key = ("rope_quant", gamma, max_ctx, interleaved, amplitude,
+               *_sizes(k_codes, v_codes, k_scales, v_scales, k_new, v_new, inv_freq, ctx_lens, q_new, q_out, positions, gammas, page_table))
+        shape, layout, rope = self._plans.get(key) or self._planned(
+            key, self._plan_rope, k_codes, v_codes, k_scales, v_scales, k_new, v_new, inv_freq, ctx_lens, q_new, q_out, positions, gammas,
+            page_table, gamma, max_ctx, interleaved, amplitude)
+        rc = self.lib.rapid_kv_append_rope_quant(self._ctx, shape, layout, rope, _dptr(q_new), k_new.data_ptr(), v_new.data_ptr(),
+                                                 inv_freq.data_ptr(), _dptr(positions), ctx_lens.data_ptr(), _dptr(gammas), _dptr(page_table),
+                                                 _dptr(q_out), k_codes.data_ptr(), v_codes.data_ptr(), k_scales.data_ptr(),
+                                                 v_scales.data_ptr(), _stream_ptr(self.device))
+        if rc:
+            _check(self.lib, rc, self._ctx)
+        return q_out
+
+    def _row_stride(self, t, name: str) -> int:
+        """Elements from one row (sequence, position) of t [B, Qmax, heads, d] to the next."""
+        B, Q, heads, d = t.shape
+        s0, s1, s2, s3 = t.stride()
+        row = s1 if Q > 1 else s0 if B > 1 else heads * d
+        self._need((s3 == 1 or d == 1) and (s2 == d or heads == 1) and (Q == 1 or B == 1 or s0 == Q * s1),
+                   f"{name}: heads side by side, rows the same distance apart")
+        return row
+
+    def _plan_rope(self, k_cache, v_cache, k_scales, v_scales, k_new, v_new, inv_freq, ctx_lens, q_new, q_out, positions, gammas, page_table,
+                   gamma, max_ctx, interleaved, amplitude):
+        news = [(t, name) for t, name in ((q_new, "q_new"), (k_new, "k_new"), (v_new, "v_new")) if t is not None]
+        self._need(all(t.dtype == torch.bfloat16 and t.dim() == 4 for t, _ in news), "q_new, k_new and v_new: bf16 [B, Qmax, heads, d]")
+        B, Q, hkv, d = k_new.shape
+        self._need(v_new.shape == k_new.shape and k_cache.dim() == 4 and k_cache.shape[2:] == k_new.shape[2:],
+                   "k_new, v_new and the cache differ in heads or head_dim")
+        self._need(inv_freq.dtype == torch.float32 and inv_freq.dim() == 1 and inv_freq.is_contiguous(), "inv_freq: fp32 [rotary_dim / 2]")
+        self._need(positions is None or (positions.dtype == torch.int32 and positions.shape == (B, Q) and positions.is_contiguous()),
+                   "positions: int32 [B, Qmax], contiguous")
+        self._need((q_new is None) == (q_out is None), "q_out goes with q_new")
+        hq = hkv
+        if q_new is not None:
+            hq = q_new.shape[2]
+            self._need(q_new.shape == (B, Q, hq, d), "q_new: as many sequences, positions and elements a head as k_new")
+            self._need(q_out.dtype == torch.bfloat16 and q_out.shape == q_new.shape and q_out.is_contiguous(), "q_out: bf16 like q_new, contiguous")
+        self._check_lengths(B, ctx_lens, gammas, page_table)
+        strides = [self._row_stride(t, name) for t, name in news]
+        rope = Rope(2 * inv_freq.numel(), int(bool(interleaved)), float(amplitude), *([0] if q_new is None else []), *strides)
+        if k_scales is not None:
+            return (*self._quant_shape(B, Q, hq, gamma, k_cache, v_cache, k_scales, v_scales, page_table, max_ctx, 1.0), ctypes.byref(rope))
+        self._need(k_cache.dtype == torch.bfloat16 and v_cache.dtype == torch.bfloat16 and k_cache.shape == v_cache.shape
+                   and _strides(k_cache) == _strides(v_cache) and k_cache.stride(3) == 1,
+                   "k_cache and v_cache: bf16 [B or pages, tokens, Hkv, d], d contiguous, the same sizes and strides")
+        return ctypes.byref(self._cache_shape(B, Q, hq, k_cache, gamma, page_table, max_ctx, 1.0)), ctypes.byref(rope)
+
+    def _cache_shape(self, batch, q_max, hq, k_cache, gamma, page_table, max_ctx, scale) -> AttnShape:
+        """Of a bf16 cache [B or pages, tokens, Hkv, d]."""
+        (rows, tokens, hkv, d), st = k_cache.shape, _strides(k_cache)
+        gamma = q_max - 1 if gamma is None else int(gamma)
+        if page_table is None:
+            ctx_max = tokens if max_ctx is None else int(max_ctx)
+            self._need(rows == batch and ctx_max <= tokens, "the cache holds fewer sequences or tokens than the call names")
+            return AttnShape(batch, q_max, hq, hkv, d, ctx_max, gamma, scale, st[0], st[1], st[2], 0, 0, 0, 0, 0, 0)
+        ctx_max = page_table.shape[1] * tokens if max_ctx is None else int(max_ctx)
+        return AttnShape(batch, q_max, hq, hkv, d, ctx_max, gamma, scale, 0, st[1], st[2], st[0], tokens, page_table.shape[1], 0, rows, 0)
 
     # ------------------------------------------------------------------ retrieval
     def rapid_retrieve(self, chunk_emb, query_emb, top_k: int, threshold: float = 0.3):
@@ -679,6 +781,66 @@ class Rapid:
                                     _dptr(stats) if want_stats else None, _stream_ptr(self.device))
         _check(self.lib, rc, self._ctx)
         return logits, (stats if want_stats else None)
+
+    def rapid_quant_rows(self, x, codes=None, scales=None):
+        """Rows of x (bf16 [rows, cols], any row stride) as 8-bit integers: (codes int8 [rows, pitch], scales fp32 [rows]), pitch = cols
+        rounded up to a multiple of 256 (zeros behind the row): what :meth:`rapid_lm_head_quant` takes for an output embedding."""
+        self._need(x.dim() == 2 and x.dtype == torch.bfloat16 and (x.stride(1) == 1 or x.shape[1] == 1), "x: bf16 [rows, cols], cols contiguous")
+        rows, cols = x.shape
+        pitch = -(-cols // 256) * 256
+        if codes is None:
+            codes = torch.empty((rows, pitch), dtype=torch.int8, device=self.device)
+        if scales is None:
+            scales = torch.empty(rows, dtype=torch.float32, device=self.device)
+        self._need(codes.dtype == torch.int8 and codes.shape == (rows, pitch) and codes.is_contiguous(),
+                   "codes: int8 [rows, cols rounded up to a multiple of 256], contiguous")
+        self._need(scales.dtype == torch.float32 and scales.shape == (rows,) and scales.is_contiguous(), "scales: fp32 [rows], contiguous")
+        self._need(x.device == codes.device == scales.device == self.device, f"a tensor is not on {self.device}")
+        rc = self.lib.rapid_quant_rows(self._ctx, rows, cols, x.data_ptr(), x.stride(0) if rows > 1 else cols, codes.data_ptr(),
+                                       scales.data_ptr(), _stream_ptr(self.device))
+        if rc:
+            _check(self.lib, rc, self._ctx)
+        return codes, scales
+
+    def rapid_lm_head_quant(self, h, w_codes, w_scales, *, temperature: float = 1.0, want_stats: bool = True, logits=None, stats=None):
+        """:meth:`rapid_lm_head` on an output embedding in 8-bit integers (:meth:`rapid_quant_rows` of it): h bf16 [rows, hidden], w_codes
+        int8 [vocab, pitch], w_scales fp32 [vocab] -> (logits fp32 [rows, vocab], stats fp32 [rows, chunks, 2] or None).  Streams and
+        graphs as for :meth:`rapid_verify_attn_quant`."""
+        self._need(h.dim() == 2 and w_codes.dim() == 2, "h [rows, hidden], w_codes [vocab, pitch]")
+        (rows, hidden), (vocab, pitch) = h.shape, w_codes.shape
+        if logits is None:
+            logits = torch.empty((rows, vocab), dtype=torch.float32, device=self.device)
+        if not want_stats:
+            stats = None
+        elif stats is None:
+            stats = torch.empty((rows, self.lib.rapid_lm_head_stat_chunks(self._ctx, vocab, rows), 2), dtype=torch.float32,
+                                device=self.device)
+        key = ("head", *_sizes(h, w_codes, w_scales, logits, stats))
+        ldz = self._plans.get(key) or self._planned(key, self._plan_head, h, w_codes, w_scales, logits, stats)
+        args = (self._ctx, rows, hidden, vocab, h.data_ptr(), w_codes.data_ptr(), w_scales.data_ptr(), float(temperature), logits.data_ptr(),
+                ldz, _dptr(stats))
+        call, stream = self.lib.rapid_lm_head_quant, _stream_ptr(self.device)
+        rc = call(*args, *self._stream_workspace(stream), stream)
+        if rc == RAPID_EWORKSPACE:                             # the last check of the call: nothing has been launched
+            ws = self._new_workspace(stream, self.lib.rapid_lm_head_quant_workspace_bytes(self._ctx, rows, hidden))
+            rc = call(*args, ws.data_ptr(), ws.numel(), stream)
+        if rc:
+            _check(self.lib, rc, self._ctx)
+        return logits, stats
+
+    def _plan_head(self, h, w_codes, w_scales, logits, stats):
+        """The distance of the logits' rows."""
+        (rows, hidden), (vocab, pitch) = h.shape, w_codes.shape
+        self._need(h.dtype == torch.bfloat16 and h.is_contiguous(), "h: bf16 [rows, hidden], contiguous")
+        self._need(w_codes.dtype == torch.int8 and w_codes.is_contiguous() and pitch == -(-hidden // 256) * 256,
+                   "w_codes: int8 [vocab, hidden rounded up to a multiple of 256], contiguous")
+        self._need(w_scales.dtype == torch.float32 and w_scales.shape == (vocab,) and w_scales.is_contiguous(), "w_scales: fp32 [vocab], contiguous")
+        self._need(logits.dtype == torch.float32 and logits.shape == (rows, vocab) and (logits.stride(1) == 1 or vocab == 1),
+                   "logits: fp32 [rows, vocab], vocab contiguous")
+        self._need(stats is None or (stats.dtype == torch.float32 and stats.is_contiguous() and
+                                     stats.shape == (rows, self.lib.rapid_lm_head_stat_chunks(self._ctx, vocab, rows), 2)),
+                   "stats: fp32 [rows, chunks, 2], contiguous")
+        return logits.stride(0) if rows > 1 else vocab
 
     # ------------------------------------------------------------------ measurement aid
     def rapid_hbm_read_probe(self, buf: torch.Tensor, nbytes: Optional[int] = None):
@@ -725,3 +887,8 @@ def rapid_verify_attn_quant(q, k_codes, v_codes, k_scales, v_scales, ctx_lens, g
 def rapid_verify_attn_prefix(q, k_cache, v_cache, ctx_lens, prefix_len, gamma=None, **kw):
     """Module-level form of :meth:`Rapid.rapid_verify_attn_prefix` on the tensors' device."""
     return _get(q.device.index or 0).rapid_verify_attn_prefix(q, k_cache, v_cache, ctx_lens, prefix_len, gamma, **kw)
+
+
+def rapid_lm_head_quant(h, w_codes, w_scales, **kw):
+    """Module-level form of :meth:`Rapid.rapid_lm_head_quant` on the tensors' device."""
+    return _get(h.device.index or 0).rapid_lm_head_quant(h, w_codes, w_scales, **kw)

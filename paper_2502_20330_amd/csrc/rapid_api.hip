@@ -51,7 +51,8 @@ int hip_fail(rapid_ctx* ctx, hipError_t e)
     return RAPID_EHIP;
 }
 
-int check_attn_shape(const rapid_attn_shape* s)
+// `few`: a call that packs all rows of a sequence and kv head, and addresses q with 32 bits.
+int check_attn_shape(const rapid_attn_shape* s, bool few = true)
 {
     if (!s) return RAPID_EINVAL;
     if (s->batch < 1 || s->q_max < 1 || s->n_q_heads < 1 || s->n_kv_heads < 1 || s->max_ctx < 1) return RAPID_EINVAL;
@@ -62,7 +63,7 @@ int check_attn_shape(const rapid_attn_shape* s)
     if (s->head_dim != 64 && s->head_dim != 128) return RAPID_EUNSUPPORTED;
     if (s->batch > 65535) return RAPID_EUNSUPPORTED;                       // grid z dimension
     const int G = s->n_q_heads / s->n_kv_heads;
-    if ((int64_t)s->q_max * G > 96) return RAPID_EUNSUPPORTED;
+    if (few && (int64_t)s->q_max * G > 96) return RAPID_EUNSUPPORTED;
     if (s->page_size != 0) {
         if (s->page_size < 16 || (s->page_size & (s->page_size - 1))) return RAPID_EUNSUPPORTED;
         if (s->max_pages < 1 || (int64_t)s->max_pages * s->page_size < s->max_ctx) return RAPID_EINVAL;
@@ -75,7 +76,7 @@ int check_attn_shape(const rapid_attn_shape* s)
     const int64_t span_tokens = s->page_size ? s->page_size : s->max_ctx;
     if (s->kv_token_stride > (((int64_t)1 << 31) - 1) / span_tokens) return RAPID_EUNSUPPORTED;
     // and so are the rows of q
-    if ((int64_t)s->batch * s->q_max * s->n_q_heads * s->head_dim * 2 >= (int64_t)1 << 32) return RAPID_EUNSUPPORTED;
+    if (few && (int64_t)s->batch * s->q_max * s->n_q_heads * s->head_dim * 2 >= (int64_t)1 << 32) return RAPID_EUNSUPPORTED;
     return RAPID_OK;
 }
 
@@ -278,6 +279,35 @@ int check_quant_layout(const rapid_attn_shape* s, const rapid_quant_layout* l)
     return RAPID_OK;
 }
 
+// The new rows and the rotation of an append.  Grid dimensions bound the batch and the parts of the heads.
+int check_rope(const rapid_attn_shape* s, const rapid_rope* r, bool queries)
+{
+    if (!r) return RAPID_EINVAL;
+    if (!(r->amplitude - r->amplitude == 0.f) || (r->interleaved != 0 && r->interleaved != 1)) return RAPID_EINVAL;
+    if (r->rotary_dim < 16 || r->rotary_dim > s->head_dim || r->rotary_dim % 16) return RAPID_EUNSUPPORTED;
+    if (s->batch > 65535 || (queries ? (int64_t)s->n_q_heads : 0) + 2 * (int64_t)s->n_kv_heads > 1 << 16) return RAPID_EUNSUPPORTED;
+    const int64_t q_row = (int64_t)s->n_q_heads * s->head_dim, kv_row = (int64_t)s->n_kv_heads * s->head_dim;
+    if ((queries && (r->q_stride < q_row || r->q_stride % 8)) || r->k_stride < kv_row || r->k_stride % 8 || r->v_stride < kv_row ||
+        r->v_stride % 8) return RAPID_EALIGN;
+    return RAPID_OK;
+}
+
+// ---- rows of 8-bit integers
+constexpr int kMaxQuantCols = 1 << 17;            // 127^2 times as many stays below 2^31
+int quant_pitch(int cols) { return (cols + 255) / 256 * 256; }
+QuantRowsLaunch quant_rows_of(int64_t rows, int cols, const void* x, int64_t stride, void* codes, float* scales)
+{
+    QuantRowsLaunch a{};
+    a.x = static_cast<const uint16_t*>(x);
+    a.codes = static_cast<int8_t*>(codes);
+    a.scales = scales;
+    a.rows = rows;
+    a.stride = stride;
+    a.cols = cols;
+    a.pitch = quant_pitch(cols);
+    return a;
+}
+
 AttnSource source_of(const rapid_attn_shape* s, const void* k, const void* v, const int32_t* page_table)
 {
     AttnSource r{};
@@ -393,6 +423,7 @@ int rapid_create(rapid_ctx** out, int device)
     if ((e = hipSetDevice(device)) != hipSuccess) return RAPID_EHIP;
     hipError_t ec = configure_verify_attn();
     if (ec == hipSuccess) ec = configure_lm_head();
+    if (ec == hipSuccess) ec = configure_lm_head_quant();
     if (ec == hipSuccess) ec = configure_attn_stream();
     if (ec == hipSuccess) ec = configure_attn_prefix();
     if (ec == hipSuccess) ec = configure_hbm_read_probe();
@@ -707,12 +738,13 @@ int rapid_lm_head(rapid_ctx* ctx, int n_rows, int hidden, int vocab,
     if (n_rows > 96 || hidden % 128 || vocab < 16) return RAPID_EUNSUPPORTED;
     if (!aligned(h, 16) || !aligned(w, 16) || !aligned(logits, 4) || !aligned(stats, 8)) return RAPID_EALIGN;
     LmHeadLaunch a{};
-    a.h = static_cast<const uint16_t*>(h);
-    a.w = static_cast<const uint16_t*>(w);
+    a.h = h;
+    a.w = w;
     a.logits = logits;
     a.stats = stats;
     a.n_rows = n_rows;
     a.hidden = hidden;
+    a.row_bytes = hidden * 2;
     a.vocab = vocab;
     a.ldz = logits_row_stride;
     a.nb = lm_head_blocks(ctx, vocab, n_rows);
@@ -720,6 +752,64 @@ int rapid_lm_head(rapid_ctx* ctx, int n_rows, int hidden, int vocab,
     DeviceScope dev(ctx->device);
     if (dev.err != hipSuccess) return hip_fail(ctx, dev.err);
     hipError_t e = launch_lm_head(a, static_cast<hipStream_t>(stream));
+    if (e != hipSuccess) return hip_fail(ctx, e);
+    return RAPID_OK;
+}
+
+int rapid_quant_rows(rapid_ctx* ctx, int64_t rows, int cols, const void* x, int64_t row_stride, void* codes, float* scales,
+                     void* stream)
+{
+    if (!ctx || !x || !codes || !scales) return RAPID_EINVAL;
+    if (rows < 1 || cols < 1 || row_stride < cols) return RAPID_EINVAL;
+    if (rows > 0x7fffffff || cols > kMaxQuantCols || cols % 8) return RAPID_EUNSUPPORTED;
+    if (!aligned(x, 16) || !aligned(codes, 16) || !aligned(scales, 4) || row_stride % 8) return RAPID_EALIGN;
+    const QuantRowsLaunch a = quant_rows_of(rows, cols, x, row_stride, codes, scales);
+    DeviceScope dev(ctx->device);
+    if (dev.err != hipSuccess) return hip_fail(ctx, dev.err);
+    hipError_t e = launch_quant_rows(a, static_cast<hipStream_t>(stream));
+    if (e != hipSuccess) return hip_fail(ctx, e);
+    return RAPID_OK;
+}
+
+// The codes of h, and behind them their scales.
+static size_t head_codes_bytes(int n_rows, int hidden) { return (size_t)n_rows * quant_pitch(hidden); }
+
+size_t rapid_lm_head_quant_workspace_bytes(const rapid_ctx*, int n_rows, int hidden)
+{
+    if (n_rows < 1 || n_rows > 96 || hidden < 1 || hidden > kMaxQuantCols || hidden % 8) return 0;
+    return head_codes_bytes(n_rows, hidden) + (size_t)n_rows * 4;
+}
+
+int rapid_lm_head_quant(rapid_ctx* ctx, int n_rows, int hidden, int vocab,
+                        const void* h, const void* w_codes, const float* w_scales, float temperature,
+                        float* logits, int64_t logits_row_stride, float* stats,
+                        void* workspace, size_t workspace_bytes, void* stream)
+{
+    if (!ctx || !h || !w_codes || !w_scales || !logits) return RAPID_EINVAL;
+    if (n_rows < 1 || hidden < 1 || vocab < 1 || logits_row_stride < vocab || !(temperature > 0.f)) return RAPID_EINVAL;
+    if (n_rows > 96 || hidden > kMaxQuantCols || hidden % 8 || vocab < 16) return RAPID_EUNSUPPORTED;
+    if (!aligned(h, 16) || !aligned(w_codes, 16) || !aligned(w_scales, 4) || !aligned(logits, 4) || !aligned(stats, 8)) return RAPID_EALIGN;
+    if (!workspace || !aligned(workspace, 256) || workspace_bytes < rapid_lm_head_quant_workspace_bytes(ctx, n_rows, hidden))
+        return RAPID_EWORKSPACE;
+    LmHeadLaunch a{};
+    a.h = workspace;
+    a.h_scales = reinterpret_cast<const float*>(static_cast<char*>(workspace) + head_codes_bytes(n_rows, hidden));
+    a.w = w_codes;
+    a.w_scales = w_scales;
+    a.logits = logits;
+    a.stats = stats;
+    a.n_rows = n_rows;
+    a.hidden = hidden;
+    a.row_bytes = quant_pitch(hidden);
+    a.vocab = vocab;
+    a.ldz = logits_row_stride;
+    a.nb = lm_head_blocks(ctx, vocab, n_rows);
+    a.inv_T = (float)(1.0 / (double)temperature);
+    const QuantRowsLaunch rows = quant_rows_of(n_rows, hidden, h, hidden, workspace, const_cast<float*>(a.h_scales));
+    DeviceScope dev(ctx->device);
+    if (dev.err != hipSuccess) return hip_fail(ctx, dev.err);
+    hipError_t e = launch_quant_rows(rows, static_cast<hipStream_t>(stream));
+    if (e == hipSuccess) e = launch_lm_head_quant(a, static_cast<hipStream_t>(stream));
     if (e != hipSuccess) return hip_fail(ctx, e);
     return RAPID_OK;
 }
@@ -813,6 +903,91 @@ int rapid_kv_commit_pages(rapid_ctx* ctx, const rapid_attn_shape* shape, const i
     return RAPID_OK;
 }
 
+// Where the rows of a cache lie; without a layout of scales it is bf16, and its strides become bytes.
+static void bind_quant_shape(KvQuantLaunch& a, const rapid_attn_shape* shape, const rapid_quant_layout* layout,
+                             const int32_t* ctx_lens, const int32_t* gammas, const int32_t* page_table)
+{
+    const int64_t bytes = layout ? 1 : 2;
+    a.ctx_lens = ctx_lens;
+    a.gammas = gammas;
+    a.page_table = shape->page_size ? page_table : nullptr;
+    a.B = shape->batch;
+    a.Qmax = shape->q_max;
+    a.Hkv = shape->n_kv_heads;
+    a.D = shape->head_dim;
+    a.gamma = shape->gamma;
+    a.max_ctx = shape->max_ctx;
+    a.bstride = shape->kv_batch_stride * bytes;
+    a.tstride = shape->kv_token_stride * bytes;
+    a.hstride = shape->kv_head_stride * bytes;
+    a.pstride = shape->kv_page_stride * bytes;
+    a.sbstride = layout ? layout->scale_batch_stride : 0;
+    a.shstride = layout ? layout->scale_head_stride : 0;
+    a.spstride = layout ? layout->scale_page_stride : 0;
+    a.page_shift = page_shift_of(shape);
+    a.page_mask = shape->page_size ? shape->page_size - 1 : 0;
+    a.max_pages = shape->max_pages;
+    a.page_hi = page_hi_of(shape);
+}
+
+static int rope_call(rapid_ctx* ctx, const rapid_attn_shape* shape, bool quant, const rapid_quant_layout* layout, const rapid_rope* rope,
+                     const void* q_new, const void* k_new, const void* v_new, const float* inv_freq, const int32_t* positions,
+                     const int32_t* ctx_lens, const int32_t* gammas, const int32_t* page_table,
+                     void* q_out, void* k_cache, void* v_cache, void* k_scales, void* v_scales, void* stream)
+{
+    if (!ctx) return RAPID_EINVAL;
+    int rc = quant ? check_quant_shape(shape, false) : check_attn_shape(shape, false);
+    if (rc == RAPID_OK && quant) rc = check_quant_layout(shape, layout);
+    if (rc == RAPID_OK) rc = check_rope(shape, rope, q_new != nullptr);
+    if (rc != RAPID_OK) return rc;
+    if (!k_new || !v_new || !inv_freq || !ctx_lens || !k_cache || !v_cache || !q_new != !q_out) return RAPID_EINVAL;
+    if (quant && (!k_scales || !v_scales)) return RAPID_EINVAL;
+    if (shape->page_size != 0 && !page_table) return RAPID_EINVAL;
+    if (!aligned(q_new, 16) || !aligned(k_new, 16) || !aligned(v_new, 16) || !aligned(q_out, 16) || !aligned(k_cache, 16) ||
+        !aligned(v_cache, 16) || !aligned(k_scales, 16) || !aligned(v_scales, 16) || !aligned(inv_freq, 4) || !aligned(positions, 4))
+        return RAPID_EALIGN;
+    KvRopeLaunch a{};
+    a.q = static_cast<const uint16_t*>(q_new);
+    a.k = static_cast<const uint16_t*>(k_new);
+    a.v = static_cast<const uint16_t*>(v_new);
+    a.q_out = static_cast<uint16_t*>(q_out);
+    a.inv_freq = inv_freq;
+    a.positions = positions;
+    a.q_stride = rope->q_stride;
+    a.k_stride = rope->k_stride;
+    a.v_stride = rope->v_stride;
+    a.Hq = q_new ? shape->n_q_heads : 0;
+    a.rot = rope->rotary_dim;
+    a.adjacent = rope->interleaved;
+    a.amplitude = rope->amplitude;
+    a.cache.side[0] = KvQuantSide{nullptr, static_cast<uint8_t*>(k_cache), static_cast<uint8_t*>(k_scales)};
+    a.cache.side[1] = KvQuantSide{nullptr, static_cast<uint8_t*>(v_cache), static_cast<uint8_t*>(v_scales)};
+    bind_quant_shape(a.cache, shape, layout, ctx_lens, gammas, page_table);
+    DeviceScope dev(ctx->device);
+    if (dev.err != hipSuccess) return hip_fail(ctx, dev.err);
+    hipError_t e = launch_kv_append_rope(a, static_cast<hipStream_t>(stream));
+    if (e != hipSuccess) return hip_fail(ctx, e);
+    return RAPID_OK;
+}
+
+int rapid_kv_append_rope(rapid_ctx* ctx, const rapid_attn_shape* shape, const rapid_rope* rope,
+                         const void* q_new, const void* k_new, const void* v_new, const float* inv_freq, const int32_t* positions,
+                         const int32_t* ctx_lens, const int32_t* gammas, const int32_t* page_table,
+                         void* q_out, void* k_cache, void* v_cache, void* stream)
+{
+    return rope_call(ctx, shape, false, nullptr, rope, q_new, k_new, v_new, inv_freq, positions, ctx_lens, gammas, page_table, q_out,
+                     k_cache, v_cache, nullptr, nullptr, stream);
+}
+
+int rapid_kv_append_rope_quant(rapid_ctx* ctx, const rapid_attn_shape* shape, const rapid_quant_layout* layout, const rapid_rope* rope,
+                               const void* q_new, const void* k_new, const void* v_new, const float* inv_freq, const int32_t* positions,
+                               const int32_t* ctx_lens, const int32_t* gammas, const int32_t* page_table,
+                               void* q_out, void* k_codes, void* v_codes, void* k_scales, void* v_scales, void* stream)
+{
+    return rope_call(ctx, shape, true, layout, rope, q_new, k_new, v_new, inv_freq, positions, ctx_lens, gammas, page_table, q_out,
+                     k_codes, v_codes, k_scales, v_scales, stream);
+}
+
 static int quant_rows_call(rapid_ctx* ctx, const rapid_attn_shape* shape, const rapid_quant_layout* layout, bool append,
                            const void* k_rows, const void* v_rows, const void* k_codes, const void* v_codes,
                            const void* k_scales, const void* v_scales,
@@ -834,26 +1009,7 @@ static int quant_rows_call(rapid_ctx* ctx, const rapid_attn_shape* shape, const 
     };
     a.side[0] = side(k_rows, k_codes, k_scales);
     a.side[1] = side(v_rows, v_codes, v_scales);
-    a.ctx_lens = ctx_lens;
-    a.gammas = gammas;
-    a.page_table = shape->page_size ? page_table : nullptr;
-    a.B = shape->batch;
-    a.Qmax = shape->q_max;
-    a.Hkv = shape->n_kv_heads;
-    a.D = shape->head_dim;
-    a.gamma = shape->gamma;
-    a.max_ctx = shape->max_ctx;
-    a.bstride = shape->kv_batch_stride;
-    a.tstride = shape->kv_token_stride;
-    a.hstride = shape->kv_head_stride;
-    a.pstride = shape->kv_page_stride;
-    a.sbstride = layout->scale_batch_stride;
-    a.shstride = layout->scale_head_stride;
-    a.spstride = layout->scale_page_stride;
-    a.page_shift = page_shift_of(shape);
-    a.page_mask = shape->page_size ? shape->page_size - 1 : 0;
-    a.max_pages = shape->max_pages;
-    a.page_hi = page_hi_of(shape);
+    bind_quant_shape(a, shape, layout, ctx_lens, gammas, page_table);
     DeviceScope dev(ctx->device);
     if (dev.err != hipSuccess) return hip_fail(ctx, dev.err);
     hipError_t e = append ? launch_kv_append_quant(a, static_cast<hipStream_t>(stream))

@@ -103,17 +103,22 @@ hipError_t launch_hbm_read_probe(const rapid_ctx* ctx, const void* buf, size_t b
 
 // ---- output head (lm_head.hip)
 struct LmHeadLaunch {
-    const uint16_t* h;      // [n_rows][hidden] bf16
-    const uint16_t* w;      // [vocab][hidden] bf16
+    const void* h;          // [n_rows][row_bytes]: bf16, or codes of 8 bits
+    const void* w;          // [vocab][row_bytes]
+    const float* h_scales;  // codes: [n_rows], [vocab]
+    const float* w_scales;
     float* logits;          // [n_rows][ldz]
     float* stats;           // [n_rows][ceil(vocab / (16 nb))][2] or null
     int32_t n_rows, hidden, vocab;
+    int32_t row_bytes;
     int32_t nb;             // 16-row vocabulary blocks per workgroup, 1..32 (statistics chunk = 16 nb)
     int64_t ldz;
     float inv_T;
 };
 hipError_t launch_lm_head(const LmHeadLaunch& a, hipStream_t stream);
 hipError_t configure_lm_head();
+hipError_t launch_lm_head_quant(const LmHeadLaunch& a, hipStream_t stream);
+hipError_t configure_lm_head_quant();
 
 // ---- cache bookkeeping (kv_cache.hip)
 struct KvAppendLaunch {
@@ -165,6 +170,31 @@ struct KvQuantLaunch {
 };
 hipError_t launch_kv_append_quant(const KvQuantLaunch& a, hipStream_t stream);
 hipError_t launch_kv_read_quant(const KvQuantLaunch& a, hipStream_t stream);
+
+// ---- append with rotary positions (kv_rope.hip)
+struct KvRopeLaunch {
+    const uint16_t* q;          // new rows, or null with Hq = 0; (b, i) at (b Qmax + i) * stride elements, heads side by side
+    const uint16_t* k;
+    const uint16_t* v;
+    uint16_t* q_out;            // [B][Qmax][Hq][D]
+    const float* inv_freq;      // [rot / 2]
+    const int32_t* positions;   // [B][Qmax] or null: a row's token
+    int64_t q_stride, k_stride, v_stride;
+    KvQuantLaunch cache;        // strides in bytes; without scales: bf16, whose bytes stand for the codes
+    int32_t Hq, rot, adjacent, heads_each;
+    float amplitude;
+};
+hipError_t launch_kv_append_rope(const KvRopeLaunch& a, hipStream_t stream);
+
+// ---- rows of 8-bit integers (quant_rows.hip)
+struct QuantRowsLaunch {
+    const uint16_t* x;          // row r at x + r * stride, bf16
+    int8_t* codes;              // [rows][pitch], zeros from `cols` on
+    float* scales;              // [rows]
+    int64_t rows, stride;
+    int32_t cols, pitch;
+};
+hipError_t launch_quant_rows(const QuantRowsLaunch& a, hipStream_t stream);
 
 // ---- retrieval chunk selection (retrieve.hip)
 struct RetrieveLaunch {
