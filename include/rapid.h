@@ -509,6 +509,26 @@ int rapid_kv_append_rope_quant(rapid_ctx* ctx, const rapid_attn_shape* shape, co
                                void* q_out, void* k_codes, void* v_codes, void* k_scales, void* v_scales, void* stream);
 
 /*
+ * rapid_verify_attn with a sliding window and sinks: row i of sequence b, at position p = L-Q+i (L = ctx_lens[b], Q = gamma_b + 1), attends
+ * the keys j <= p with j > p - window or j < sinks: the last `window` ones, its own among them, and the first `sinks`.
+ *   window        >= 1 (max_ctx or more: all keys up to p);  sinks >= 0
+ *   shape         as for rapid_verify_attn, but q_max may be anything up to max_ctx: one position, a round's, a whole prompt, or a piece of
+ *                 one behind what is cached already (chunk_tokens and ctx_sum_hint are not used)
+ *   The cache holds every token at its own place.  What no row attends costs nothing and has no effect, whatever it holds: paged, the pages between
+ *                 the sinks and the windows may be given away, and their entries in page_table may be anything (ids are clamped)
+ *   q, k_cache, v_cache, ctx_lens, gammas, page_table, out, lse_out   as for rapid_verify_attn; rows i >= Q are written as zeros (lse_out 0), rows
+ *                 that attend nothing (those of an empty sequence, or at positions below 0 of one shorter than its rows) as zeros, their lse_out as -infinity
+ *   Sums are fp32, weights are rounded to bf16 before the second product; the bounds of values and of batch * max_ctx are those of
+ *   rapid_verify_attn_quant.  A NaN or infinity in a token's K or V reaches the rows that attend this token and no others.
+ *   workspace     >= rapid_verify_attn_window_workspace_bytes(), 256-byte aligned, any content
+ */
+size_t rapid_verify_attn_window_workspace_bytes(const rapid_ctx* ctx, const rapid_attn_shape* shape, int window, int sinks);   /* 0 on a bad shape */
+int rapid_verify_attn_window(rapid_ctx* ctx, const rapid_attn_shape* shape, int window, int sinks,
+                             const void* q, const void* k_cache, const void* v_cache,
+                             const int32_t* ctx_lens, const int32_t* gammas, const int32_t* page_table,
+                             void* out, float* lse_out, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
  * Verification attention of a batch whose sequences share one prefix (several requests, or several drafts, about one long
  * context): the prefix is kept once and read once for all of the batch's rows.  With P = prefix_len[0] and the rest as for rapid_verify_attn,
  * sequence b's own tokens follow the prefix, ctx_lens[b] counts them alone, and row i of head h attends the prefix and its own keys 0 .. L-Q+i:

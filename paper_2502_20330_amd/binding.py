@@ -27,6 +27,7 @@ EXPORTS = ["rapid_create", "rapid_destroy", "rapid_strerror", "rapid_last_hip_er
            "rapid_kv_commit_pages",
            "rapid_kv_append_quant", "rapid_kv_read_quant", "rapid_verify_attn_quant", "rapid_verify_attn_quant_workspace_bytes",
            "rapid_verify_attn_prefix", "rapid_verify_attn_prefix_workspace_bytes",
+           "rapid_verify_attn_window", "rapid_verify_attn_window_workspace_bytes",
            "rapid_kv_append_rope", "rapid_kv_append_rope_quant", "rapid_quant_rows", "rapid_lm_head_quant",
            "rapid_lm_head_quant_workspace_bytes",
            "rapid_retrieve", "rapid_hbm_read_probe"]
@@ -148,6 +149,11 @@ def load_library() -> ctypes.CDLL:
     lib.rapid_verify_attn_prefix.argtypes = [vp, shape_p, prefix_p, vp, vp, vp, i32p, i32p, vp, vp, i32p, i32p, i32p, vp, f32p,
                                              vp, ctypes.c_size_t, vp]
     lib.rapid_verify_attn_prefix.restype = ctypes.c_int
+    lib.rapid_verify_attn_window_workspace_bytes.argtypes = [vp, shape_p, ctypes.c_int, ctypes.c_int]
+    lib.rapid_verify_attn_window_workspace_bytes.restype = ctypes.c_size_t
+    lib.rapid_verify_attn_window.argtypes = [vp, shape_p, ctypes.c_int, ctypes.c_int, vp, vp, vp, i32p, i32p, i32p, vp, f32p,
+                                             vp, ctypes.c_size_t, vp]
+    lib.rapid_verify_attn_window.restype = ctypes.c_int
     rope_p = ctypes.POINTER(Rope)
     lib.rapid_kv_append_rope.argtypes = [vp, shape_p, rope_p, vp, vp, vp, f32p, i32p, i32p, i32p, i32p, vp, vp, vp, vp]
     lib.rapid_kv_append_rope.restype = ctypes.c_int
@@ -474,6 +480,12 @@ class Rapid:
                                        lse_out.shape == (q.shape[0], q.shape[2], q.shape[1])),
                    "lse_out: fp32 [B, Hq, Qmax], contiguous")
 
+    def _check_cache(self, k_cache, v_cache):
+        """A bf16 cache."""
+        self._need(k_cache.dtype == torch.bfloat16 and v_cache.dtype == torch.bfloat16 and k_cache.dim() == 4
+                   and k_cache.shape == v_cache.shape and _strides(k_cache) == _strides(v_cache) and k_cache.stride(3) == 1,
+                   "k_cache and v_cache: bf16 [B or pages, tokens, Hkv, d], d contiguous, the same sizes and strides")
+
     def _quant_shape(self, batch, q_max, hq, gamma, k_codes, v_codes, k_scales, v_scales, page_table, max_ctx, softmax_scale):
         """References to the AttnShape and QuantLayout of a cache in 8 bits: codes [B or pages, tokens, Hkv, d] with any outer strides, scales
         [B or pages, Hkv, tokens], tokens contiguous and the rows a multiple of 16 long (views of memory that goes on are fine)."""
@@ -631,9 +643,7 @@ class Rapid:
                      gamma, max_prefix, max_ctx, softmax_scale):
         self._check_attn(q, out, lse_out)
         self._check_lengths(q.shape[0], ctx_lens, gammas, page_table)
-        self._need(k_cache.dtype == torch.bfloat16 and v_cache.dtype == torch.bfloat16 and k_cache.dim() == 4
-                   and k_cache.shape == v_cache.shape and _strides(k_cache) == _strides(v_cache) and k_cache.stride(3) == 1,
-                   "k_cache and v_cache: bf16 [B or pages, tokens, Hkv, d], d contiguous, the same sizes and strides")
+        self._check_cache(k_cache, v_cache)
         self._need(k_cache.shape[3] == q.shape[3], "q and the cache differ in head_dim")
         self._need(prefix_len.dtype == torch.int32 and prefix_len.numel() == 1, "prefix_len: int32 [1]")
         tokens, hkv, d = k_cache.shape[1:]
@@ -654,6 +664,40 @@ class Rapid:
         n = k_prefix.shape[0]
         self._need(max_prefix is None or max_prefix <= n, "the prefix holds fewer tokens than max_prefix")
         return ctypes.byref(shape), ctypes.byref(PrefixLayout(n if max_prefix is None else int(max_prefix), 0, sp[1], sp[2]))
+
+    # ------------------------------------------------------------------ a window
+    def rapid_verify_attn_window(self, q, k_cache, v_cache, ctx_lens, window: int, gamma: Optional[int] = None, *, sinks: int = 0,
+                                 gammas=None, page_table=None, max_ctx: Optional[int] = None, softmax_scale: Optional[float] = None,
+                                 out=None, lse_out=None):
+        """:meth:`rapid_verify_attn` where a row attends the last `window` keys up to its own, and the first `sinks`.  q bf16 [B,Qmax,Hq,d]
+        of any Qmax: one position, a round's, a whole prompt or a piece of one.  Streams and graphs as for
+        :meth:`rapid_verify_attn_quant`."""
+        if out is None:
+            out = torch.empty_like(q)
+        key = ("window", gamma, window, sinks, max_ctx, softmax_scale,
+               *_sizes(q, k_cache, v_cache, ctx_lens, gammas, page_table, out, lse_out))
+        shape, window, sinks = self._plans.get(key) or self._planned(
+            key, self._plan_window, q, k_cache, v_cache, ctx_lens, gammas, page_table, out, lse_out, gamma, window, sinks, max_ctx, softmax_scale)
+        args = (self._ctx, shape, window, sinks, q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), ctx_lens.data_ptr(), _dptr(gammas),
+                _dptr(page_table), out.data_ptr(), _dptr(lse_out))
+        call, stream = self.lib.rapid_verify_attn_window, _stream_ptr(self.device)
+        rc = call(*args, *self._stream_workspace(stream), stream)
+        if rc == RAPID_EWORKSPACE:                             # the last check of the call: nothing has been launched
+            ws = self._new_workspace(stream, self.lib.rapid_verify_attn_window_workspace_bytes(self._ctx, shape, window, sinks))
+            rc = call(*args, ws.data_ptr(), ws.numel(), stream)
+        if rc:
+            _check(self.lib, rc, self._ctx)
+        return out
+
+    def _plan_window(self, q, k_cache, v_cache, ctx_lens, gammas, page_table, out, lse_out, gamma, window, sinks, max_ctx, softmax_scale):
+        self._check_attn(q, out, lse_out)
+        self._check_lengths(q.shape[0], ctx_lens, gammas, page_table)
+        self._check_cache(k_cache, v_cache)
+        self._need(k_cache.shape[3] == q.shape[3], "q and the cache differ in head_dim")
+        self._need(int(window) == window and int(sinks) == sinks, "window and sinks are whole numbers")
+        scale = q.shape[3] ** -0.5 if softmax_scale is None else float(softmax_scale)
+        most = (1 << 31) - 1                                   # of a C int; more is all there is
+        return ctypes.byref(self._cache_shape(*q.shape[:3], k_cache, gamma, page_table, max_ctx, scale)), min(int(window), most), min(int(sinks), most)
 
     # ------------------------------------------------------------------ append with rotary positions
     def rapid_kv_append_rope(self, k_cache, v_cache, k_new, v_new, inv_freq, ctx_lens, gamma: Optional[int] = None, *, q_new=None,
@@ -727,9 +771,7 @@ class Rapid:
         rope = Rope(2 * inv_freq.numel(), int(bool(interleaved)), float(amplitude), *([0] if q_new is None else []), *strides)
         if k_scales is not None:
             return (*self._quant_shape(B, Q, hq, gamma, k_cache, v_cache, k_scales, v_scales, page_table, max_ctx, 1.0), ctypes.byref(rope))
-        self._need(k_cache.dtype == torch.bfloat16 and v_cache.dtype == torch.bfloat16 and k_cache.shape == v_cache.shape
-                   and _strides(k_cache) == _strides(v_cache) and k_cache.stride(3) == 1,
-                   "k_cache and v_cache: bf16 [B or pages, tokens, Hkv, d], d contiguous, the same sizes and strides")
+        self._check_cache(k_cache, v_cache)
         return ctypes.byref(self._cache_shape(B, Q, hq, k_cache, gamma, page_table, max_ctx, 1.0)), ctypes.byref(rope)
 
     def _cache_shape(self, batch, q_max, hq, k_cache, gamma, page_table, max_ctx, scale) -> AttnShape:
@@ -892,3 +934,8 @@ def rapid_verify_attn_prefix(q, k_cache, v_cache, ctx_lens, prefix_len, gamma=No
 def rapid_lm_head_quant(h, w_codes, w_scales, **kw):
     """Module-level form of :meth:`Rapid.rapid_lm_head_quant` on the tensors' device."""
     return _get(h.device.index or 0).rapid_lm_head_quant(h, w_codes, w_scales, **kw)
+
+
+def rapid_verify_attn_window(q, k_cache, v_cache, ctx_lens, window, gamma=None, **kw):
+    """Module-level form of :meth:`Rapid.rapid_verify_attn_window` on the tensors' device."""
+    return _get(q.device.index or 0).rapid_verify_attn_window(q, k_cache, v_cache, ctx_lens, window, gamma, **kw)

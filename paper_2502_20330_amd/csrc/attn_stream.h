@@ -29,12 +29,15 @@ struct StreamLaunch {
     int32_t quantum;            // tokens that shares are cut by
     int32_t rot;                // 1: share g of slot x serves head (x + g) mod Hkv, 0: head x
     int32_t direct;             // 1: short sequences, one workgroup for each and kv head, which writes the result; no partials
+    int32_t window, sinks;      // window > 0: a row at position p attends tokens of (p - window, p] and the first `sinks`; 0: all up to p
     float scale_log2e;
 };
 constexpr int kStreamRows = 96;      // packed rows that the streaming kernel takes
 // Fill the plan (RP .. direct) from the shape and the source's layout.
 void plan_attn_stream(StreamLaunch& a, int n_cu);
 void plan_attn_prefix(StreamLaunch& a, int n_cu);
+// Windowed attention of more rows than kStreamRows (attn_window.hip): `groups` shares of a row tile's tokens; direct where that is one.
+void plan_attn_window(StreamLaunch& a, int n_cu);
 // Both for one launch: the tokens of a shared prefix, its rows in tiles of at most kStreamRows, and the sequences' own.  Where the two lie differently
 // (one paged, the other not), for two launches in turn.
 void plan_attn_stream_pair(StreamLaunch& own, StreamLaunch& prefix, int n_cu);
@@ -46,5 +49,9 @@ hipError_t configure_attn_prefix();
 hipError_t launch_attn_stream(const StreamLaunch& a, hipStream_t stream);
 hipError_t launch_attn_stream_pair(const StreamLaunch& own, const StreamLaunch& prefix, hipStream_t stream);
 hipError_t launch_attn_prefix(const StreamLaunch& a, hipStream_t stream);
+hipError_t configure_attn_window();
+size_t attn_window_workspace_bytes(const StreamLaunch& a);
+void bind_attn_window(StreamLaunch& a, void* workspace);
+hipError_t launch_attn_window(const StreamLaunch& a, hipStream_t stream);        // writes the result (with a second launch where groups > 1)
 // Joins the partials of `own`, and of a shared prefix where `prefix` has any (prefix.part_o not null).
 hipError_t launch_attn_stream_merge(const StreamLaunch& own, const StreamLaunch& prefix, hipStream_t stream);

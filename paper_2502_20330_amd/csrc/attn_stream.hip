@@ -65,25 +65,44 @@ struct Piece {
     int* taken;                                   // teams: the stream's word for take_not_finite
     uint32_t kring_lds, vring_lds, sring_lds;
     int b, h;
-    int L, Q, R, c0, c1, nt, last_tok;            // nt: this stream's tiles (tokens c0 + (part + it NP) TT ..)
+    int L, Q, R, c0, c1, nt, last_tok;            // nt: this stream's tiles (positions c0 + (part + it NP) TT ..; these are tokens, but for a window)
+    int joint, gap;                               // a window: of its span
     int lane, wave, part, team;
 };
 
+// ---- a window: a sequence's span (attn_tile.h) takes its tokens' place
+constexpr int kWindowStep = 32;
+__device__ __forceinline__ WindowSpan window_span(const StreamLaunch& a, int b, int L)
+{
+    return WindowSpan(L - seq_queries(a, b), L - 1, a.window, a.sinks, kWindowStep);
+}
+// What a sequence has for the workgroups to divide.
+template <bool WINDOW>
+__device__ __forceinline__ int shared_len(const StreamLaunch& a, int b)
+{
+    const int L = seq_len(a, b);
+    return WINDOW ? window_span(a, b, L).len : L;
+}
+template <bool WINDOW>
+__device__ __forceinline__ int tile_token(const Piece& w, int x) { return WINDOW && x >= w.joint ? x + w.gap : x; }
+
 // Row blocks row0 / 16 .. of the workgroup, over this wave's stream.
-template <class G, int RB, bool PAGED>
+template <class G, int RB, bool PAGED, bool WINDOW>
 __device__ __forceinline__ void run_piece(const StreamLaunch& a, const Piece& w, char* smem, int row0, int64_t pbase)
 {
     constexpr int MLS = (G::TEAMS && G::RB1 > G::RB0 ? G::RB1 : G::RB0) * 16;
     const int lane = w.lane, ln = lane & 15, lg = lane >> 4;
-    auto tile_t0 = [&](int it) { return w.c0 + (w.part + it * G::NP) * G::TT; };
+    auto tile_t0 = [&](int it) { return tile_token<WINDOW>(w, w.c0 + (w.part + it * G::NP) * G::TT); };
 
     bf16x8 qf[RB][G::KS];
     int lim[RB];                                         // last token that a row attends in this piece
+    [[maybe_unused]] int before[RB];                     // last token ahead of a row's window
 #pragma unroll
     for (int rb = 0; rb < RB; ++rb) {
         const int row = row0 + rb * 16 + ln;
         const bool real = row < w.R;
-        lim[rb] = min(real && !a.shared ? w.L - w.Q + row / a.G : w.L - 1, w.c1 - 1);
+        lim[rb] = min(real && !a.shared ? w.L - w.Q + row / a.G : w.L - 1, WINDOW ? w.last_tok : w.c1 - 1);
+        before[rb] = WINDOW && real ? w.L - w.Q + row / a.G - a.window : -1;
 #pragma unroll
         for (int ks = 0; ks < G::KS; ++ks) {
             const int chunk = G::QUANT ? (ks >> 1) * 8 + 2 * lg + (ks & 1) : ks * 4 + lg;
@@ -101,7 +120,11 @@ __device__ __forceinline__ void run_piece(const StreamLaunch& a, const Piece& w,
         for (int db = 0; db < G::DB; ++db) st.acc[db][rb] = floatx4{0.f, 0.f, 0.f, 0.f};
     }
     const float c = a.scale_log2e;
+    auto hidden = [&](int tok, int rb) { return tok > lim[rb] || (WINDOW && tok <= before[rb] && tok >= a.sinks); };
     const int first_masked_t0 = min(a.shared ? w.L : w.L - w.Q, w.c1) - (G::TT - 1);     // tiles from here on hold tokens that some row does not attend
+    auto masked = [&](int t0) {
+        return WINDOW ? window_masks(t0, G::TT, w.L - w.Q, w.L - 1, w.last_tok, a.window, a.sinks) : t0 >= first_masked_t0;
+    };
     TilePages<G, PAGED> pages;
     bool taken = false;
     [[maybe_unused]] const uint32_t no_scales[G::TB] = {};
@@ -113,11 +136,11 @@ __device__ __forceinline__ void run_piece(const StreamLaunch& a, const Piece& w,
         // Streams of their own: S tiles are under way, and the slot is filled again by the wave that has read it.
         // Two waves a stream: each issues half of a tile's loads (both the scales); at the meeting tile `it` is complete and everybody has read
         // tile it - 1, whose slot takes tile it + S - 1.
-        int before = G::S - 1;
-        for (int it = 0; it < w.nt; ++it, before = slot, slot = next(slot)) {
+        int before_slot = G::S - 1;
+        for (int it = 0; it < w.nt; ++it, before_slot = slot, slot = next(slot)) {
             char* kt = w.kring + slot * G::SLOT;
             char* vt = w.vring + slot * G::SLOT;
-            const int t0 = tile_t0(it), fill = G::TEAMS ? before : slot, t_fill = tile_t0(it + G::S - (G::TEAMS ? 1 : 0));
+            const int t0 = tile_t0(it), fill = G::TEAMS ? before_slot : slot, t_fill = tile_t0(it + G::S - (G::TEAMS ? 1 : 0));
             constexpr int H = G::TEAMS ? G::NLD / 2 : G::NLD;
             auto refill = [&]() {
                 load_scales<G, PAGED>(w.addr, pages, w.sring_lds + fill * 256, t_fill, w.last_tok, lane);
@@ -130,7 +153,7 @@ __device__ __forceinline__ void run_piece(const StreamLaunch& a, const Piece& w,
                 meet();
                 refill();
             }
-            if (t0 >= first_masked_t0) taken |= take_not_finite<G>(vt, lane);      // (of a team, whoever comes second finds zeros)
+            if (masked(t0)) taken |= take_not_finite<G>(vt, lane);      // (of a team, whoever comes second finds zeros)
             RawTile<G> x;
             x.read_k(kt, w.sring + slot * 256, lane);
             in_order();
@@ -140,7 +163,7 @@ __device__ __forceinline__ void run_piece(const StreamLaunch& a, const Piece& w,
             x.read_v(vt, lane);
             lds_reads_done();
             if (!G::TEAMS) refill();
-            softmax_tile<G, RB>(st, s, pb, x.vs, t0, t0 >= first_masked_t0, lim, w.c1, c, lane);
+            softmax_tile<G, RB>(st, s, pb, x.vs, t0, masked(t0), hidden, w.c1, c, lane);
             x.add_values(st, pb);
         }
     } else if constexpr (!G::TEAMS) {
@@ -158,10 +181,10 @@ __device__ __forceinline__ void run_piece(const StreamLaunch& a, const Piece& w,
             lds_reads_done();
             load_tile<G, PAGED, false, G::NLD>(w.addr, pages, w.kring_lds + slot * G::SLOT, t_next, w.last_tok, lane, 0);
 
-            softmax_tile<G, RB>(st, s, pb, no_scales, t0, t0 >= first_masked_t0, lim, w.c1, c, lane);
+            softmax_tile<G, RB>(st, s, pb, no_scales, t0, masked(t0), hidden, w.c1, c, lane);
 
             wait_loads<(2 * G::S - 1) * G::NLD>();              // V(it)
-            if (t0 >= first_masked_t0) taken |= take_not_finite<G>(vt, lane);
+            if (masked(t0)) taken |= take_not_finite<G>(vt, lane);
             pv_tile<G, RB>(st, pb, vt, lane);
             lds_reads_done();
             load_tile<G, PAGED, true, G::NLD>(w.addr, pages, w.vring_lds + slot * G::SLOT, t_next, w.last_tok, lane, 0);
@@ -173,8 +196,8 @@ __device__ __forceinline__ void run_piece(const StreamLaunch& a, const Piece& w,
         constexpr int H = G::NLD / 2, BEHIND = 2 * (G::S - 1) * H;
         TilePages<G, PAGED> vpages;
         vpages.find(w.addr, tile_t0(G::S - 1), w.last_tok);
-        int before = G::S - 1;                                  // the slot of tile it - 1
-        for (int it = 0; it < w.nt; ++it, before = slot, slot = next(slot)) {
+        int before_slot = G::S - 1;                             // the slot of tile it - 1
+        for (int it = 0; it < w.nt; ++it, before_slot = slot, slot = next(slot)) {
             char* kt = w.kring + slot * G::SLOT;
             char* vt = w.vring + slot * G::SLOT;
             const int t0 = tile_t0(it), t_next = tile_t0(it + G::S);
@@ -184,15 +207,15 @@ __device__ __forceinline__ void run_piece(const StreamLaunch& a, const Piece& w,
             pages.find(w.addr, t_next, w.last_tok);
             wait_loads<BEHIND>();                               // own half of K(it)
             __syncthreads();                                    // A
-            load_tile<G, PAGED, true, H>(w.addr, vpages, w.vring_lds + before * G::SLOT, t_next - G::QUANTUM, w.last_tok, lane, w.team * H);
+            load_tile<G, PAGED, true, H>(w.addr, vpages, w.vring_lds + before_slot * G::SLOT, tile_t0(it + G::S - 1), w.last_tok, lane, w.team * H);
             score_tile<G, RB>(s, qf, kt, lane);
-            softmax_tile<G, RB>(st, s, pb, no_scales, t0, t0 >= first_masked_t0, lim, w.c1, c, lane);
+            softmax_tile<G, RB>(st, s, pb, no_scales, t0, masked(t0), hidden, w.c1, c, lane);
 
             wait_loads<BEHIND>();                               // own half of V(it)
             lds_reads_done();
             __syncthreads();                                    // B
             load_tile<G, PAGED, false, H>(w.addr, pages, w.kring_lds + slot * G::SLOT, t_next, w.last_tok, lane, w.team * H);
-            if (t0 >= first_masked_t0) taken |= take_not_finite<G>(vt, lane);      // (whoever comes second finds zeros)
+            if (masked(t0)) taken |= take_not_finite<G>(vt, lane);      // (whoever comes second finds zeros)
             pv_tile<G, RB>(st, pb, vt, lane);
             lds_reads_done();
             vpages = pages;
@@ -204,7 +227,15 @@ __device__ __forceinline__ void run_piece(const StreamLaunch& a, const Piece& w,
         __syncthreads();
         taken = *w.taken != 0;
     }
-    if (taken) {
+    if (WINDOW && taken) {
+#pragma unroll 1
+        for (int it = 0; it < w.nt; ++it) {
+            const int t0 = tile_t0(it), end = min(t0 + G::TT - 1, w.last_tok), lg = opaque(lane) >> 4;
+            if (!masked(t0)) continue;
+#pragma unroll 1
+            for (int tok = t0; tok <= end; ++tok) add_not_finite_of<G, RB, PAGED>(st, w.addr, tok, hidden, lg);
+        }
+    } else if (taken) {
         const int it = (max(first_masked_t0 - tile_t0(0), 0) + G::QUANTUM - 1) / G::QUANTUM;
         add_not_finite<G, RB, PAGED>(st, w.addr, tile_t0(it), w.c1, G::QUANTUM, lim, lane);
     }
@@ -274,7 +305,7 @@ __device__ __forceinline__ void run_piece(const StreamLaunch& a, const Piece& w,
     }
 }
 
-template <class G, bool PAGED>
+template <class G, bool PAGED, bool WINDOW>
 __device__ __forceinline__ void stream_piece(const StreamLaunch& a, char* smem, int b, int h, int L, int c0, int c1, int64_t pbase, int r0)
 {                                                        // r0: the first of the packed rows (of a shared prefix, there may be more than RP)
     Piece w;
@@ -295,7 +326,13 @@ __device__ __forceinline__ void stream_piece(const StreamLaunch& a, char* smem, 
     // apart: 128K tokens at 4 rows 48.4 us instead of 46.2, at 36 rows 61 instead of 59, at 72 rows 75 instead of 72.5.)
     // Teams meet at barriers, so there every stream runs as many tiles; those past the end are masked.
     w.nt = (ntile + G::NP - 1 - (G::TEAMS ? 0 : w.part)) / G::NP;
-    w.last_tok = c1 - 1;
+    if (WINDOW) {
+        static_assert(!WINDOW || G::TT == kWindowStep, "");
+        const WindowSpan span = window_span(a, b, L);
+        w.joint = span.joint;
+        w.gap = span.gap;
+    }
+    w.last_tok = tile_token<WINDOW>(w, c1 - 1);
     w.addr = make_row_addr<G, PAGED>(a.own, b, h);
     const int ring = w.part * G::RING;
     const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)smem;
@@ -320,7 +357,7 @@ __device__ __forceinline__ void stream_piece(const StreamLaunch& a, char* smem, 
             dma16_keep(reinterpret_cast<const char*>(a.q), off, lds + G::NP * G::RING + e * 1024);
         }
     }
-    auto tile_t0 = [&](int it) { return c0 + (w.part + it * G::NP) * G::TT; };
+    auto tile_t0 = [&](int it) { return tile_token<WINDOW>(w, c0 + (w.part + it * G::NP) * G::TT); };
     TilePages<G, PAGED> pages;
     constexpr int H = G::TEAMS ? G::NLD / 2 : G::NLD;
     const int e0 = G::TEAMS ? w.team * H : 0;
@@ -342,13 +379,13 @@ __device__ __forceinline__ void stream_piece(const StreamLaunch& a, char* smem, 
     __syncthreads();                                     // the whole Q block is in LDS
 
     if constexpr (!G::TEAMS) {
-        run_piece<G, G::RB0, PAGED>(a, w, smem, 0, pbase);
+        run_piece<G, G::RB0, PAGED, WINDOW>(a, w, smem, 0, pbase);
     } else if constexpr (G::RB0 == G::RB1) {
-        run_piece<G, G::RB0, PAGED>(a, w, smem, w.team * G::RB0 * 16, pbase);
+        run_piece<G, G::RB0, PAGED, WINDOW>(a, w, smem, w.team * G::RB0 * 16, pbase);
     } else {
         // the two arms run the same barriers
-        if (w.team == 0) run_piece<G, G::RB0, PAGED>(a, w, smem, 0, pbase);
-        else run_piece<G, G::RB1, PAGED>(a, w, smem, G::RB0 * 16, pbase);
+        if (w.team == 0) run_piece<G, G::RB0, PAGED, WINDOW>(a, w, smem, 0, pbase);
+        else run_piece<G, G::RB1, PAGED, WINDOW>(a, w, smem, G::RB0 * 16, pbase);
     }
 }
 
@@ -364,25 +401,35 @@ __device__ __forceinline__ void write_missing_rows(const StreamLaunch& a, int b,
 }
 
 // Grid: one workgroup per (kv head, share).  Partials: [kv head][g + b], which no two pieces of a head share.  Direct: per (kv head, sequence).
-template <class G, bool PAGED>
+template <class G, bool PAGED, bool WINDOW = false>
 __device__ __forceinline__ void stream_share(const StreamLaunch& a, char* smem, int g, int len, int rt = 0)
 {                                                        // len: of sequence `lane`, 0 where there is none
     const int h = __builtin_amdgcn_readfirstlane(a.rot ? (blockIdx.x + g) % a.Hkv : blockIdx.x);     // (base addresses go through scalar registers)
     if (a.direct) {
         const int L = __builtin_amdgcn_readfirstlane(seq_len(a, g));
         write_missing_rows<G>(a, g, h, L);
-        if (L > 0) stream_piece<G, PAGED>(a, smem, g, h, L, 0, L, 0, 0);
+        const int all = WINDOW ? window_span(a, g, L).len : L;
+        if (L > 0) stream_piece<G, PAGED, WINDOW>(a, smem, g, h, L, 0, all, 0, 0);
         return;
     }
-    for_each_piece(a, g, threadIdx.x & 63, len, G::QUANTUM, [&](int b, int L, int c0, int c1) {
-        stream_piece<G, PAGED>(a, smem, b, h, L, c0, c1, ((int64_t)(h * a.tiles + rt) * a.nslots + g + b) * G::RP, rt * G::RP);
+    for_each_piece(a, g, threadIdx.x & 63, len, G::QUANTUM, [&](int b, int all, int c0, int c1) {
+        const int L = WINDOW ? __builtin_amdgcn_readfirstlane(seq_len(a, b)) : all;
+        stream_piece<G, PAGED, WINDOW>(a, smem, b, h, L, c0, c1, ((int64_t)(h * a.tiles + rt) * a.nslots + g + b) * G::RP, rt * G::RP);
         wait_loads<0>();                                 // the partial's stores are out of the load account
-    });
+    }, [&](int b) { return shared_len<WINDOW>(a, b); });
 }
+template <bool WINDOW = false>
 __device__ __forceinline__ int first_len(const StreamLaunch& a)
 {
     const int lane = threadIdx.x & 63;
-    return !a.direct && lane < a.B ? seq_len(a, lane) : 0;
+    return !a.direct && lane < a.B ? shared_len<WINDOW>(a, lane) : 0;
+}
+// bf16, a window.
+template <class G, bool PAGED>
+__global__ void __launch_bounds__(G::NW * 64) attn_stream_window(StreamLaunch a)
+{
+    extern __shared__ __attribute__((aligned(1024))) char smem[];
+    stream_share<G, PAGED, true>(a, smem, blockIdx.y, first_len<true>(a));
 }
 template <class G, bool PAGED>
 __global__ void __launch_bounds__(G::NW * 64) attn_stream(StreamLaunch a)
@@ -454,11 +501,12 @@ struct Partials {
 struct Place {
     int before = 0, cost = 0, total = 0, n = 0;          // n: sequences that have tokens
 };
+template <bool WINDOW>
 __device__ __forceinline__ Place find_place(const StreamLaunch& a, int b, int lane, int len)
 {                                                        // len: of sequence `lane`, 0 where there is none
     Place p;
     for (int b0 = 0; b0 < a.B; b0 += 64) {
-        if (b0) len = b0 + lane < a.B ? seq_len(a, b0 + lane) : 0;
+        if (b0) len = b0 + lane < a.B ? shared_len<WINDOW>(a, b0 + lane) : 0;
         const int mine = seq_cost(len, b0 + lane, a.quantum);
         const int end = p.total + scan_costs(mine);
         if (b >= b0 && b < b0 + 64) {
@@ -532,7 +580,7 @@ __device__ __forceinline__ int64_t first_slot(const StreamLaunch& a, int h, int 
 
 // One workgroup of D threads per (sequence, kv head, packed row): out = sum 2^(m_s - M) O_s / sum 2^(m_s - M) l_s, over the row's partials of the
 // prefix and of its own tokens.
-template <int D, bool PREFIX>
+template <int D, bool PREFIX, bool WINDOW>
 __global__ void __launch_bounds__(D) attn_stream_merge(StreamLaunch a, StreamLaunch prefix)
 {
     const int row = blockIdx.x, h = blockIdx.y, b = blockIdx.z;
@@ -546,14 +594,14 @@ __global__ void __launch_bounds__(D) attn_stream_merge(StreamLaunch a, StreamLau
     // All that can be asked for is asked for at once: the lengths, the first block of a single sequence (the prefix is one) before its length is known, the
     // other's as soon as the lengths are there.
     const int lane = d & 63;
-    const int len = lane < a.B ? seq_len(a, lane) : 0, prefix_len = PREFIX ? seq_len(prefix, 0) : 0;
+    const int len = lane < a.B ? shared_len<WINDOW>(a, lane) : 0, prefix_len = PREFIX ? seq_len(prefix, 0) : 0;
     const bool there = seq_len(a, b) > 0;                 // (a sequence without tokens has no rows, behind a prefix either)
     const int prefix_row = b * a.Qmax * a.G + row;
     PartialBlock x, y;
     const int64_t x_slot = PREFIX ? first_slot(prefix, h, prefix_row) : 0;
     if (PREFIX) x.load<D>(prefix, x_slot, prefix.nslots, d);
     if (a.B == 1) y.load<D>(a, first_slot(a, h, row), a.nslots, d);
-    const Place at = find_place(a, b, lane, len);
+    const Place at = find_place<WINDOW>(a, b, lane, len);
     PairGroups groups{a.groups, 0};
     if (PREFIX) groups = pair_groups(a, prefix, at.total, at.n, prefix_len);
     const Partials own = find_partials(a, at, groups.own, b, h, row);
@@ -610,8 +658,10 @@ hipError_t configure_attn_stream()
                         const hipError_t e = raise(attn_stream<G, false>);
                         return e == hipSuccess ? raise(attn_stream<G, true>) : e;
                     } else {
-                        const hipError_t e = raise(attn_stream_pair<G, false>);
-                        return e == hipSuccess ? raise(attn_stream_pair<G, true>) : e;
+                        hipError_t e = raise(attn_stream_pair<G, false>);
+                        if (e == hipSuccess) e = raise(attn_stream_pair<G, true>);
+                        if (e == hipSuccess) e = raise(attn_stream_window<G, false>);
+                        return e == hipSuccess ? raise(attn_stream_window<G, true>) : e;
                     }
                 });
                 if (e != hipSuccess) return e;
@@ -627,6 +677,13 @@ namespace {
 // round (16 sequences, 20 rows: 512 tokens 11.4 instead of 18, 1024 14.3 instead of 20, 2048 19.7 instead of 24.5).
 constexpr int kDirectQuanta = 2, kDirectBatchQuanta = 8;
 
+// The most that a sequence has for the workgroups to divide.
+int64_t most_tokens(const StreamLaunch& a)
+{
+    const int64_t span = (int64_t)a.sinks + a.window + a.Qmax + 2 * kWindowStep;
+    return a.window && span < a.max_ctx ? span : a.max_ctx;
+}
+
 void plan_shares(StreamLaunch& a, int rb, int groups)
 {
     a.RP = rb * 16;
@@ -636,7 +693,7 @@ void plan_shares(StreamLaunch& a, int rb, int groups)
         return hipSuccess;
     });
     // no more shares than the longest possible batch has quanta
-    const int64_t most = (int64_t)a.B * (((int64_t)a.max_ctx + a.quantum - 1) / a.quantum + kPieceQuanta);
+    const int64_t most = (int64_t)a.B * ((most_tokens(a) + a.quantum - 1) / a.quantum + kPieceQuanta);
     a.groups = groups < 1 ? 1 : groups;
     if (a.groups > most) a.groups = (int)most;
     a.nslots = a.groups + a.B - 1;
@@ -652,7 +709,7 @@ void plan_attn_stream(StreamLaunch& a, int n_cu)
     plan_shares(a, (a.Qmax * a.G + 15) / 16, n_cu / a.Hkv);
     const int64_t units = (int64_t)a.B * a.Hkv;
     const int quanta = 2 * units >= n_cu && units <= n_cu ? kDirectBatchQuanta : kDirectQuanta;
-    a.direct = a.max_ctx <= quanta * a.quantum;
+    a.direct = most_tokens(a) <= quanta * a.quantum;
 }
 
 void plan_attn_stream_pair(StreamLaunch& own, StreamLaunch& prefix, int n_cu)
@@ -688,6 +745,9 @@ hipError_t launch_attn_stream(const StreamLaunch& a, hipStream_t stream)
         if constexpr (G::QUANT) {
             auto fn = a.own.page_table ? attn_stream<G, true> : attn_stream<G, false>;
             hipLaunchKernelGGL(fn, grid, block, G::LDS, stream, a);
+        } else if (a.window) {
+            auto fn = a.own.page_table ? attn_stream_window<G, true> : attn_stream_window<G, false>;
+            hipLaunchKernelGGL(fn, grid, block, G::LDS, stream, a);
         } else {
             auto fn = a.own.page_table ? attn_stream_pair<G, true> : attn_stream_pair<G, false>;
             hipLaunchKernelGGL(fn, grid, block, G::LDS, stream, a, StreamLaunch{});
@@ -717,8 +777,9 @@ hipError_t launch_attn_stream_pair(const StreamLaunch& own, const StreamLaunch& 
 
 hipError_t launch_attn_stream_merge(const StreamLaunch& a, const StreamLaunch& prefix, hipStream_t stream)
 {
-    auto fn = prefix.part_o ? (a.D == 128 ? attn_stream_merge<128, true> : attn_stream_merge<64, true>)
-                            : (a.D == 128 ? attn_stream_merge<128, false> : attn_stream_merge<64, false>);
+    auto fn = prefix.part_o ? (a.D == 128 ? attn_stream_merge<128, true, false> : attn_stream_merge<64, true, false>)
+              : a.window    ? (a.D == 128 ? attn_stream_merge<128, false, true> : attn_stream_merge<64, false, true>)
+                            : (a.D == 128 ? attn_stream_merge<128, false, false> : attn_stream_merge<64, false, false>);
     hipLaunchKernelGGL(fn, dim3(a.Qmax * a.G, a.Hkv, a.B), dim3(a.D), 0, stream, a, prefix);
     return hipGetLastError();
 }

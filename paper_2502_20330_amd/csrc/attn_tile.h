@@ -66,15 +66,16 @@ struct Shares {
         return x < head ? (int)((unsigned)x / (unsigned)(len + 1)) : rest + (int)((unsigned)(x - head) / (unsigned)max(len, 1));
     }
 };
-// Calls piece(b, L, c0, c1) for every piece [c0, c1) of a sequence b in share g, in order.  Sequences are taken 64 at a time, one a lane.
-template <class Piece>
-__device__ __forceinline__ void for_each_piece(const StreamLaunch& a, int g, int lane, int len, int quantum, Piece piece)
+// Calls piece(b, L, c0, c1) for every piece [c0, c1) of a sequence b in share g, in order.  Sequences are taken 64 at a time, one a lane; len_of(b): their
+// lengths.
+template <class Piece, class Len>
+__device__ __forceinline__ void for_each_piece(const StreamLaunch& a, int g, int lane, int len, int quantum, Piece piece, Len len_of)
 {                                                        // len: of sequence `lane`, 0 where there is none
     int cost = seq_cost(len, lane, quantum);
     int end = scan_costs(cost);                          // cost of the sequences up to this one
     int total = __builtin_amdgcn_readlane(end, 63);
     for (int b0 = 64; b0 < a.B; b0 += 64)
-        total += __builtin_amdgcn_readlane(scan_costs(b0 + lane < a.B ? seq_cost(seq_len(a, b0 + lane), b0 + lane, quantum) : 0), 63);
+        total += __builtin_amdgcn_readlane(scan_costs(b0 + lane < a.B ? seq_cost(len_of(b0 + lane), b0 + lane, quantum) : 0), 63);
     const Shares sh(total, a.groups);
     const int x0 = sh.begin(g), x1 = min(sh.begin(g + 1), total);
     if (x0 >= x1) return;
@@ -91,10 +92,15 @@ __device__ __forceinline__ void for_each_piece(const StreamLaunch& a, int g, int
         const int before = __builtin_amdgcn_readlane(end, 63);
         b0 += 64;
         if (b0 >= a.B || before >= x1) return;
-        len = b0 + lane < a.B ? seq_len(a, b0 + lane) : 0;
+        len = b0 + lane < a.B ? len_of(b0 + lane) : 0;
         cost = seq_cost(len, b0 + lane, quantum);
         end = before + scan_costs(cost);
     }
+}
+template <class Piece>
+__device__ __forceinline__ void for_each_piece(const StreamLaunch& a, int g, int lane, int len, int quantum, Piece piece)
+{
+    for_each_piece(a, g, lane, len, quantum, piece, [&](int b) { return seq_len(a, b); });
 }
 
 // The same number, of which the compiler knows nothing: what rare paths make of it is computed there, and does not take registers from the
@@ -359,9 +365,10 @@ __device__ __forceinline__ float rounded_exponent(float s, float c, float m)
 // own rounding, is up to 1.4 times as far off as one of 32-bit weights.  The sum of the weights takes them unrounded.
 // The reference maximum only moves when a score exceeds it by kRescaleLog2; until then p = 2^(s - ref) <= 2^kRescaleLog2, exact in the final
 // ratio.  So a tile's own maxima are only looked at lane by lane, and brought together over the lanes of a row when one of them asks for it.
-template <class G, int RB>
+// hidden(token, rb): whether the row of block rb does not attend a token, asked where `masked`.
+template <class G, int RB, class Hidden>
 __device__ __forceinline__ void softmax_tile(WaveState<G, RB>& st, floatx4 (&s)[G::TB][RB], bf16x8 (&pb)[G::TB / 2][RB],
-                                             const uint32_t (&vs)[G::TB], int t0, bool masked, const int (&lim)[RB], int end, float c, int lane)
+                                             const uint32_t (&vs)[G::TB], int t0, bool masked, Hidden hidden, int end, float c, int lane)
 {
     float vscale[G::TB][4];
     if (G::QUANT) {
@@ -380,7 +387,7 @@ __device__ __forceinline__ void softmax_tile(WaveState<G, RB>& st, floatx4 (&s)[
                 const int tok = t0 + tb * 16 + lg * 4 + i;
 #pragma unroll
                 for (int rb = 0; rb < RB; ++rb)
-                    if (tok > lim[rb]) s[tb][rb][i] = -INFINITY;
+                    if (hidden(tok, rb)) s[tb][rb][i] = -INFINITY;
                 if (G::QUANT && tok >= end) vscale[tb][i] = 0.f;       // a scale that belongs to no token may be anything
             }
     }
@@ -498,41 +505,67 @@ __device__ __forceinline__ bool take_not_finite(char* vt, int lane)
     }
     return __any(any);
 }
+// What is not finite in V of token t, to the rows that attend it.
+template <class G, int RB, bool PAGED, class Hidden>
+__device__ __forceinline__ void add_not_finite_of(WaveState<G, RB>& st, const RowAddr& ra, int t, Hidden hidden, int lg)
+{
+    const char* row = ra.v;
+    if (PAGED) row += (int64_t)min(max(ra.pages[t >> ra.page_shift], 0), ra.page_hi) * ra.page_bytes;
+    row += (uint32_t)(PAGED ? t & ra.page_mask : t) * ra.tok_bytes;
+#pragma unroll
+    for (int db = 0; db < G::DB; ++db) {
+        uint32_t bits[4];                                // columns 16 db + 4 lg .. + 3
+        if (G::QUANT) {
+            const uint32_t w = *reinterpret_cast<const uint32_t*>(row + db * 16 + lg * 4);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) bits[i] = (w >> (8 * i) & 0x7fu) == 0x7fu ? 0x7fc00000u : 0u;
+        } else {
+            const u32x2 w = *reinterpret_cast<const u32x2*>(row + db * 32 + lg * 8);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const uint32_t x = i & 1 ? w[i >> 1] & 0xffff0000u : w[i >> 1] << 16;
+                bits[i] = (x & 0x7f800000u) == 0x7f800000u ? x : 0u;
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int rb = 0; rb < RB; ++rb)
+                if (bits[i] && !hidden(t, rb)) st.acc[db][rb][i] += __uint_as_float(bits[i]);
+    }
+}
 template <class G, int RB, bool PAGED>
 __device__ __forceinline__ void add_not_finite(WaveState<G, RB>& st, const RowAddr& ra, int begin, int end, int step, const int (&lim)[RB], int lane)
 {                                                        // tiles of a stream, `step` tokens apart, from token `begin` on
     const int lg = opaque(lane) >> 4;
 #pragma unroll 1
     for (int t = begin, left = G::TT; t < end; ++t) {
-        const char* row = ra.v;
-        if (PAGED) row += (int64_t)min(max(ra.pages[t >> ra.page_shift], 0), ra.page_hi) * ra.page_bytes;
-        row += (uint32_t)(PAGED ? t & ra.page_mask : t) * ra.tok_bytes;
-#pragma unroll
-        for (int db = 0; db < G::DB; ++db) {
-            uint32_t bits[4];                            // columns 16 db + 4 lg .. + 3
-            if (G::QUANT) {
-                const uint32_t w = *reinterpret_cast<const uint32_t*>(row + db * 16 + lg * 4);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) bits[i] = (w >> (8 * i) & 0x7fu) == 0x7fu ? 0x7fc00000u : 0u;
-            } else {
-                const u32x2 w = *reinterpret_cast<const u32x2*>(row + db * 32 + lg * 8);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const uint32_t x = i & 1 ? w[i >> 1] & 0xffff0000u : w[i >> 1] << 16;
-                    bits[i] = (x & 0x7f800000u) == 0x7f800000u ? x : 0u;
-                }
-            }
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-#pragma unroll
-                for (int rb = 0; rb < RB; ++rb)
-                    if (bits[i] && t <= lim[rb]) st.acc[db][rb][i] += __uint_as_float(bits[i]);
-        }
+        add_not_finite_of<G, RB, PAGED>(st, ra, t, [&](int tok, int rb) { return tok > lim[rb]; }, lg);
         if (--left == 0) {
             left = G::TT;
             t += step - G::TT;
         }
     }
+}
+
+// ---- a window
+// Rows at positions p attend the tokens of (p - window, p] and the first `sinks`.  What a set of rows at positions first .. last attends is two runs
+// of tokens, which the kernels take for one: its positions are tokens up to `joint`, and tokens less `gap` from there on.  Both are multiples of `step`, a
+// tile's tokens, so that no tile lies on both sides.
+struct WindowSpan {
+    int joint, gap, len;
+    __device__ __forceinline__ WindowSpan(int first, int last, int window, int sinks, int step)
+    {
+        joint = (min(sinks, last + 1) + step - 1) / step * step;
+        gap = max(max(first - window + 1, 0) / step * step - joint, 0);
+        len = max(last + 1 - gap, 0);
+    }
+    __device__ __forceinline__ int token(int x) const { return x < joint ? x : x + gap; }
+};
+// Whether a tile holds a token that some of the rows do not attend.
+__device__ __forceinline__ bool window_masks(int t0, int tokens, int first, int last, int last_tok, int window, int sinks)
+{
+    return t0 + tokens - 1 > min(first, last_tok) || (t0 <= last - window && t0 + tokens > sinks);
 }
 
 }  // namespace

@@ -364,6 +364,29 @@ StreamLaunch plan_quant(const rapid_ctx* ctx, const rapid_attn_shape* s, const A
     plan_attn_stream(a, compute_units(ctx));
     return a;
 }
+// A window: few rows a kv head are packed and stream the tokens, more are cut into row tiles.
+bool few_rows(const rapid_attn_shape* s) { return (int64_t)s->q_max * (s->n_q_heads / s->n_kv_heads) <= kStreamRows; }
+int check_window_shape(const rapid_attn_shape* s, int window, int sinks)
+{
+    int rc = check_attn_shape(s, false);
+    if (rc == RAPID_OK && (window < 1 || sinks < 0)) rc = RAPID_EINVAL;
+    if (rc == RAPID_OK && few_rows(s)) rc = check_attn_shape(s);
+    if (rc == RAPID_OK) rc = check_tokens(s->batch, s->max_ctx);
+    if (rc != RAPID_OK) return rc;
+    // packed rows and row tiles are counted in 32 bits
+    const int64_t rows = (int64_t)s->q_max * (s->n_q_heads / s->n_kv_heads);
+    if (rows > 1 << 30 || s->n_kv_heads > 65535 || (rows / 128 + 1) * s->batch * s->n_kv_heads > 1 << 30) return RAPID_EUNSUPPORTED;
+    return RAPID_OK;
+}
+StreamLaunch plan_window(const rapid_ctx* ctx, const rapid_attn_shape* s, int window, int sinks, const AttnSource& own)
+{
+    StreamLaunch a = stream_shape(s, own);
+    a.window = window < s->max_ctx ? window : s->max_ctx;                  // (more is all there is)
+    a.sinks = sinks < s->max_ctx ? sinks : s->max_ctx;
+    if (few_rows(s)) plan_attn_stream(a, compute_units(ctx));
+    else plan_attn_window(a, compute_units(ctx));
+    return a;
+}
 // The sequences' own tokens, and the shared prefix with the rows of all of them.
 struct PrefixPlan {
     StreamLaunch own, prefix;
@@ -426,6 +449,7 @@ int rapid_create(rapid_ctx** out, int device)
     if (ec == hipSuccess) ec = configure_lm_head_quant();
     if (ec == hipSuccess) ec = configure_attn_stream();
     if (ec == hipSuccess) ec = configure_attn_prefix();
+    if (ec == hipSuccess) ec = configure_attn_window();
     if (ec == hipSuccess) ec = configure_hbm_read_probe();
     void* scratch_ptr = nullptr;                      // this device's copy of `scratch`
     if (ec == hipSuccess) ec = hipGetSymbolAddress(&scratch_ptr, HIP_SYMBOL(scratch));
@@ -1136,6 +1160,44 @@ int rapid_verify_attn_prefix(rapid_ctx* ctx, const rapid_attn_shape* shape, cons
         if (e == hipSuccess) e = launch_attn_stream(a, st);
     }
     if (e == hipSuccess && !a.direct) e = launch_attn_stream_merge(a, p.prefix, st);
+    if (e != hipSuccess) return hip_fail(ctx, e);
+    return RAPID_OK;
+}
+
+size_t rapid_verify_attn_window_workspace_bytes(const rapid_ctx* ctx, const rapid_attn_shape* shape, int window, int sinks)
+{
+    if (check_window_shape(shape, window, sinks) != RAPID_OK) return 0;
+    const StreamLaunch a = plan_window(ctx, shape, window, sinks, AttnSource{});
+    return few_rows(shape) ? attn_stream_workspace_bytes(a) : attn_window_workspace_bytes(a);
+}
+
+int rapid_verify_attn_window(rapid_ctx* ctx, const rapid_attn_shape* shape, int window, int sinks,
+                             const void* q, const void* k_cache, const void* v_cache,
+                             const int32_t* ctx_lens, const int32_t* gammas, const int32_t* page_table,
+                             void* out, float* lse_out, void* workspace, size_t workspace_bytes, void* stream)
+{
+    if (!ctx) return RAPID_EINVAL;
+    const int rc = check_window_shape(shape, window, sinks);
+    if (rc != RAPID_OK) return rc;
+    if (!q || !k_cache || !v_cache || !ctx_lens || !out) return RAPID_EINVAL;
+    if (shape->page_size != 0 && !page_table) return RAPID_EINVAL;
+    if (!aligned(q, 16) || !aligned(k_cache, 16) || !aligned(v_cache, 16) || !aligned(out, 16)) return RAPID_EALIGN;
+    const bool few = few_rows(shape);
+    StreamLaunch a = plan_window(ctx, shape, window, sinks, source_of(shape, k_cache, v_cache, page_table));
+    const size_t need = few ? attn_stream_workspace_bytes(a) : attn_window_workspace_bytes(a);
+    if (!workspace || !aligned(workspace, 256) || workspace_bytes < need) return RAPID_EWORKSPACE;
+    if (few) bind_attn_stream(a, workspace);
+    else bind_attn_window(a, workspace);
+    a.q = static_cast<const uint16_t*>(q);
+    a.out = static_cast<uint16_t*>(out);
+    a.lse_out = lse_out;
+    a.ctx_lens = ctx_lens;
+    a.gammas = gammas;
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    DeviceScope dev(ctx->device);
+    if (dev.err != hipSuccess) return hip_fail(ctx, dev.err);
+    hipError_t e = few ? launch_attn_stream(a, st) : launch_attn_window(a, st);
+    if (e == hipSuccess && few && !a.direct) e = launch_attn_stream_merge(a, StreamLaunch{}, st);
     if (e != hipSuccess) return hip_fail(ctx, e);
     return RAPID_OK;
 }

@@ -116,3 +116,62 @@ def test_quotients_of_32_bits_fall_on_the_right_side():
     assert (np.where(keep, got, 0) <= 127).all() and (got[np.arange(128), np.arange(128), 0] == 127).all()
     gap = np.where(twice == den, 1.0, np.abs(twice - den) / (2.0 * den))
     assert np.where(keep & (got > 0), gap, 1.0).min() >= 2.0 ** -17
+
+
+def window_call(s, window=100, sinks=4, **kw):
+    lib = binding.load_library()
+    p = dict(ctx=ctx(), q=P, k=P, v=P, lens=P, table=P if s.page_size else None, out=P, ws=P, nbytes=1 << 40)
+    p.update(kw)
+    return lib.rapid_verify_attn_window(p["ctx"], s, window, sinks, p["q"], p["k"], p["v"], p["lens"], None, p["table"], p["out"], None,
+                                        p["ws"], p["nbytes"], None)
+
+
+@pytest.mark.parametrize("kw,want", [
+    (dict(batch=0), EINVAL), (dict(q_max=0), EINVAL), (dict(n_q_heads=7), EINVAL), (dict(gamma=5), EINVAL), (dict(max_ctx=4), EINVAL),
+    (dict(softmax_scale=0.0), EINVAL), (dict(softmax_scale=float("nan")), EINVAL), (dict(chunk_tokens=-1), EINVAL), (dict(n_pages=-1), EINVAL),
+    (dict(head_dim=96), EUNSUPPORTED), (dict(kv_token_stride=252), EALIGN), (dict(kv_head_stride=4), EALIGN), (dict(batch=70000), EUNSUPPORTED),
+    (dict(PAGED, page_size=24), EUNSUPPORTED), (dict(PAGED, max_pages=62), EINVAL), (dict(kv_token_stride=1 << 62), EUNSUPPORTED),
+    (dict(PAGED, max_pages=1 << 27, max_ctx=(1 << 30) + 1), EUNSUPPORTED), (dict(PAGED, max_pages=1 << 27, max_ctx=1 << 30, batch=64), EUNSUPPORTED),
+    (dict(PAGED, max_pages=1 << 26, max_ctx=1 << 30, q_max=1 << 29, gamma=0), EUNSUPPORTED),
+    (dict(PAGED, max_pages=1 << 26, max_ctx=1 << 30, q_max=1 << 24, gamma=0, batch=8, n_kv_heads=8), None),
+])
+def test_shapes_that_the_window_refuses(kw, want):
+    s = shape(**kw)
+    lib = binding.load_library()
+    if want is None:
+        assert window_call(s, ws=None) == EWORKSPACE and lib.rapid_verify_attn_window_workspace_bytes(None, s, 100, 4) > 0
+        return
+    assert window_call(s) == want
+    assert lib.rapid_verify_attn_window_workspace_bytes(None, s, 100, 4) == 0
+
+
+@pytest.mark.parametrize("Q", [5, 200])
+def test_arguments_that_the_window_refuses(Q):
+    s, lib = shape(q_max=Q, gamma=Q - 1), binding.load_library()
+    for key in ("ctx", "q", "k", "v", "lens", "out"):
+        assert window_call(s, **{key: None}) == EINVAL, key
+    for key in ("q", "k", "v", "out"):
+        assert window_call(s, **{key: P + 8}) == EALIGN, key
+    assert window_call(shape(q_max=Q, gamma=Q - 1, **PAGED), table=None) == EINVAL
+    for window, sinks in ((0, 4), (-1, 4), (100, -1)):
+        assert window_call(s, window, sinks) == EINVAL
+        assert lib.rapid_verify_attn_window_workspace_bytes(None, s, window, sinks) == 0
+    need = lib.rapid_verify_attn_window_workspace_bytes(None, s, 100, 4)
+    assert need > 0
+    for kw in (dict(ws=None), dict(ws=P + 16), dict(nbytes=need - 1)):
+        assert window_call(s, **kw) == EWORKSPACE, kw
+
+
+def test_workspaces_of_the_window_are_bounded_whatever_the_sizes():
+    """Partials are kept only where the row tiles do not fill the chip: never more than twice the chip's workgroups of the largest tile."""
+    lib = binding.load_library()
+    rng = np.random.default_rng(1)
+    for _ in range(300):
+        d, hkv, group = int(rng.choice([64, 128])), int(rng.choice([1, 2, 4, 8])), int(rng.choice([1, 4, 7, 8]))
+        ctx_max = int(2 ** rng.uniform(0, 20))
+        q = int(max(1, min(ctx_max, 2 ** rng.uniform(0, 15))))
+        s = binding.AttnShape(int(rng.integers(1, 20)), q, hkv * group, hkv, d, ctx_max, q - 1, 0.1, ctx_max * d * hkv, d, ctx_max * d, 0, 0, 0, 0, 0,
+                              0)
+        window, sinks = int(2 ** rng.uniform(0, 31)) - 1 or 1, int(2 ** rng.uniform(0, 31)) - 1
+        need = lib.rapid_verify_attn_window_workspace_bytes(None, s, window, sinks)
+        assert 256 <= need <= 2 * 256 * 384 * (d + 2) * 4 + 512
