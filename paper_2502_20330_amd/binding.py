@@ -197,9 +197,15 @@ def _strides(t: torch.Tensor):
                  for i, (n, s) in enumerate(zip(t.shape, t.stride())))
 
 
-def _sizes(*tensors):
-    """What a call's checks go by, for a key."""
-    return [None if t is None else (t.shape, t.stride(), t.dtype, t.device) for t in tensors]
+def _sizes(*tensors) -> bytes:
+    """What a call's checks go by, for a key: each tensor's type, device, sizes and strides."""
+    global _sizes
+    try:
+        from ._signature import sizes
+    except ImportError as e:
+        raise RapidError(-100, f"{_PKG}/_signature.so: {e}; build it with `python -m paper_2502_20330_amd.build`") from e
+    _sizes = sizes
+    return sizes(*tensors)
 
 
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
@@ -540,7 +546,7 @@ class Rapid:
         every sequence (ctx_lens counts them).  k_codes/v_codes: float8_e4m3fn or uint8 [B,Lmax,Hkv,d] (any batch/token/head
         strides) or, with page_table, [n_pages,page,Hkv,d]; k_scales/v_scales: float8_e8m0fnu or uint8 [B,Hkv,Lmax] or
         [n_pages,Hkv,page], rows of a multiple of 16."""
-        key = ("append", gamma, max_ctx, *_sizes(k_codes, v_codes, k_scales, v_scales, k_new, v_new, ctx_lens, gammas, page_table))
+        key = ("append", gamma, max_ctx, _sizes(k_codes, v_codes, k_scales, v_scales, k_new, v_new, ctx_lens, gammas, page_table))
         shape, layout = self._plans.get(key) or self._planned(
             key, self._plan_append, k_codes, v_codes, k_scales, v_scales, k_new, v_new, ctx_lens, gammas, page_table, gamma, max_ctx)
         rc = self.lib.rapid_kv_append_quant(self._ctx, shape, layout, k_new.data_ptr(), v_new.data_ptr(), ctx_lens.data_ptr(),
@@ -565,7 +571,7 @@ class Rapid:
             shape = (ctx_lens.numel(), int(rows), *k_codes.shape[2:])
             outs = tuple(torch.empty(shape, dtype=torch.bfloat16, device=self.device) for _ in range(2))
         k_out, v_out = outs
-        key = ("read", rows, gamma, max_ctx, *_sizes(k_codes, v_codes, k_scales, v_scales, k_out, v_out, ctx_lens, gammas, page_table))
+        key = ("read", rows, gamma, max_ctx, _sizes(k_codes, v_codes, k_scales, v_scales, k_out, v_out, ctx_lens, gammas, page_table))
         shape, layout = self._plans.get(key) or self._planned(
             key, self._plan_read, k_codes, v_codes, k_scales, v_scales, k_out, v_out, ctx_lens, gammas, page_table, rows, gamma, max_ctx)
         rc = self.lib.rapid_kv_read_quant(self._ctx, shape, layout, k_codes.data_ptr(), v_codes.data_ptr(), k_scales.data_ptr(),
@@ -592,7 +598,7 @@ class Rapid:
             out = torch.empty_like(q)
 
         key = ("attn", gamma, max_ctx, softmax_scale,
-               *_sizes(q, k_codes, v_codes, k_scales, v_scales, ctx_lens, gammas, page_table, out, lse_out))
+               _sizes(q, k_codes, v_codes, k_scales, v_scales, ctx_lens, gammas, page_table, out, lse_out))
         shape, layout = self._plans.get(key) or self._planned(key, self._plan_attn, q, k_codes, v_codes, k_scales, v_scales, ctx_lens, gammas,
                                                               page_table, out, lse_out, gamma, max_ctx, softmax_scale)
         args = (self._ctx, shape, layout, q.data_ptr(), k_codes.data_ptr(), v_codes.data_ptr(), k_scales.data_ptr(),
@@ -623,7 +629,7 @@ class Rapid:
         if out is None:
             out = torch.empty_like(q)
         key = ("prefix", gamma, max_prefix, max_ctx, softmax_scale,
-               *_sizes(q, k_cache, v_cache, ctx_lens, prefix_len, k_prefix, v_prefix, prefix_table, gammas, page_table, out, lse_out))
+               _sizes(q, k_cache, v_cache, ctx_lens, prefix_len, k_prefix, v_prefix, prefix_table, gammas, page_table, out, lse_out))
         shape, prefix = self._plans.get(key) or self._planned(
             key, self._plan_prefix, q, k_cache, v_cache, ctx_lens, prefix_len, k_prefix, v_prefix, prefix_table, gammas, page_table, out,
             lse_out, gamma, max_prefix, max_ctx, softmax_scale)
@@ -675,7 +681,7 @@ class Rapid:
         if out is None:
             out = torch.empty_like(q)
         key = ("window", gamma, window, sinks, max_ctx, softmax_scale,
-               *_sizes(q, k_cache, v_cache, ctx_lens, gammas, page_table, out, lse_out))
+               _sizes(q, k_cache, v_cache, ctx_lens, gammas, page_table, out, lse_out))
         shape, window, sinks = self._plans.get(key) or self._planned(
             key, self._plan_window, q, k_cache, v_cache, ctx_lens, gammas, page_table, out, lse_out, gamma, window, sinks, max_ctx, softmax_scale)
         args = (self._ctx, shape, window, sinks, q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), ctx_lens.data_ptr(), _dptr(gammas),
@@ -711,7 +717,7 @@ class Rapid:
         if q_out is None and q_new is not None:
             q_out = torch.empty(q_new.shape, dtype=torch.bfloat16, device=self.device)
         key = ("rope", gamma, max_ctx, interleaved, amplitude,
-               *_sizes(k_cache, v_cache, k_new, v_new, inv_freq, ctx_lens, q_new, q_out, positions, gammas, page_table))
+               _sizes(k_cache, v_cache, k_new, v_new, inv_freq, ctx_lens, q_new, q_out, positions, gammas, page_table))
         shape, rope = self._plans.get(key) or self._planned(
             key, self._plan_rope, k_cache, v_cache, None, None, k_new, v_new, inv_freq, ctx_lens, q_new, q_out, positions, gammas, page_table,
             gamma, max_ctx, interleaved, amplitude)
@@ -729,7 +735,7 @@ class Rapid:
         if q_out is None and q_new is not None:
             q_out = torch.empty(q_new.shape, dtype=torch.bfloat16, device=self.device)
         key = ("rope_quant", gamma, max_ctx, interleaved, amplitude,
-               *_sizes(k_codes, v_codes, k_scales, v_scales, k_new, v_new, inv_freq, ctx_lens, q_new, q_out, positions, gammas, page_table))
+               _sizes(k_codes, v_codes, k_scales, v_scales, k_new, v_new, inv_freq, ctx_lens, q_new, q_out, positions, gammas, page_table))
         shape, layout, rope = self._plans.get(key) or self._planned(
             key, self._plan_rope, k_codes, v_codes, k_scales, v_scales, k_new, v_new, inv_freq, ctx_lens, q_new, q_out, positions, gammas,
             page_table, gamma, max_ctx, interleaved, amplitude)
@@ -857,7 +863,7 @@ class Rapid:
         elif stats is None:
             stats = torch.empty((rows, self.lib.rapid_lm_head_stat_chunks(self._ctx, vocab, rows), 2), dtype=torch.float32,
                                 device=self.device)
-        key = ("head", *_sizes(h, w_codes, w_scales, logits, stats))
+        key = ("head", _sizes(h, w_codes, w_scales, logits, stats))
         ldz = self._plans.get(key) or self._planned(key, self._plan_head, h, w_codes, w_scales, logits, stats)
         args = (self._ctx, rows, hidden, vocab, h.data_ptr(), w_codes.data_ptr(), w_scales.data_ptr(), float(temperature), logits.data_ptr(),
                 ldz, _dptr(stats))

@@ -10,6 +10,7 @@ PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "librapid.so")
+SIGNATURE = os.path.join(PKG, "_signature.so")
 SOURCES = ["rapid_api.hip", "verify_attn.hip", "accept.hip", "accept_greedy.hip", "hbm_probe.hip", "lm_head.hip", "kv_cache.hip", "retrieve.hip",
            "kv_quant.hip", "attn_stream.hip", "attn_prefix.hip", "attn_window.hip", "kv_rope.hip", "quant_rows.hip", "lm_head_quant.hip"]
 # packed-fp32 instructions are switched off on purpose: some of their forms have given
@@ -36,9 +37,27 @@ def _compile(src: str, extra) -> str:
     return obj
 
 
+def build_signature() -> str:
+    """The binding's helper (csrc/signature.cpp), a Python module against torch's headers; no GPU code."""
+    import sysconfig
+
+    import torch
+    from torch.utils import cpp_extension
+    lib = os.path.join(os.path.dirname(torch.__file__), "lib")
+    cmd = ["g++", "-O2", "-std=c++17", "-shared", "-fPIC", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
+           *(f"-I{d}" for d in (*cpp_extension.include_paths(), sysconfig.get_paths()["include"])), os.path.join(CSRC, "signature.cpp"),
+           "-o", SIGNATURE, f"-L{lib}", "-ltorch_python", "-ltorch_cpu", "-lc10"]
+    r = subprocess.run(cmd, capture_output=True, text=True)
+    if r.returncode != 0:
+        raise RuntimeError(f"g++ failed for signature.cpp:\n{r.stdout}\n{r.stderr}")
+    return SIGNATURE
+
+
 def build(verbose: bool = False, extra_flags=()) -> str:
-    with ThreadPoolExecutor(max_workers=len(SOURCES)) as ex:
+    with ThreadPoolExecutor(max_workers=len(SOURCES) + 1) as ex:
+        signature = ex.submit(build_signature)
         objs = list(ex.map(lambda s: _compile(s, list(extra_flags)), SOURCES))
+        signature.result()
     cmd = ["hipcc", "--offload-arch=gfx950", "-shared", "-fPIC", "-o", LIB, *objs]
     r = subprocess.run(cmd, capture_output=True, text=True)
     if r.returncode != 0:
