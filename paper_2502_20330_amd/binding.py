@@ -833,22 +833,25 @@ class Rapid:
     def rapid_quant_rows(self, x, codes=None, scales=None):
         """Rows of x (bf16 [rows, cols], any row stride) as 8-bit integers: (codes int8 [rows, pitch], scales fp32 [rows]), pitch = cols
         rounded up to a multiple of 256 (zeros behind the row): what :meth:`rapid_lm_head_quant` takes for an output embedding."""
-        self._need(x.dim() == 2 and x.dtype == torch.bfloat16 and (x.stride(1) == 1 or x.shape[1] == 1), "x: bf16 [rows, cols], cols contiguous")
-        rows, cols = x.shape
-        pitch = -(-cols // 256) * 256
-        if codes is None:
-            codes = torch.empty((rows, pitch), dtype=torch.int8, device=self.device)
-        if scales is None:
-            scales = torch.empty(rows, dtype=torch.float32, device=self.device)
-        self._need(codes.dtype == torch.int8 and codes.shape == (rows, pitch) and codes.is_contiguous(),
-                   "codes: int8 [rows, cols rounded up to a multiple of 256], contiguous")
-        self._need(scales.dtype == torch.float32 and scales.shape == (rows,) and scales.is_contiguous(), "scales: fp32 [rows], contiguous")
-        self._need(x.device == codes.device == scales.device == self.device, f"a tensor is not on {self.device}")
-        rc = self.lib.rapid_quant_rows(self._ctx, rows, cols, x.data_ptr(), x.stride(0) if rows > 1 else cols, codes.data_ptr(),
-                                       scales.data_ptr(), _stream_ptr(self.device))
+        if codes is None or scales is None:
+            self._need(x.dim() == 2, "x: bf16 [rows, cols], cols contiguous")
+            codes = torch.empty((x.shape[0], -(-x.shape[1] // 256) * 256), dtype=torch.int8, device=self.device) if codes is None else codes
+            scales = torch.empty(x.shape[0], dtype=torch.float32, device=self.device) if scales is None else scales
+        key = ("rows", _sizes(x, codes, scales))
+        rows, cols, stride = self._plans.get(key) or self._planned(key, self._plan_rows, x, codes, scales)
+        rc = self.lib.rapid_quant_rows(self._ctx, rows, cols, x.data_ptr(), stride, codes.data_ptr(), scales.data_ptr(),
+                                       _stream_ptr(self.device))
         if rc:
             _check(self.lib, rc, self._ctx)
         return codes, scales
+
+    def _plan_rows(self, x, codes, scales):
+        self._need(x.dim() == 2 and x.dtype == torch.bfloat16 and (x.stride(1) == 1 or x.shape[1] == 1), "x: bf16 [rows, cols], cols contiguous")
+        rows, cols = x.shape
+        self._need(codes.dtype == torch.int8 and codes.shape == (rows, -(-cols // 256) * 256) and codes.is_contiguous(),
+                   "codes: int8 [rows, cols rounded up to a multiple of 256], contiguous")
+        self._need(scales.dtype == torch.float32 and scales.shape == (rows,) and scales.is_contiguous(), "scales: fp32 [rows], contiguous")
+        return rows, cols, x.stride(0) if rows > 1 else cols
 
     def rapid_lm_head_quant(self, h, w_codes, w_scales, *, temperature: float = 1.0, want_stats: bool = True, logits=None, stats=None):
         """:meth:`rapid_lm_head` on an output embedding in 8-bit integers (:meth:`rapid_quant_rows` of it): h bf16 [rows, hidden], w_codes

@@ -66,96 +66,87 @@ __device__ __forceinline__ uint32_t largest_of(const u32x4& v, bool finite)
     return m;
 }
 
-// Grid: (blocks of T rows, sequences, parts of the heads).  Units of a workgroup: (row, head), U of them a thread at a time.
-template <int D, bool QUANT, bool ADJACENT, int T, int U>
-__global__ void __launch_bounds__(256) kv_append_rope(KvRopeLaunch a)
+constexpr int kMostThreads = 512;
+
+// The 16 elements of a kv head that this lane holds; `codes` and `scale` are the head's.
+template <bool QUANT, int LPH>
+__device__ __forceinline__ void store_row(const Sixteen& y, uint8_t* codes, uint8_t* scale, int lo, int hi, int j)
 {
-    constexpr int LPH = D / 16, UNITS = 256 / LPH;
-    __shared__ float2 turns[T][D / 2];
+    if constexpr (!QUANT) {
+        *reinterpret_cast<u32x4*>(codes + lo * 2) = y.lo;
+        *reinterpret_cast<u32x4*>(codes + hi * 2) = y.hi;
+    } else {
+        uint32_t m = row_max<LPH>(max_u16x2(largest_of(y.lo, false), largest_of(y.hi, false)));
+        const bool large = m >= kLargeBits;
+        if (large) m = row_max<LPH>(max_u16x2(largest_of(y.lo, true), largest_of(y.hi, true)));
+        const int k = scale_exponent(m);
+        const float inv = power_of_two(-k);
+        u32x2 c_lo = {plain_codes_of(y.lo[0], y.lo[1], inv), plain_codes_of(y.lo[2], y.lo[3], inv)};
+        u32x2 c_hi = {plain_codes_of(y.hi[0], y.hi[1], inv), plain_codes_of(y.hi[2], y.hi[3], inv)};
+        if (large) {
+            c_lo = u32x2{codes_of(y.lo[0], y.lo[1], inv), codes_of(y.lo[2], y.lo[3], inv)};
+            c_hi = u32x2{codes_of(y.hi[0], y.hi[1], inv), codes_of(y.hi[2], y.hi[3], inv)};
+        }
+        *reinterpret_cast<u32x2*>(codes + lo) = c_lo;
+        *reinterpret_cast<u32x2*>(codes + hi) = c_hi;
+        if (j == 0) *scale = (uint8_t)(k + 127);
+    }
+}
+
+// Grid: (rows, sequences).  A workgroup's units are the heads of a row, of q, k and v.
+template <int D, bool QUANT, bool ADJACENT>
+__global__ void __launch_bounds__(kMostThreads) kv_append_rope(KvRopeLaunch a)
+{
+    constexpr int LPH = D / 16;
+    const int at_a_time = blockDim.x / LPH;
+    __shared__ float2 turns[D / 2];
     const KvQuantLaunch& c = a.cache;
-    const int b = blockIdx.y, i0 = blockIdx.x * T, tid = threadIdx.x;
-    const int Q = min(max(c.gammas ? c.gammas[b] : c.gamma, 0), c.Qmax - 1) + 1;
-    if (i0 >= Q) return;
-    const int first = max(min(c.ctx_lens[b], c.max_ctx), 0) - Q;          // token of row 0; negative: rows without a token
-    if (first + min(i0 + T, Q) <= 0) return;
-    const int h0 = blockIdx.z * a.heads_each, nh = min(a.Hq + 2 * c.Hkv - h0, a.heads_each);
-    const int j = tid % LPH, half = a.rot / 2;
+    const int b = blockIdx.y, i = blockIdx.x, tid = threadIdx.x;
+    const int heads = a.Hq + 2 * c.Hkv, j = tid % LPH, half = a.rot / 2;
     const bool turned = j < a.rot / 16;
     const int lo = turned && !ADJACENT ? 8 * j : 16 * j, hi = turned && !ADJACENT ? half + 8 * j : 16 * j + 8;
-
-    for (int u0 = tid / LPH, start = 0; start < T * nh; start += U * UNITS, u0 += U * UNITS) {
-        Sixteen x[U];
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int unit = min(u0 + u * UNITS, T * nh - 1);
-            const int r = T == 1 ? 0 : unit / nh, h = h0 + unit - r * nh;
-            const int64_t row = (int64_t)b * c.Qmax + min(i0 + r, Q - 1);
-            const uint16_t* src = h < a.Hq ? a.q + row * a.q_stride + (int64_t)h * D
-                                  : h < a.Hq + c.Hkv ? a.k + row * a.k_stride + (int64_t)(h - a.Hq) * D
-                                                     : a.v + row * a.v_stride + (int64_t)(h - a.Hq - c.Hkv) * D;
-            x[u].lo = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(src + lo));
-            x[u].hi = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(src + hi));
-        }
-        if (start == 0) {
-            for (int t = tid; t < T * half; t += 256) {
-                const int r = T == 1 ? 0 : t / half, p = t - r * half, i = min(i0 + r, Q - 1);
-                const int pos = a.positions ? a.positions[(int64_t)b * c.Qmax + i] : first + i;
-                turns[r][p] = turn_of(pos, a.inv_freq[p], a.amplitude);
-            }
-            __syncthreads();
-        }
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int unit = u0 + u * UNITS;
-            const int r = T == 1 ? 0 : unit / nh, h = h0 + unit - r * nh, i = i0 + r, tok = first + i;
-            if (unit >= T * nh || i >= Q || tok < 0) continue;             // (all lanes of a head alike)
-            const bool value = h >= a.Hq + c.Hkv;
-            const Sixteen y = turned && !value ? rotated<ADJACENT>(x[u], &turns[r][8 * j]) : x[u];
-            if (h < a.Hq) {
-                uint16_t* dst = a.q_out + (((int64_t)b * c.Qmax + i) * a.Hq + h) * D;
-                *reinterpret_cast<u32x4*>(dst + lo) = y.lo;
-                *reinterpret_cast<u32x4*>(dst + hi) = y.hi;
-                continue;
-            }
+    const int64_t row = (int64_t)b * c.Qmax + i;
+    const uint16_t *q = a.q + row * a.q_stride, *k = a.k + row * a.k_stride, *v = a.v + row * a.v_stride;
+    Sixteen x;
+    auto load = [&](int h) {
+        const uint16_t* src = h < a.Hq ? q + (int64_t)h * D : h < a.Hq + c.Hkv ? k + (int64_t)(h - a.Hq) * D : v + (int64_t)(h - a.Hq - c.Hkv) * D;
+        x.lo = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(src + lo));
+        x.hi = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(src + hi));
+    };
+    const float freq = tid < half ? a.inv_freq[tid] : 0.f;
+    const int Q = min(max(c.gammas ? c.gammas[b] : c.gamma, 0), c.Qmax - 1) + 1;
+    const int tok = max(min(c.ctx_lens[b], c.max_ctx), 0) - Q + i;        // negative: a row without a token
+    if (i >= Q || tok < 0) return;
+    const RowPlace at = place(c, b, tok, 0);
+    load(min(tid / LPH, heads - 1));
+    if (tid < half) turns[tid] = turn_of(a.positions ? a.positions[row] : tok, freq, a.amplitude);
+    __syncthreads();
+    for (int h = tid / LPH; h < heads; h += at_a_time) {                       // (all lanes of a head alike)
+        const bool value = h >= a.Hq + c.Hkv;
+        const Sixteen y = turned && !value ? rotated<ADJACENT>(x, &turns[8 * j]) : x;
+        if (h + at_a_time < heads) load(h + at_a_time);
+        if (h < a.Hq) {
+            uint16_t* dst = a.q_out + (row * a.Hq + h) * D;
+            *reinterpret_cast<u32x4*>(dst + lo) = y.lo;
+            *reinterpret_cast<u32x4*>(dst + hi) = y.hi;
+        } else {
             const int kv = h - a.Hq - (value ? c.Hkv : 0);
             const KvQuantSide& side = c.side[value];
-            const RowPlace at = place(c, b, tok, kv);
-            if constexpr (!QUANT) {
-                *reinterpret_cast<u32x4*>(side.codes + at.codes + lo * 2) = y.lo;
-                *reinterpret_cast<u32x4*>(side.codes + at.codes + hi * 2) = y.hi;
-            } else {
-                uint32_t m = row_max<LPH>(max_u16x2(largest_of(y.lo, false), largest_of(y.hi, false)));
-                const bool large = m >= kLargeBits;
-                if (large) m = row_max<LPH>(max_u16x2(largest_of(y.lo, true), largest_of(y.hi, true)));
-                const int k = scale_exponent(m);
-                const float inv = power_of_two(-k);
-                u32x2 c_lo = {plain_codes_of(y.lo[0], y.lo[1], inv), plain_codes_of(y.lo[2], y.lo[3], inv)};
-                u32x2 c_hi = {plain_codes_of(y.hi[0], y.hi[1], inv), plain_codes_of(y.hi[2], y.hi[3], inv)};
-                if (large) {
-                    c_lo = u32x2{codes_of(y.lo[0], y.lo[1], inv), codes_of(y.lo[2], y.lo[3], inv)};
-                    c_hi = u32x2{codes_of(y.hi[0], y.hi[1], inv), codes_of(y.hi[2], y.hi[3], inv)};
-                }
-                *reinterpret_cast<u32x2*>(side.codes + at.codes + lo) = c_lo;
-                *reinterpret_cast<u32x2*>(side.codes + at.codes + hi) = c_hi;
-                if (j == 0) side.scales[at.scales] = (uint8_t)(k + 127);
-            }
+            store_row<QUANT, LPH>(y, side.codes + at.codes + kv * c.hstride, side.scales + at.scales + kv * c.shstride, lo, hi, j);
         }
     }
 }
 
+// A row of q, k and v to a workgroup, with as many threads as its heads take, or the half, third .. of them that is at most 512.  The more workgroups a compute
+// unit has, the more of their waits for lengths, pages and angles pass under others' loads, but a thread that has a second head to do waits twice.
+// 64K rows of 32 / 8 / 8 heads of 128, which take 384 threads: 287 us with these, 295 with 256, 301 with 128, 310 with 64 (two rows to a workgroup: 307, four
+// 317, eight 334); 72 such rows 3.4, 4.9 with 64; 2800 rows of 16 / 8 / 8 heads of 64 in 8 bits, which take 128: 8.5, 10.2 with 256, 13.7 with 384.
 template <int D, bool QUANT, bool ADJACENT>
-hipError_t launch(KvRopeLaunch a, hipStream_t stream)
+hipError_t launch(const KvRopeLaunch& a, hipStream_t stream)
 {
-    constexpr int UNITS = 256 / (D / 16);
-    const int heads = a.Hq + 2 * a.cache.Hkv;
-    if ((int64_t)a.cache.B * a.cache.Qmax >= 2048) {
-        a.heads_each = heads;
-        hipLaunchKernelGGL((kv_append_rope<D, QUANT, ADJACENT, 4, 4>), dim3((a.cache.Qmax + 3) / 4, a.cache.B, 1), dim3(256), 0, stream, a);
-    } else {
-        a.heads_each = heads < UNITS ? heads : UNITS;
-        hipLaunchKernelGGL((kv_append_rope<D, QUANT, ADJACENT, 1, 1>), dim3(a.cache.Qmax, a.cache.B, (heads + a.heads_each - 1) / a.heads_each),
-                           dim3(256), 0, stream, a);
-    }
+    const int all = (a.Hq + 2 * a.cache.Hkv) * (D / 16), parts = (all + kMostThreads - 1) / kMostThreads;
+    const int threads = ((all + parts - 1) / parts + 63) / 64 * 64;
+    hipLaunchKernelGGL((kv_append_rope<D, QUANT, ADJACENT>), dim3(a.cache.Qmax, a.cache.B), dim3(threads), 0, stream, a);
     return hipGetLastError();
 }
 template <int D>

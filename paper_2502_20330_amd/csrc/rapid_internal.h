@@ -181,7 +181,7 @@ struct KvRopeLaunch {
     const int32_t* positions;   // [B][Qmax] or null: a row's token
     int64_t q_stride, k_stride, v_stride;
     KvQuantLaunch cache;        // strides in bytes; without scales: bf16, whose bytes stand for the codes
-    int32_t Hq, rot, adjacent, heads_each;
+    int32_t Hq, rot, adjacent;
     float amplitude;
 };
 hipError_t launch_kv_append_rope(const KvRopeLaunch& a, hipStream_t stream);
