@@ -28,7 +28,7 @@ def check_rows(x, codes, scales, cols):
 
 
 @pytest.mark.parametrize("rows,cols", [(1, 8), (3, 256), (2, 264), (5, 2048), (4, 2056), (70, 4096), (9, 4104), (6, 8192), (3, 8200), (2, 20000),
-                                       (1, 131072), (1000, 904)])
+                                       (1, 131072), (1000, 904), (3, 16384), (2, 16392), (7, 12000)])
 def test_rows_of_every_length(rows, cols):
     rng = np.random.default_rng(rows + cols)
     x = qu.bf16(rng, (rows, cols + 16)) * torch.from_numpy(2.0 ** rng.integers(-30, 30, (rows, 1))).to(torch.bfloat16)
