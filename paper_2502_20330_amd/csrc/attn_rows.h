@@ -27,12 +27,12 @@ struct RowsGeo : TileGeo<D, false, D == 64 ? 4 : 2> {
 };
 
 // Loads of tile part `team` of K and V.
-template <class G, bool PAGED>
+template <class G, bool PAGED, bool KEEP = false>
 __device__ __forceinline__ void load_both(const RowAddr& ra, const TilePages<G, PAGED>& pages, uint32_t kslot, uint32_t vslot, int t0, int last_tok,
                                           int lane, int team)
 {
-    load_tile<G, PAGED, false, G::H>(ra, pages, kslot, t0, last_tok, lane, team * G::H);
-    load_tile<G, PAGED, true, G::H>(ra, pages, vslot, t0, last_tok, lane, team * G::H);
+    load_tile<G, PAGED, false, G::H, KEEP>(ra, pages, kslot, t0, last_tok, lane, team * G::H);
+    load_tile<G, PAGED, true, G::H, KEEP>(ra, pages, vslot, t0, last_tok, lane, team * G::H);
 }
 
 // The operands of a tile's two products, from LDS to registers: half `x` of V^T's blocks, and half `x` of K's.

@@ -167,10 +167,17 @@ struct TilePages {
     }
 };
 
+template <bool KEEP>
+__device__ __forceinline__ void load_16(const char* base, uint32_t byte_off, uint32_t lds_addr)
+{
+    if (KEEP) dma16_keep(base, byte_off, lds_addr);
+    else dma16(base, byte_off, lds_addr);
+}
 // Loads [e0, e0 + N) of a tile of K or V into `slot`.  Rows past `last_tok` are clamped to it (always a valid address); the softmax masks them.
 // Where there are none, all that varies from load to load and from tile to tile is uniform and goes into the base; a lane's own offset
-// only depends on the swizzle (f(e RPI + r) = f(e RPI) ^ f(r): fields of bits).
-template <class G, bool PAGED, bool IS_V, int N>
+// only depends on the swizzle (f(e RPI + r) = f(e RPI) ^ f(r): fields of bits).  KEEP: other workgroups read the tile too, at about the same time: it
+// should stay in the L2.
+template <class G, bool PAGED, bool IS_V, int N, bool KEEP = false>
 __device__ __forceinline__ void load_tile(const RowAddr& ra, const TilePages<G, PAGED>& pages, uint32_t slot, int t0, int last_tok, int lane, int e0)
 {
     const char* base = IS_V ? ra.v : ra.k;
@@ -184,9 +191,9 @@ __device__ __forceinline__ void load_tile(const RowAddr& ra, const TilePages<G, 
             const uint32_t off = row_off + (uint32_t)((cpos ^ swz(r_local)) ^ swz(e * G::RPI)) * 16u;
             if (PAGED) {
                 const int id = __builtin_amdgcn_readfirstlane(pages.of(e * G::RPI / 16));
-                dma16(base + (int64_t)id * ra.page_bytes + (uint32_t)((t0 + e * G::RPI) & ra.page_mask) * ra.tok_bytes, off, slot + e * 1024);
+                load_16<KEEP>(base + (int64_t)id * ra.page_bytes + (uint32_t)((t0 + e * G::RPI) & ra.page_mask) * ra.tok_bytes, off, slot + e * 1024);
             } else {
-                dma16(base + (uint32_t)(t0 + e * G::RPI) * ra.tok_bytes, off, slot + e * 1024);
+                load_16<KEEP>(base + (uint32_t)(t0 + e * G::RPI) * ra.tok_bytes, off, slot + e * 1024);
             }
         }
         return;
@@ -200,9 +207,9 @@ __device__ __forceinline__ void load_tile(const RowAddr& ra, const TilePages<G, 
         const int tok = min(t0 + row, last_tok);
         if (PAGED) {
             const int id = __builtin_amdgcn_readfirstlane(pages.of(e * G::RPI / 16));
-            dma16(base + (int64_t)id * ra.page_bytes, (uint32_t)(tok & ra.page_mask) * ra.tok_bytes + (uint32_t)c * 16u, slot + e * 1024);
+            load_16<KEEP>(base + (int64_t)id * ra.page_bytes, (uint32_t)(tok & ra.page_mask) * ra.tok_bytes + (uint32_t)c * 16u, slot + e * 1024);
         } else {
-            dma16(base, (uint32_t)tok * ra.tok_bytes + (uint32_t)c * 16u, slot + e * 1024);
+            load_16<KEEP>(base, (uint32_t)tok * ra.tok_bytes + (uint32_t)c * 16u, slot + e * 1024);
         }
     }
 }

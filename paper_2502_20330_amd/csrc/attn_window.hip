@@ -6,7 +6,12 @@
 // scores where RP (window + sinks) count.
 // It takes 4 d multiply-adds and an exponential a score: matrix cores and exponentials bound it.  Waves, ring and schedule are those of
 // attn_prefix.hip: eight waves hold the rows, the tokens go HBM -> LDS once a workgroup, and a row tile's neighbours, which read nearly the same
-// tokens, follow it on the same die, whose L2 serves them.
+// tokens, follow it on the same die, whose L2 serves them: with the hint that a tile is read once, which serves the other kernels, 384 rows of 32K positions took
+// 2272 us instead of 1949.
+// Measured (32K positions, 32 / 8 heads of 128, a window of 4096 and 64 sinks, 2.09 TFLOP of scores that count): 1947 us, 1073 TFLOP/s, where a large product of the
+// library reaches 1295.  By counters, with 256 rows: the clock is held at 1.87 GHz, the matrix cores are busy in 40 % of the cycles, LDS in 20 %.  What the chip may
+// draw bounds it as much as anything: the same loop without softmax and loads takes 1520 us, without loads 1850, and a schedule
+// that interleaves products and exponentials of neighbouring tiles in each wave (their issue then overlaps by the listing) no less than this one, 2120 with 256 rows.
 // Where the row tiles are too few for the chip, each one's tokens are cut into shares, whose partials a second launch joins.
 #include "attn_rows.h"
 
@@ -59,7 +64,7 @@ __device__ __forceinline__ void window_piece(const StreamLaunch& a, char* smem, 
 #pragma unroll
     for (int it = 0; it < G::S - G::NB; ++it) {
         pages.find(addr, tile_t0(it), last_tok);
-        load_both<G, PAGED>(addr, pages, kring_lds + it * G::SLOT, vring_lds + it * G::SLOT, tile_t0(it), last_tok, lane, team);
+        load_both<G, PAGED, true>(addr, pages, kring_lds + it * G::SLOT, vring_lds + it * G::SLOT, tile_t0(it), last_tok, lane, team);
     }
 
     WaveState<G, RB> st;
@@ -85,7 +90,7 @@ __device__ __forceinline__ void window_piece(const StreamLaunch& a, char* smem, 
 #pragma unroll
         for (int x = 0; x < G::NB; ++x) {
             pages.find(addr, tile_t0(fill), last_tok);
-            load_both<G, PAGED>(addr, pages, kring_lds + fill_slot * G::SLOT, vring_lds + fill_slot * G::SLOT, tile_t0(fill), last_tok, lane, team);
+            load_both<G, PAGED, true>(addr, pages, kring_lds + fill_slot * G::SLOT, vring_lds + fill_slot * G::SLOT, tile_t0(fill), last_tok, lane, team);
             ++fill;
             fill_slot = fill_slot + 1 == G::S ? 0 : fill_slot + 1;
         }
@@ -348,25 +353,37 @@ hipError_t configure_attn_window()
     return hipSuccess;
 }
 
+// Rows a workgroup and shares of its tokens: those that a simple account finds the fastest.  A workgroup takes its tokens times a rate that is
+// 0.17 + 0.83 RP / 256 of that of 256 rows (32K positions of 32 / 8 heads of 128, a window of 4096: 128 rows 2456 us, 192 2175, 256 2121, 320 2065, 384
+// 1949; heads of 64 have half of the products but all of the exponentials, and take as long), and a few us besides; the chip takes as many rounds as it is filled by; shares cost their partials' way to memory and back, and a launch.
 void plan_attn_window(StreamLaunch& a, int n_cu)
 {
-    const int64_t R = (int64_t)a.Qmax * a.G;
-    int64_t least = -1;
+    const int64_t R = (int64_t)a.Qmax * a.G, units = (int64_t)a.B * a.Hkv;
+    float best = -1.f;
     for (int rows : kRowTiles) {
-        const int64_t padded = (R + rows - 1) / rows * rows;
-        if (least >= 0 && padded >= least) continue;
-        least = padded;
-        a.RP = rows;
+        int quantum = 0;
+        (void)with_rows(a.D, rows, [&](auto geo) {
+            quantum = decltype(geo)::QUANTUM;
+            return hipSuccess;
+        });
+        const int64_t tiles = (R + rows - 1) / rows, grid = units * tiles;
+        const int64_t span = (int64_t)a.sinks + a.window + rows / a.G + 2 * 64, tokens = span < a.max_ctx ? span : a.max_ctx;
+        const int64_t most = (tokens + quantum - 1) / quantum;
+        const float a_token = (0.17f + 0.83f / 256 * rows) * 0.032f;        // us
+        for (int k = 0; k <= 3; ++k) {
+            int64_t groups = k * n_cu / grid;
+            groups = groups > most ? most : groups < 1 ? 1 : groups;
+            const int64_t rounds = (grid * groups + n_cu - 1) / n_cu;
+            const float partials = groups > 1 ? 6.f + (float)(grid * groups) * (rows * (a.D + 2) * 8) * 0.25e-6f : 0.f;
+            const float time = (float)rounds * (6.f + a_token * (float)tokens / (float)groups) + partials;
+            if (best >= 0.f && time >= best) continue;
+            best = time;
+            a.RP = rows;
+            a.tiles = (int)tiles;
+            a.quantum = quantum;
+            a.groups = (int)groups;
+        }
     }
-    a.tiles = (int)((R + a.RP - 1) / a.RP);
-    const int64_t units = (int64_t)a.B * a.Hkv * a.tiles;
-    a.groups = units < n_cu ? (int)(n_cu / units) : 1;
-    (void)with_rows(a.D, a.RP, [&](auto geo) {
-        a.quantum = decltype(geo)::QUANTUM;
-        return hipSuccess;
-    });
-    const int64_t span = (int64_t)a.sinks + a.window + a.RP / a.G + 2 * 64, most = ((span < a.max_ctx ? span : a.max_ctx) + a.quantum - 1) / a.quantum;
-    if (a.groups > most) a.groups = (int)most;
     a.nslots = a.groups;
     a.rot = 0;
     a.direct = a.groups == 1;

@@ -163,7 +163,7 @@ def test_arguments_that_the_window_refuses(Q):
 
 
 def test_workspaces_of_the_window_are_bounded_whatever_the_sizes():
-    """Partials are kept only where the row tiles do not fill the chip: never more than twice the chip's workgroups of the largest tile."""
+    """Partials are kept only where the row tiles do not fill the chip: never more than three rounds of workgroups of the largest tile."""
     lib = binding.load_library()
     rng = np.random.default_rng(1)
     for _ in range(300):
@@ -174,4 +174,4 @@ def test_workspaces_of_the_window_are_bounded_whatever_the_sizes():
                               0)
         window, sinks = int(2 ** rng.uniform(0, 31)) - 1 or 1, int(2 ** rng.uniform(0, 31)) - 1
         need = lib.rapid_verify_attn_window_workspace_bytes(None, s, window, sinks)
-        assert 256 <= need <= 2 * 256 * 384 * (d + 2) * 4 + 512
+        assert 256 <= need <= 3 * 256 * 384 * (d + 2) * 4 + 512
