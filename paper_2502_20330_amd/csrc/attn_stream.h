@@ -35,6 +35,7 @@ struct StreamLaunch {
 constexpr int kStreamRows = 96;      // packed rows that the streaming kernel takes
 // Fill the plan (RP .. direct) from the shape and the source's layout.
 void plan_attn_stream(StreamLaunch& a, int n_cu);
+void plan_attn_stream_window(StreamLaunch& a, int n_cu);                         // a window of at most kStreamRows: `groups` shares of each sequence
 void plan_attn_prefix(StreamLaunch& a, int n_cu);
 // Windowed attention of more rows than kStreamRows (attn_window.hip): `groups` shares of a row tile's tokens; direct where that is one.
 void plan_attn_window(StreamLaunch& a, int n_cu);

@@ -76,13 +76,10 @@ __device__ __forceinline__ WindowSpan window_span(const StreamLaunch& a, int b, 
 {
     return WindowSpan(L - seq_queries(a, b), L - 1, a.window, a.sinks, kWindowStep);
 }
-// What a sequence has for the workgroups to divide.
-template <bool WINDOW>
-__device__ __forceinline__ int shared_len(const StreamLaunch& a, int b)
-{
-    const int L = seq_len(a, b);
-    return WINDOW ? window_span(a, b, L).len : L;
-}
+// Into how many shares a sequence is cut: `groups`, of a quantum at least.
+__device__ __forceinline__ int window_shares(const StreamLaunch& a, int len) { return min(a.groups, (len + a.quantum - 1) / a.quantum); }
+// The partials of (sequence b, kv head h, packed row `row`), RP slots apart.
+__device__ __forceinline__ int64_t window_slot(const StreamLaunch& a, int b, int h, int row) { return ((int64_t)h * a.B + b) * a.groups * a.RP + row; }
 template <bool WINDOW>
 __device__ __forceinline__ int tile_token(const Piece& w, int x) { return WINDOW && x >= w.joint ? x + w.gap : x; }
 
@@ -401,41 +398,48 @@ __device__ __forceinline__ void write_missing_rows(const StreamLaunch& a, int b,
 }
 
 // Grid: one workgroup per (kv head, share).  Partials: [kv head][g + b], which no two pieces of a head share.  Direct: per (kv head, sequence).
-template <class G, bool PAGED, bool WINDOW = false>
+template <class G, bool PAGED>
 __device__ __forceinline__ void stream_share(const StreamLaunch& a, char* smem, int g, int len, int rt = 0)
 {                                                        // len: of sequence `lane`, 0 where there is none
     const int h = __builtin_amdgcn_readfirstlane(a.rot ? (blockIdx.x + g) % a.Hkv : blockIdx.x);     // (base addresses go through scalar registers)
     if (a.direct) {
         const int L = __builtin_amdgcn_readfirstlane(seq_len(a, g));
         write_missing_rows<G>(a, g, h, L);
-        const int all = WINDOW ? window_span(a, g, L).len : L;
-        if (L > 0) stream_piece<G, PAGED, WINDOW>(a, smem, g, h, L, 0, all, 0, 0);
+        if (L > 0) stream_piece<G, PAGED, false>(a, smem, g, h, L, 0, L, 0, 0);
         return;
     }
-    for_each_piece(a, g, threadIdx.x & 63, len, G::QUANTUM, [&](int b, int all, int c0, int c1) {
-        const int L = WINDOW ? __builtin_amdgcn_readfirstlane(seq_len(a, b)) : all;
-        stream_piece<G, PAGED, WINDOW>(a, smem, b, h, L, c0, c1, ((int64_t)(h * a.tiles + rt) * a.nslots + g + b) * G::RP, rt * G::RP);
+    for_each_piece(a, g, threadIdx.x & 63, len, G::QUANTUM, [&](int b, int L, int c0, int c1) {
+        stream_piece<G, PAGED, false>(a, smem, b, h, L, c0, c1, ((int64_t)(h * a.tiles + rt) * a.nslots + g + b) * G::RP, rt * G::RP);
         wait_loads<0>();                                 // the partial's stores are out of the load account
-    }, [&](int b) { return shared_len<WINDOW>(a, b); });
+    });
 }
-template <bool WINDOW = false>
 __device__ __forceinline__ int first_len(const StreamLaunch& a)
 {
     const int lane = threadIdx.x & 63;
-    return !a.direct && lane < a.B ? shared_len<WINDOW>(a, lane) : 0;
-}
-// bf16, a window.
-template <class G, bool PAGED>
-__global__ void __launch_bounds__(G::NW * 64) attn_stream_window(StreamLaunch a)
-{
-    extern __shared__ __attribute__((aligned(1024))) char smem[];
-    stream_share<G, PAGED, true>(a, smem, blockIdx.y, first_len<true>(a));
+    return !a.direct && lane < a.B ? seq_len(a, lane) : 0;
 }
 template <class G, bool PAGED>
 __global__ void __launch_bounds__(G::NW * 64) attn_stream(StreamLaunch a)
 {
     extern __shared__ __attribute__((aligned(1024))) char smem[];
     stream_share<G, PAGED>(a, smem, blockIdx.y, first_len(a));
+}
+// bf16, a window: one workgroup per (kv head, sequence, share).  What sequences have is alike, so each is cut by itself, and a workgroup need not look
+// at the others.
+template <class G, bool PAGED>
+__global__ void __launch_bounds__(G::NW * 64) attn_stream_window(StreamLaunch a)
+{
+    extern __shared__ __attribute__((aligned(1024))) char smem[];
+    const int y = blockIdx.y, b = __builtin_amdgcn_readfirstlane(y / a.groups), share = y - b * a.groups;
+    const int h = __builtin_amdgcn_readfirstlane(a.rot ? (blockIdx.x + y) % a.Hkv : blockIdx.x);
+    const int L = __builtin_amdgcn_readfirstlane(seq_len(a, b));
+    if (a.direct) write_missing_rows<G>(a, b, h, L);
+    if (L <= 0) return;
+    const int len = window_span(a, b, L).len, quanta = (len + G::QUANTUM - 1) / G::QUANTUM, shares = window_shares(a, len);
+    if (share >= shares) return;
+    const int c0 = (int)((int64_t)quanta * share / shares) * G::QUANTUM;
+    const int c1 = min((int)((int64_t)quanta * (share + 1) / shares) * G::QUANTUM, len);
+    stream_piece<G, PAGED, true>(a, smem, b, h, L, c0, c1, window_slot(a, b, h, 0) + (int64_t)share * G::RP, 0);
 }
 
 // How a prefix and the sequences' own tokens divide the `units` workgroups of a kv head: by what there is to read, of the prefix once for each row tile.
@@ -501,12 +505,11 @@ struct Partials {
 struct Place {
     int before = 0, cost = 0, total = 0, n = 0;          // n: sequences that have tokens
 };
-template <bool WINDOW>
 __device__ __forceinline__ Place find_place(const StreamLaunch& a, int b, int lane, int len)
 {                                                        // len: of sequence `lane`, 0 where there is none
     Place p;
     for (int b0 = 0; b0 < a.B; b0 += 64) {
-        if (b0) len = b0 + lane < a.B ? shared_len<WINDOW>(a, b0 + lane) : 0;
+        if (b0) len = b0 + lane < a.B ? seq_len(a, b0 + lane) : 0;
         const int mine = seq_cost(len, b0 + lane, a.quantum);
         const int end = p.total + scan_costs(mine);
         if (b >= b0 && b < b0 + 64) {
@@ -580,7 +583,7 @@ __device__ __forceinline__ int64_t first_slot(const StreamLaunch& a, int h, int 
 
 // One workgroup of D threads per (sequence, kv head, packed row): out = sum 2^(m_s - M) O_s / sum 2^(m_s - M) l_s, over the row's partials of the
 // prefix and of its own tokens.
-template <int D, bool PREFIX, bool WINDOW>
+template <int D, bool PREFIX>
 __global__ void __launch_bounds__(D) attn_stream_merge(StreamLaunch a, StreamLaunch prefix)
 {
     const int row = blockIdx.x, h = blockIdx.y, b = blockIdx.z;
@@ -594,14 +597,14 @@ __global__ void __launch_bounds__(D) attn_stream_merge(StreamLaunch a, StreamLau
     // All that can be asked for is asked for at once: the lengths, the first block of a single sequence (the prefix is one) before its length is known, the
     // other's as soon as the lengths are there.
     const int lane = d & 63;
-    const int len = lane < a.B ? shared_len<WINDOW>(a, lane) : 0, prefix_len = PREFIX ? seq_len(prefix, 0) : 0;
+    const int len = lane < a.B ? seq_len(a, lane) : 0, prefix_len = PREFIX ? seq_len(prefix, 0) : 0;
     const bool there = seq_len(a, b) > 0;                 // (a sequence without tokens has no rows, behind a prefix either)
     const int prefix_row = b * a.Qmax * a.G + row;
     PartialBlock x, y;
     const int64_t x_slot = PREFIX ? first_slot(prefix, h, prefix_row) : 0;
     if (PREFIX) x.load<D>(prefix, x_slot, prefix.nslots, d);
     if (a.B == 1) y.load<D>(a, first_slot(a, h, row), a.nslots, d);
-    const Place at = find_place<WINDOW>(a, b, lane, len);
+    const Place at = find_place(a, b, lane, len);
     PairGroups groups{a.groups, 0};
     if (PREFIX) groups = pair_groups(a, prefix, at.total, at.n, prefix_len);
     const Partials own = find_partials(a, at, groups.own, b, h, row);
@@ -618,6 +621,25 @@ __global__ void __launch_bounds__(D) attn_stream_merge(StreamLaunch a, StreamLau
     const __bf16 o = (__bf16)(r.den == 0.f ? 0.f : num / r.den);
     *dst = __builtin_bit_cast(uint16_t, o);
     if (a.lse_out && d == 0) a.lse_out[lse_index(a, b, h, row)] = (r.M + log2f(r.den)) * 0.6931471805599453f;
+}
+
+// The same for a window's few rows, whose partials lie where they lie whatever the lengths are.
+template <int D>
+__global__ void __launch_bounds__(D) attn_window_rows_merge(StreamLaunch a, StreamLaunch)
+{
+    const int row = blockIdx.x, h = blockIdx.y, b = blockIdx.z, d = threadIdx.x;
+    const int64_t slot = window_slot(a, b, h, row);
+    PartialBlock y;
+    y.load<D>(a, slot, a.groups, d);
+    const int L = seq_len(a, b), n = L > 0 ? window_shares(a, window_span(a, b, L).len) : 0;
+    const bool real = row < seq_queries(a, b) * a.G;
+    RowMerge r;
+    float num = 0.f;
+    y.fold(real ? n : 0, d, r, num);
+    fold_partials<D>(a, slot + (int64_t)kMergeBlock * a.RP, (real ? n : 0) - kMergeBlock, d, r, num);
+    const __bf16 o = (__bf16)(r.den == 0.f ? 0.f : num / r.den);
+    a.out[out_index<D>(a, b, h, row) + d] = __builtin_bit_cast(uint16_t, o);
+    if (a.lse_out && d == 0) a.lse_out[lse_index(a, b, h, row)] = real ? (n > 0 ? (r.M + log2f(r.den)) * 0.6931471805599453f : -INFINITY) : 0.f;
 }
 
 // Calls f(Geo, paged) for the kernel that a shape takes; row blocks 1..6.
@@ -677,13 +699,6 @@ namespace {
 // round (16 sequences, 20 rows: 512 tokens 11.4 instead of 18, 1024 14.3 instead of 20, 2048 19.7 instead of 24.5).
 constexpr int kDirectQuanta = 2, kDirectBatchQuanta = 8;
 
-// The most that a sequence has for the workgroups to divide.
-int64_t most_tokens(const StreamLaunch& a)
-{
-    const int64_t span = (int64_t)a.sinks + a.window + a.Qmax + 2 * kWindowStep;
-    return a.window && span < a.max_ctx ? span : a.max_ctx;
-}
-
 void plan_shares(StreamLaunch& a, int rb, int groups)
 {
     a.RP = rb * 16;
@@ -693,7 +708,7 @@ void plan_shares(StreamLaunch& a, int rb, int groups)
         return hipSuccess;
     });
     // no more shares than the longest possible batch has quanta
-    const int64_t most = (int64_t)a.B * ((most_tokens(a) + a.quantum - 1) / a.quantum + kPieceQuanta);
+    const int64_t most = (int64_t)a.B * (((int64_t)a.max_ctx + a.quantum - 1) / a.quantum + kPieceQuanta);
     a.groups = groups < 1 ? 1 : groups;
     if (a.groups > most) a.groups = (int)most;
     a.nslots = a.groups + a.B - 1;
@@ -709,7 +724,34 @@ void plan_attn_stream(StreamLaunch& a, int n_cu)
     plan_shares(a, (a.Qmax * a.G + 15) / 16, n_cu / a.Hkv);
     const int64_t units = (int64_t)a.B * a.Hkv;
     const int quanta = 2 * units >= n_cu && units <= n_cu ? kDirectBatchQuanta : kDirectQuanta;
-    a.direct = most_tokens(a) <= quanta * a.quantum;
+    a.direct = a.max_ctx <= quanta * a.quantum;
+}
+
+// The shares of a sequence's window: those that a simple account finds the fastest.  A workgroup takes a fixed time, of which most is code that each of them runs
+// for the first time, and its tokens times a rate, that of its arithmetic or what the memory gives to so many workgroups; the chip takes as many rounds as it
+// is filled by; more than one share cost a second launch.  (us, one share against what the account takes: 64 sequences, 4 rows of 32 / 8 heads of 128, 2000 tokens 84, one;
+// 36 rows, 500 tokens 43, one; one sequence, 36 rows, 4000 tokens 45 and 17, 32 shares.  The division of the whole batch's tokens into equal shares, which unequal lengths
+// ask for, takes 90, 65 and 17.7.)
+void plan_attn_stream_window(StreamLaunch& a, int n_cu)
+{
+    const int rb = (a.Qmax * a.G + 15) / 16;
+    plan_shares(a, rb, 1);
+    const int64_t span = (int64_t)a.sinks + a.window + a.Qmax + 2 * kWindowStep, tokens = span < a.max_ctx ? span : a.max_ctx;
+    const int64_t units = (int64_t)a.B * a.Hkv, most = (tokens + a.quantum - 1) / a.quantum;
+    const float fixed = rb == 1 ? 7.f : rb == 2 ? 9.f : 13.f, a_token = 0.005f + 0.001f * rb, bytes = 4.f * a.D;      // us
+    float best = -1.f;
+    for (int64_t k = 0; k <= 4; ++k) {                                     // shares that fill k rounds
+        int64_t groups = k * n_cu / units;
+        groups = groups > most ? most : groups < 1 ? 1 : groups;
+        const int64_t grid = units * groups, busy = grid < n_cu ? grid : n_cu, rounds = (grid + n_cu - 1) / n_cu;
+        const float from_memory = bytes * (float)busy / 6.8e6f, rate = from_memory > a_token ? from_memory : a_token;
+        const float time = (float)rounds * (fixed + rate * (float)tokens / (float)groups) + (groups > 1 ? 3.f : 0.f);
+        if (best >= 0.f && time >= best) continue;
+        best = time;
+        a.groups = (int)groups;
+    }
+    a.nslots = a.B * a.groups;
+    a.direct = a.groups == 1;
 }
 
 void plan_attn_stream_pair(StreamLaunch& own, StreamLaunch& prefix, int n_cu)
@@ -741,7 +783,7 @@ hipError_t launch_attn_stream(const StreamLaunch& a, hipStream_t stream)
 {
     return with_geo(a.D, a.own.ks != nullptr, a.RP / 16, [&](auto geo) {
         using G = decltype(geo);
-        const dim3 grid(a.Hkv, a.direct ? a.B : a.groups * a.tiles), block(G::NW * 64);
+        const dim3 grid(a.Hkv, a.window ? a.B * a.groups : a.direct ? a.B : a.groups * a.tiles), block(G::NW * 64);
         if constexpr (G::QUANT) {
             auto fn = a.own.page_table ? attn_stream<G, true> : attn_stream<G, false>;
             hipLaunchKernelGGL(fn, grid, block, G::LDS, stream, a);
@@ -777,9 +819,9 @@ hipError_t launch_attn_stream_pair(const StreamLaunch& own, const StreamLaunch& 
 
 hipError_t launch_attn_stream_merge(const StreamLaunch& a, const StreamLaunch& prefix, hipStream_t stream)
 {
-    auto fn = prefix.part_o ? (a.D == 128 ? attn_stream_merge<128, true, false> : attn_stream_merge<64, true, false>)
-              : a.window    ? (a.D == 128 ? attn_stream_merge<128, false, true> : attn_stream_merge<64, false, true>)
-                            : (a.D == 128 ? attn_stream_merge<128, false, false> : attn_stream_merge<64, false, false>);
+    auto fn = prefix.part_o ? (a.D == 128 ? attn_stream_merge<128, true> : attn_stream_merge<64, true>)
+              : a.window    ? (a.D == 128 ? attn_window_rows_merge<128> : attn_window_rows_merge<64>)
+                            : (a.D == 128 ? attn_stream_merge<128, false> : attn_stream_merge<64, false>);
     hipLaunchKernelGGL(fn, dim3(a.Qmax * a.G, a.Hkv, a.B), dim3(a.D), 0, stream, a, prefix);
     return hipGetLastError();
 }

@@ -66,16 +66,15 @@ struct Shares {
         return x < head ? (int)((unsigned)x / (unsigned)(len + 1)) : rest + (int)((unsigned)(x - head) / (unsigned)max(len, 1));
     }
 };
-// Calls piece(b, L, c0, c1) for every piece [c0, c1) of a sequence b in share g, in order.  Sequences are taken 64 at a time, one a lane; len_of(b): their
-// lengths.
-template <class Piece, class Len>
-__device__ __forceinline__ void for_each_piece(const StreamLaunch& a, int g, int lane, int len, int quantum, Piece piece, Len len_of)
+// Calls piece(b, L, c0, c1) for every piece [c0, c1) of a sequence b in share g, in order.  Sequences are taken 64 at a time, one a lane.
+template <class Piece>
+__device__ __forceinline__ void for_each_piece(const StreamLaunch& a, int g, int lane, int len, int quantum, Piece piece)
 {                                                        // len: of sequence `lane`, 0 where there is none
     int cost = seq_cost(len, lane, quantum);
     int end = scan_costs(cost);                          // cost of the sequences up to this one
     int total = __builtin_amdgcn_readlane(end, 63);
     for (int b0 = 64; b0 < a.B; b0 += 64)
-        total += __builtin_amdgcn_readlane(scan_costs(b0 + lane < a.B ? seq_cost(len_of(b0 + lane), b0 + lane, quantum) : 0), 63);
+        total += __builtin_amdgcn_readlane(scan_costs(b0 + lane < a.B ? seq_cost(seq_len(a, b0 + lane), b0 + lane, quantum) : 0), 63);
     const Shares sh(total, a.groups);
     const int x0 = sh.begin(g), x1 = min(sh.begin(g + 1), total);
     if (x0 >= x1) return;
@@ -92,15 +91,10 @@ __device__ __forceinline__ void for_each_piece(const StreamLaunch& a, int g, int
         const int before = __builtin_amdgcn_readlane(end, 63);
         b0 += 64;
         if (b0 >= a.B || before >= x1) return;
-        len = b0 + lane < a.B ? len_of(b0 + lane) : 0;
+        len = b0 + lane < a.B ? seq_len(a, b0 + lane) : 0;
         cost = seq_cost(len, b0 + lane, quantum);
         end = before + scan_costs(cost);
     }
-}
-template <class Piece>
-__device__ __forceinline__ void for_each_piece(const StreamLaunch& a, int g, int lane, int len, int quantum, Piece piece)
-{
-    for_each_piece(a, g, lane, len, quantum, piece, [&](int b) { return seq_len(a, b); });
 }
 
 // The same number, of which the compiler knows nothing: what rare paths make of it is computed there, and does not take registers from the

@@ -383,7 +383,7 @@ StreamLaunch plan_window(const rapid_ctx* ctx, const rapid_attn_shape* s, int wi
     StreamLaunch a = stream_shape(s, own);
     a.window = window < s->max_ctx ? window : s->max_ctx;                  // (more is all there is)
     a.sinks = sinks < s->max_ctx ? sinks : s->max_ctx;
-    if (few_rows(s)) plan_attn_stream(a, compute_units(ctx));
+    if (few_rows(s)) plan_attn_stream_window(a, compute_units(ctx));
     else plan_attn_window(a, compute_units(ctx));
     return a;
 }
