@@ -311,7 +311,7 @@ int rapid_lm_head(rapid_ctx* ctx, int n_rows, int hidden, int vocab,
  * Rows of bf16 values as 8-bit integers, a scale for each row: with m = max |x_c| of a row
  *     codes[r][c] = 127 x_c / m to the nearest whole number, ties to even;   scales[r] = m / 127 (fp32)
  * A row of zeros has codes 0 and the scale 0, a row with a NaN or an infinity codes 0 and the scale NaN.
- *   rows, cols    rows < 2^31, cols a multiple of 8, at most 2^17
+ *   rows, cols    rows < 2^24, cols a multiple of 8, at most 2^17
  *   x             bf16, row r at x + r * row_stride elements (a multiple of 8, at least cols), 16-byte aligned
  *   codes         int8 [rows, pitch], 16-byte aligned; pitch is cols rounded up to a multiple of 256, and zeros fill the rows
  *   scales        fp32 [rows]
@@ -486,7 +486,7 @@ int rapid_verify_attn_quant(rapid_ctx* ctx, const rapid_attn_shape* shape, const
  *   positions     int32 [B, q_max] or NULL: a row's position is then its token, ctx_lens[b] - (gamma_b+1) + i (behind a shared prefix, say,
  *                 or in chunks that keep their places in a document, it is not)
  *   q_out         bf16 [B, q_max, Hq, d], contiguous; may be q_new where that is contiguous too
- *   shape         as for rapid_verify_attn; q_max may be anything up to max_ctx (a whole prompt), softmax_scale is > 0 and not used otherwise
+ *   shape         as for rapid_verify_attn; q_max may be anything up to max_ctx (a whole prompt) and 2^22, softmax_scale is > 0 and not used otherwise
  *
  * rapid_kv_append_rope_quant: the same into a cache in 8 bits: what is quantised is the rotated row in bf16, so that the cache is what
  * rapid_kv_append_quant leaves of such rows.  Shape and layout as for that call.
@@ -513,7 +513,8 @@ int rapid_kv_append_rope_quant(rapid_ctx* ctx, const rapid_attn_shape* shape, co
  * the keys j <= p with j > p - window or j < sinks: the last `window` ones, its own among them, and the first `sinks`.
  *   window        >= 1 (max_ctx or more: all keys up to p);  sinks >= 0
  *   shape         as for rapid_verify_attn, but q_max may be anything up to max_ctx: one position, a round's, a whole prompt, or a piece of
- *                 one behind what is cached already (chunk_tokens and ctx_sum_hint are not used)
+ *                 one behind what is cached already (chunk_tokens and ctx_sum_hint are not used); (q_max * group / 128 + 1) * batch * n_kv_heads is
+ *                 at most 2^22
  *   The cache holds every token at its own place.  What no row attends costs nothing and has no effect, whatever it holds: paged, the pages between
  *                 the sinks and the windows may be given away, and their entries in page_table may be anything (ids are clamped)
  *   q, k_cache, v_cache, ctx_lens, gammas, page_table, out, lse_out   as for rapid_verify_attn; rows i >= Q are written as zeros (lse_out 0), rows

@@ -66,7 +66,7 @@ struct Piece {
     uint32_t kring_lds, vring_lds, sring_lds;
     int b, h;
     int L, Q, R, c0, c1, nt, last_tok;            // nt: this stream's tiles (positions c0 + (part + it NP) TT ..; these are tokens, but for a window)
-    int joint, gap;                               // a window: of its span
+    int joint, gap, r0;                           // a window: of its span; the first of the packed rows
     int lane, wave, part, team;
 };
 
@@ -79,7 +79,10 @@ __device__ __forceinline__ WindowSpan window_span(const StreamLaunch& a, int b, 
 // Into how many shares a sequence is cut: `groups`, of a quantum at least.
 __device__ __forceinline__ int window_shares(const StreamLaunch& a, int len) { return min(a.groups, (len + a.quantum - 1) / a.quantum); }
 // The partials of (sequence b, kv head h, packed row `row`), RP slots apart.
-__device__ __forceinline__ int64_t window_slot(const StreamLaunch& a, int b, int h, int row) { return ((int64_t)h * a.B + b) * a.groups * a.RP + row; }
+__device__ __forceinline__ int64_t window_slot(const StreamLaunch& a, int b, int h, int row)
+{
+    return (((int64_t)h * a.B + b) * a.tiles + row / a.RP) * a.groups * a.RP + row % a.RP;
+}
 template <bool WINDOW>
 __device__ __forceinline__ int tile_token(const Piece& w, int x) { return WINDOW && x >= w.joint ? x + w.gap : x; }
 
@@ -98,8 +101,9 @@ __device__ __forceinline__ void run_piece(const StreamLaunch& a, const Piece& w,
     for (int rb = 0; rb < RB; ++rb) {
         const int row = row0 + rb * 16 + ln;
         const bool real = row < w.R;
-        lim[rb] = min(real && !a.shared ? w.L - w.Q + row / a.G : w.L - 1, WINDOW ? w.last_tok : w.c1 - 1);
-        before[rb] = WINDOW && real ? w.L - w.Q + row / a.G - a.window : -1;
+        const int place = WINDOW ? w.r0 + row : row;
+        lim[rb] = min(real && !a.shared ? w.L - w.Q + place / a.G : w.L - 1, WINDOW ? w.last_tok : w.c1 - 1);
+        before[rb] = WINDOW && real ? w.L - w.Q + place / a.G - a.window : -1;
 #pragma unroll
         for (int ks = 0; ks < G::KS; ++ks) {
             const int chunk = G::QUANT ? (ks >> 1) * 8 + 2 * lg + (ks & 1) : ks * 4 + lg;
@@ -227,10 +231,8 @@ __device__ __forceinline__ void run_piece(const StreamLaunch& a, const Piece& w,
     if (WINDOW && taken) {
 #pragma unroll 1
         for (int it = 0; it < w.nt; ++it) {
-            const int t0 = tile_t0(it), end = min(t0 + G::TT - 1, w.last_tok), lg = opaque(lane) >> 4;
-            if (!masked(t0)) continue;
-#pragma unroll 1
-            for (int tok = t0; tok <= end; ++tok) add_not_finite_of<G, RB, PAGED>(st, w.addr, tok, hidden, lg);
+            const int t0 = tile_t0(it);
+            if (masked(t0)) add_not_finite_shown<G, RB, PAGED>(st, w.addr, t0, min(t0 + G::TT - 1, w.last_tok), hidden, lane);
         }
     } else if (taken) {
         const int it = (max(first_masked_t0 - tile_t0(0), 0) + G::QUANTUM - 1) / G::QUANTUM;
@@ -267,7 +269,7 @@ __device__ __forceinline__ void run_piece(const StreamLaunch& a, const Piece& w,
         if (w.part == 0 && lg == 0 && row < w.R) {
             if (a.direct) {
                 sums[row] = ll;
-                if (a.lse_out) a.lse_out[lse_index(a, w.b, w.h, row)] = (mm + log2f(ll)) * 0.6931471805599453f;
+                if (a.lse_out) a.lse_out[lse_index(a, w.b, w.h, WINDOW ? w.r0 + row : row)] = (mm + log2f(ll)) * 0.6931471805599453f;
             } else {
                 a.part_ml[(pbase + row) * 2 + 0] = mm;
                 a.part_ml[(pbase + row) * 2 + 1] = ll;
@@ -293,7 +295,7 @@ __device__ __forceinline__ void run_piece(const StreamLaunch& a, const Piece& w,
                 const float l = sums[row];
                 if (l != 0.f) sum /= l;
                 const bf16x4 o = {(__bf16)sum[0], (__bf16)sum[1], (__bf16)sum[2], (__bf16)sum[3]};
-                *reinterpret_cast<bf16x4*>(a.out + out_index<G::D>(a, w.b, w.h, row) + half * DH + x) = o;
+                *reinterpret_cast<bf16x4*>(a.out + out_index<G::D>(a, w.b, w.h, WINDOW ? w.r0 + row : row) + half * DH + x) = o;
             } else {
                 *reinterpret_cast<floatx4*>(a.part_o + (pbase + row) * G::D + half * DH + x) = sum;
             }
@@ -328,6 +330,7 @@ __device__ __forceinline__ void stream_piece(const StreamLaunch& a, char* smem, 
         const WindowSpan span = window_span(a, b, L);
         w.joint = span.joint;
         w.gap = span.gap;
+        w.r0 = r0;
     }
     w.last_tok = tile_token<WINDOW>(w, c1 - 1);
     w.addr = make_row_addr<G, PAGED>(a.own, b, h);
@@ -424,22 +427,23 @@ __global__ void __launch_bounds__(G::NW * 64) attn_stream(StreamLaunch a)
     extern __shared__ __attribute__((aligned(1024))) char smem[];
     stream_share<G, PAGED>(a, smem, blockIdx.y, first_len(a));
 }
-// bf16, a window: one workgroup per (kv head, sequence, share).  What sequences have is alike, so each is cut by itself, and a workgroup need not look
-// at the others.
+// bf16, a window: one workgroup per (kv head, sequence, share, row tile).  What sequences have is alike, so each is cut by itself, and a workgroup need not
+// look at the others.
 template <class G, bool PAGED>
 __global__ void __launch_bounds__(G::NW * 64) attn_stream_window(StreamLaunch a)
 {
     extern __shared__ __attribute__((aligned(1024))) char smem[];
-    const int y = blockIdx.y, b = __builtin_amdgcn_readfirstlane(y / a.groups), share = y - b * a.groups;
+    const int y = blockIdx.y / a.tiles, r0 = __builtin_amdgcn_readfirstlane((blockIdx.y - y * a.tiles) * G::RP);
+    const int b = __builtin_amdgcn_readfirstlane(y / a.groups), share = y - b * a.groups;
     const int h = __builtin_amdgcn_readfirstlane(a.rot ? (blockIdx.x + y) % a.Hkv : blockIdx.x);
     const int L = __builtin_amdgcn_readfirstlane(seq_len(a, b));
-    if (a.direct) write_missing_rows<G>(a, b, h, L);
-    if (L <= 0) return;
+    if (a.direct && r0 == 0) write_missing_rows<G>(a, b, h, L);
+    if (L <= 0 || r0 >= seq_queries(a, b) * a.G) return;
     const int len = window_span(a, b, L).len, quanta = (len + G::QUANTUM - 1) / G::QUANTUM, shares = window_shares(a, len);
     if (share >= shares) return;
     const int c0 = (int)((int64_t)quanta * share / shares) * G::QUANTUM;
     const int c1 = min((int)((int64_t)quanta * (share + 1) / shares) * G::QUANTUM, len);
-    stream_piece<G, PAGED, true>(a, smem, b, h, L, c0, c1, window_slot(a, b, h, 0) + (int64_t)share * G::RP, 0);
+    stream_piece<G, PAGED, true>(a, smem, b, h, L, c0, c1, window_slot(a, b, h, r0) + (int64_t)share * G::RP, r0);
 }
 
 // How a prefix and the sequences' own tokens divide the `units` workgroups of a kv head: by what there is to read, of the prefix once for each row tile.
@@ -727,29 +731,39 @@ void plan_attn_stream(StreamLaunch& a, int n_cu)
     a.direct = a.max_ctx <= quanta * a.quantum;
 }
 
-// The shares of a sequence's window: those that a simple account finds the fastest.  A workgroup takes a fixed time, of which most is code that each of them runs
-// for the first time, and its tokens times a rate, that of its arithmetic or what the memory gives to so many workgroups; the chip takes as many rounds as it
-// is filled by; more than one share cost a second launch.  (us, one share against what the account takes: 64 sequences, 4 rows of 32 / 8 heads of 128, 2000 tokens 84, one;
-// 36 rows, 500 tokens 43, one; one sequence, 36 rows, 4000 tokens 45 and 17, 32 shares.  The division of the whole batch's tokens into equal shares, which unequal lengths
-// ask for, takes 90, 65 and 17.7.)
+// Row tiles and shares of a sequence's window: those that a simple account finds the fastest.  A workgroup takes a fixed time, of which most is code that each of
+// them runs for the first time, more of it the more blocks of rows it has, and its tokens times a rate, that of its arithmetic or what the memory gives to so many workgroups;
+// the chip takes as many rounds as it is filled by; more than one share cost a second launch.  (us a call, 32 / 8 heads of 128: 64 sequences of 4 rows, 2000 tokens: 84
+// in one share; of 36 rows, 500 tokens: 43 in one share; one sequence of 36 rows, 120 tokens: 10.4 in tiles of 16 rows, 14.3 in one of 48; of 72 rows, 2000 tokens:
+// 13.6 and 17.5; eight of 36 rows, 8000 tokens: 55 in one tile, 61 in two.  The division of the whole batch's tokens into equal shares, which unequal lengths ask for, takes 90 and 65.)
 void plan_attn_stream_window(StreamLaunch& a, int n_cu)
 {
-    const int rb = (a.Qmax * a.G + 15) / 16;
-    plan_shares(a, rb, 1);
+    const int rows = a.Qmax * a.G, all = (rows + 15) / 16;
     const int64_t span = (int64_t)a.sinks + a.window + a.Qmax + 2 * kWindowStep, tokens = span < a.max_ctx ? span : a.max_ctx;
-    const int64_t units = (int64_t)a.B * a.Hkv, most = (tokens + a.quantum - 1) / a.quantum;
-    const float fixed = rb == 1 ? 7.f : rb == 2 ? 9.f : 13.f, a_token = 0.005f + 0.001f * rb, bytes = 4.f * a.D;      // us
     float best = -1.f;
-    for (int64_t k = 0; k <= 4; ++k) {                                     // shares that fill k rounds
-        int64_t groups = k * n_cu / units;
-        groups = groups > most ? most : groups < 1 ? 1 : groups;
-        const int64_t grid = units * groups, busy = grid < n_cu ? grid : n_cu, rounds = (grid + n_cu - 1) / n_cu;
-        const float from_memory = bytes * (float)busy / 6.8e6f, rate = from_memory > a_token ? from_memory : a_token;
-        const float time = (float)rounds * (fixed + rate * (float)tokens / (float)groups) + (groups > 1 ? 3.f : 0.f);
-        if (best >= 0.f && time >= best) continue;
-        best = time;
-        a.groups = (int)groups;
+    int best_rb = all, best_groups = 1;
+    for (int rb = all; rb >= 1; rb = rb > 3 ? 3 : rb - 1) {
+        plan_shares(a, rb, 1);
+        const int tiles = (rows + rb * 16 - 1) / (rb * 16);
+        if ((int64_t)a.B * tiles > 65535 && tiles > 1) continue;          // (a grid's second dimension)
+        const int64_t units = (int64_t)a.B * a.Hkv * tiles, most = (tokens + a.quantum - 1) / a.quantum;
+        const float fixed = rb == 1 ? (tiles > 1 ? 9.f : 7.f) : rb == 2 ? 10.f : rb == 3 ? 13.f : 15.f, a_token = 0.005f + 0.001f * rb;      // us
+        const float bytes = 4.f * a.D * (0.35f + 0.65f / tiles);           // of which row tiles beside one another share some
+        for (int64_t k = 0; k <= 4; ++k) {                                 // shares that fill k rounds
+            int64_t groups = k * n_cu / units;
+            groups = groups > most ? most : groups < 1 ? 1 : groups;
+            const int64_t grid = units * groups, busy = grid < n_cu ? grid : n_cu, rounds = (grid + n_cu - 1) / n_cu;
+            const float from_memory = bytes * (float)busy / 6.8e6f, rate = from_memory > a_token ? from_memory : a_token;
+            const float time = (float)rounds * (fixed + rate * (float)tokens / (float)groups) + (groups > 1 ? 2.5f : 0.f);
+            if (best >= 0.f && time >= best) continue;
+            best = time;
+            best_rb = rb;
+            best_groups = (int)groups;
+        }
     }
+    plan_shares(a, best_rb, 1);
+    a.tiles = (rows + best_rb * 16 - 1) / (best_rb * 16);
+    a.groups = best_groups;
     a.nslots = a.B * a.groups;
     a.direct = a.groups == 1;
 }
@@ -783,7 +797,7 @@ hipError_t launch_attn_stream(const StreamLaunch& a, hipStream_t stream)
 {
     return with_geo(a.D, a.own.ks != nullptr, a.RP / 16, [&](auto geo) {
         using G = decltype(geo);
-        const dim3 grid(a.Hkv, a.window ? a.B * a.groups : a.direct ? a.B : a.groups * a.tiles), block(G::NW * 64);
+        const dim3 grid(a.Hkv, a.window ? a.B * a.groups * a.tiles : a.direct ? a.B : a.groups * a.tiles), block(G::NW * 64);
         if constexpr (G::QUANT) {
             auto fn = a.own.page_table ? attn_stream<G, true> : attn_stream<G, false>;
             hipLaunchKernelGGL(fn, grid, block, G::LDS, stream, a);

@@ -506,42 +506,36 @@ __device__ __forceinline__ bool take_not_finite(char* vt, int lane)
     }
     return __any(any);
 }
-// What is not finite in V of token t, to the rows that attend it.
-template <class G, int RB, bool PAGED, class Hidden>
-__device__ __forceinline__ void add_not_finite_of(WaveState<G, RB>& st, const RowAddr& ra, int t, Hidden hidden, int lg)
-{
-    const char* row = ra.v;
-    if (PAGED) row += (int64_t)min(max(ra.pages[t >> ra.page_shift], 0), ra.page_hi) * ra.page_bytes;
-    row += (uint32_t)(PAGED ? t & ra.page_mask : t) * ra.tok_bytes;
-#pragma unroll
-    for (int db = 0; db < G::DB; ++db) {
-        uint32_t bits[4];                                // columns 16 db + 4 lg .. + 3
-        if (G::QUANT) {
-            const uint32_t w = *reinterpret_cast<const uint32_t*>(row + db * 16 + lg * 4);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) bits[i] = (w >> (8 * i) & 0x7fu) == 0x7fu ? 0x7fc00000u : 0u;
-        } else {
-            const u32x2 w = *reinterpret_cast<const u32x2*>(row + db * 32 + lg * 8);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const uint32_t x = i & 1 ? w[i >> 1] & 0xffff0000u : w[i >> 1] << 16;
-                bits[i] = (x & 0x7f800000u) == 0x7f800000u ? x : 0u;
-            }
-        }
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-#pragma unroll
-            for (int rb = 0; rb < RB; ++rb)
-                if (bits[i] && !hidden(t, rb)) st.acc[db][rb][i] += __uint_as_float(bits[i]);
-    }
-}
 template <class G, int RB, bool PAGED>
 __device__ __forceinline__ void add_not_finite(WaveState<G, RB>& st, const RowAddr& ra, int begin, int end, int step, const int (&lim)[RB], int lane)
 {                                                        // tiles of a stream, `step` tokens apart, from token `begin` on
     const int lg = opaque(lane) >> 4;
 #pragma unroll 1
     for (int t = begin, left = G::TT; t < end; ++t) {
-        add_not_finite_of<G, RB, PAGED>(st, ra, t, [&](int tok, int rb) { return tok > lim[rb]; }, lg);
+        const char* row = ra.v;
+        if (PAGED) row += (int64_t)min(max(ra.pages[t >> ra.page_shift], 0), ra.page_hi) * ra.page_bytes;
+        row += (uint32_t)(PAGED ? t & ra.page_mask : t) * ra.tok_bytes;
+#pragma unroll
+        for (int db = 0; db < G::DB; ++db) {
+            uint32_t bits[4];                            // columns 16 db + 4 lg .. + 3
+            if (G::QUANT) {
+                const uint32_t w = *reinterpret_cast<const uint32_t*>(row + db * 16 + lg * 4);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) bits[i] = (w >> (8 * i) & 0x7fu) == 0x7fu ? 0x7fc00000u : 0u;
+            } else {
+                const u32x2 w = *reinterpret_cast<const u32x2*>(row + db * 32 + lg * 8);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const uint32_t x = i & 1 ? w[i >> 1] & 0xffff0000u : w[i >> 1] << 16;
+                    bits[i] = (x & 0x7f800000u) == 0x7f800000u ? x : 0u;
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int rb = 0; rb < RB; ++rb)
+                    if (bits[i] && t <= lim[rb]) st.acc[db][rb][i] += __uint_as_float(bits[i]);
+        }
         if (--left == 0) {
             left = G::TT;
             t += step - G::TT;
@@ -563,6 +557,18 @@ struct WindowSpan {
     }
     __device__ __forceinline__ int token(int x) const { return x < joint ? x : x + gap; }
 };
+// add_not_finite where each row has tokens of its own that are hidden from it.
+template <class G, int RB, bool PAGED, class Hidden>
+__device__ __forceinline__ void add_not_finite_shown(WaveState<G, RB>& st, const RowAddr& ra, int first, int last, Hidden hidden, int lane)
+{
+#pragma unroll 1
+    for (int t = first; t <= last; ++t) {
+        int lim[RB];
+#pragma unroll
+        for (int rb = 0; rb < RB; ++rb) lim[rb] = hidden(t, rb) ? -1 : t;
+        add_not_finite<G, RB, PAGED>(st, ra, t, t + 1, G::TT, lim, lane);
+    }
+}
 // Whether a tile holds a token that some of the rows do not attend.
 __device__ __forceinline__ bool window_masks(int t0, int tokens, int first, int last, int last_tok, int window, int sinks)
 {

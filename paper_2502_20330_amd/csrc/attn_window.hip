@@ -137,10 +137,8 @@ __device__ __forceinline__ void window_piece(const StreamLaunch& a, char* smem, 
     if (*taken_word != 0) {
 #pragma unroll 1
         for (int it = 0; it < nt; ++it) {
-            const int t0 = tile_t0(it), end = min(t0 + G::TT - 1, last_tok), group = opaque(lane) >> 4;
-            if (!masked(t0)) continue;
-#pragma unroll 1
-            for (int tok = t0; tok <= end; ++tok) add_not_finite_of<G, RB, PAGED>(st, addr, tok, hidden, group);
+            const int t0 = tile_t0(it);
+            if (masked(t0)) add_not_finite_shown<G, RB, PAGED>(st, addr, t0, min(t0 + G::TT - 1, last_tok), hidden, lane);
         }
     }
 #pragma unroll

@@ -279,13 +279,14 @@ int check_quant_layout(const rapid_attn_shape* s, const rapid_quant_layout* l)
     return RAPID_OK;
 }
 
-// The new rows and the rotation of an append.  Grid dimensions bound the batch and the parts of the heads.
+// The new rows and the rotation of an append.  The grid bounds rows (2^32 threads) and batch.
 int check_rope(const rapid_attn_shape* s, const rapid_rope* r, bool queries)
 {
     if (!r) return RAPID_EINVAL;
     if (!(r->amplitude - r->amplitude == 0.f) || (r->interleaved != 0 && r->interleaved != 1)) return RAPID_EINVAL;
     if (r->rotary_dim < 16 || r->rotary_dim > s->head_dim || r->rotary_dim % 16) return RAPID_EUNSUPPORTED;
-    if (s->batch > 65535 || (queries ? (int64_t)s->n_q_heads : 0) + 2 * (int64_t)s->n_kv_heads > 1 << 16) return RAPID_EUNSUPPORTED;
+    if (s->q_max > 1 << 22 || s->batch > 65535 || (queries ? (int64_t)s->n_q_heads : 0) + 2 * (int64_t)s->n_kv_heads > 1 << 16)
+        return RAPID_EUNSUPPORTED;
     const int64_t q_row = (int64_t)s->n_q_heads * s->head_dim, kv_row = (int64_t)s->n_kv_heads * s->head_dim;
     if ((queries && (r->q_stride < q_row || r->q_stride % 8)) || r->k_stride < kv_row || r->k_stride % 8 || r->v_stride < kv_row ||
         r->v_stride % 8) return RAPID_EALIGN;
@@ -373,9 +374,9 @@ int check_window_shape(const rapid_attn_shape* s, int window, int sinks)
     if (rc == RAPID_OK && few_rows(s)) rc = check_attn_shape(s);
     if (rc == RAPID_OK) rc = check_tokens(s->batch, s->max_ctx);
     if (rc != RAPID_OK) return rc;
-    // packed rows and row tiles are counted in 32 bits
+    // packed rows are counted in 32 bits, and a grid has 2^32 threads, 512 a row tile
     const int64_t rows = (int64_t)s->q_max * (s->n_q_heads / s->n_kv_heads);
-    if (rows > 1 << 30 || s->n_kv_heads > 65535 || (rows / 128 + 1) * s->batch * s->n_kv_heads > 1 << 30) return RAPID_EUNSUPPORTED;
+    if (rows > 1 << 30 || s->n_kv_heads > 65535 || (rows / 128 + 1) * s->batch * s->n_kv_heads > 1 << 22) return RAPID_EUNSUPPORTED;
     return RAPID_OK;
 }
 StreamLaunch plan_window(const rapid_ctx* ctx, const rapid_attn_shape* s, int window, int sinks, const AttnSource& own)
@@ -785,7 +786,7 @@ int rapid_quant_rows(rapid_ctx* ctx, int64_t rows, int cols, const void* x, int6
 {
     if (!ctx || !x || !codes || !scales) return RAPID_EINVAL;
     if (rows < 1 || cols < 1 || row_stride < cols) return RAPID_EINVAL;
-    if (rows > 0x7fffffff || cols > kMaxQuantCols || cols % 8) return RAPID_EUNSUPPORTED;
+    if (rows >= 1 << 24 || cols > kMaxQuantCols || cols % 8) return RAPID_EUNSUPPORTED;          // (a grid has 2^32 threads)
     if (!aligned(x, 16) || !aligned(codes, 16) || !aligned(scales, 4) || row_stride % 8) return RAPID_EALIGN;
     const QuantRowsLaunch a = quant_rows_of(rows, cols, x, row_stride, codes, scales);
     DeviceScope dev(ctx->device);

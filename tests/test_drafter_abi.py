@@ -26,6 +26,7 @@ def rope_call(s, rope=None, quant=False, layout=None, **kw):
     (dict(head_dim=96), EUNSUPPORTED), (dict(kv_token_stride=252), EALIGN), (dict(kv_head_stride=4), EALIGN), (dict(batch=70000), EUNSUPPORTED),
     (dict(PAGED, page_size=24), EUNSUPPORTED), (dict(PAGED, max_pages=62), EINVAL), (dict(n_pages=-1), EINVAL),
     (dict(kv_token_stride=1 << 62), EUNSUPPORTED), (dict(n_q_heads=1 << 17, n_kv_heads=1 << 15), None),
+    (dict(PAGED, max_pages=1 << 26, max_ctx=1 << 30, q_max=(1 << 22) + 1, gamma=0), EUNSUPPORTED),
 ])
 def test_shapes_that_the_append_refuses(quant, kw, want):
     s = shape(**kw)
@@ -65,7 +66,7 @@ def test_what_the_row_quantisation_refuses():
         assert rows_call(**{key: None}) == EINVAL, key
     for kw in (dict(rows=0), dict(cols=0), dict(rows=-1), dict(stride=56)):
         assert rows_call(**kw) == EINVAL, kw
-    for kw in (dict(rows=1 << 31), dict(cols=60), dict(cols=(1 << 17) + 8, stride=1 << 18)):
+    for kw in (dict(rows=1 << 24), dict(cols=60), dict(cols=(1 << 17) + 8, stride=1 << 18)):
         assert rows_call(**kw) == EUNSUPPORTED, kw
     for kw in (dict(x=P + 8), dict(codes=P + 8), dict(scales=P + 2), dict(stride=68)):
         assert rows_call(**kw) == EALIGN, kw
@@ -133,7 +134,8 @@ def window_call(s, window=100, sinks=4, **kw):
     (dict(PAGED, page_size=24), EUNSUPPORTED), (dict(PAGED, max_pages=62), EINVAL), (dict(kv_token_stride=1 << 62), EUNSUPPORTED),
     (dict(PAGED, max_pages=1 << 27, max_ctx=(1 << 30) + 1), EUNSUPPORTED), (dict(PAGED, max_pages=1 << 27, max_ctx=1 << 30, batch=64), EUNSUPPORTED),
     (dict(PAGED, max_pages=1 << 26, max_ctx=1 << 30, q_max=1 << 29, gamma=0), EUNSUPPORTED),
-    (dict(PAGED, max_pages=1 << 26, max_ctx=1 << 30, q_max=1 << 24, gamma=0, batch=8, n_kv_heads=8), None),
+    (dict(PAGED, max_pages=1 << 26, max_ctx=1 << 30, q_max=1 << 24, gamma=0, batch=8, n_kv_heads=8), EUNSUPPORTED),
+    (dict(PAGED, max_pages=1 << 26, max_ctx=1 << 30, q_max=1 << 22, gamma=0, batch=8, n_kv_heads=8), None),
 ])
 def test_shapes_that_the_window_refuses(kw, want):
     s = shape(**kw)
