@@ -30,15 +30,17 @@ struct StreamLaunch {
     int32_t rot;                // 1: share g of slot x serves head (x + g) mod Hkv, 0: head x
     int32_t direct;             // 1: short sequences, one workgroup for each and kv head, which writes the result; no partials
     int32_t window, sinks;      // window > 0: a row at position p attends tokens of (p - window, p] and the first `sinks`; 0: all up to p
+    int32_t many;               // a window: 1: attn_window.hip's kernel, 0: the streaming one
     float scale_log2e;
 };
-constexpr int kStreamRows = 96;      // packed rows that the streaming kernel takes
+constexpr int kStreamRows = 96;      // packed rows that a workgroup of the streaming kernel takes
 // Fill the plan (RP .. direct) from the shape and the source's layout.
 void plan_attn_stream(StreamLaunch& a, int n_cu);
-void plan_attn_stream_window(StreamLaunch& a, int n_cu);                         // a window of at most kStreamRows: `groups` shares of each sequence
+// A window: row tiles of at most kStreamRows, `groups` shares of a row tile's tokens, direct where that is one.  Both return the us that they expect, the first
+// infinity where its grid does not fit.
+float plan_attn_stream_window(StreamLaunch& a, int n_cu);                        // q is addressed with 32 bits
 void plan_attn_prefix(StreamLaunch& a, int n_cu);
-// Windowed attention of more rows than kStreamRows (attn_window.hip): `groups` shares of a row tile's tokens; direct where that is one.
-void plan_attn_window(StreamLaunch& a, int n_cu);
+float plan_attn_window(StreamLaunch& a, int n_cu);                               // attn_window.hip
 // Both for one launch: the tokens of a shared prefix, its rows in tiles of at most kStreamRows, and the sequences' own.  Where the two lie differently
 // (one paged, the other not), for two launches in turn.
 void plan_attn_stream_pair(StreamLaunch& own, StreamLaunch& prefix, int n_cu);

@@ -66,17 +66,27 @@ struct Piece {
     uint32_t kring_lds, vring_lds, sring_lds;
     int b, h;
     int L, Q, R, c0, c1, nt, last_tok;            // nt: this stream's tiles (positions c0 + (part + it NP) TT ..; these are tokens, but for a window)
-    int joint, gap, r0;                           // a window: of its span; the first of the packed rows
+    int joint, gap, r0;                           // a window: of the rows' span; the first of the packed rows
+    int first, last;                              // and their positions
     int lane, wave, part, team;
 };
 
-// ---- a window: a sequence's span (attn_tile.h) takes its tokens' place
+// ---- a window: the span (attn_tile.h) of a tile of packed rows takes the tokens' place
 constexpr int kWindowStep = 32;
-__device__ __forceinline__ WindowSpan window_span(const StreamLaunch& a, int b, int L)
-{
-    return WindowSpan(L - seq_queries(a, b), L - 1, a.window, a.sinks, kWindowStep);
-}
-// Into how many shares a sequence is cut: `groups`, of a quantum at least.
+// Packed rows r0 .. r0 + RP - 1 of sequence b, of which `rows` exist.
+struct WindowRows {
+    int L, Q, r0, rows;
+    int first, last;                              // the positions of those that do
+    __device__ __forceinline__ WindowRows(const StreamLaunch& a, int b, int r0_) : L(seq_len(a, b)), Q(seq_queries(a, b)), r0(r0_)
+    {
+        rows = min(Q * a.G - r0, a.RP);
+        first = L - Q + r0 / a.G;
+        last = L - Q + (r0 + rows - 1) / a.G;
+    }
+    __device__ __forceinline__ bool attend() const { return rows > 0 && L > 0 && last >= 0; }
+    __device__ __forceinline__ WindowSpan span(const StreamLaunch& a) const { return WindowSpan(first, last, a.window, a.sinks, kWindowStep); }
+};
+// Into how many shares a span is cut: `groups`, of a quantum at least.
 __device__ __forceinline__ int window_shares(const StreamLaunch& a, int len) { return min(a.groups, (len + a.quantum - 1) / a.quantum); }
 // The partials of (sequence b, kv head h, packed row `row`), RP slots apart.
 __device__ __forceinline__ int64_t window_slot(const StreamLaunch& a, int b, int h, int row)
@@ -124,7 +134,7 @@ __device__ __forceinline__ void run_piece(const StreamLaunch& a, const Piece& w,
     auto hidden = [&](int tok, int rb) { return tok > lim[rb] || (WINDOW && tok <= before[rb] && tok >= a.sinks); };
     const int first_masked_t0 = min(a.shared ? w.L : w.L - w.Q, w.c1) - (G::TT - 1);     // tiles from here on hold tokens that some row does not attend
     auto masked = [&](int t0) {
-        return WINDOW ? window_masks(t0, G::TT, w.L - w.Q, w.L - 1, w.last_tok, a.window, a.sinks) : t0 >= first_masked_t0;
+        return WINDOW ? window_masks(t0, G::TT, w.first, w.last, w.last_tok, a.window, a.sinks) : t0 >= first_masked_t0;
     };
     TilePages<G, PAGED> pages;
     bool taken = false;
@@ -327,10 +337,13 @@ __device__ __forceinline__ void stream_piece(const StreamLaunch& a, char* smem, 
     w.nt = (ntile + G::NP - 1 - (G::TEAMS ? 0 : w.part)) / G::NP;
     if (WINDOW) {
         static_assert(!WINDOW || G::TT == kWindowStep, "");
-        const WindowSpan span = window_span(a, b, L);
+        const WindowRows rows(a, b, r0);
+        const WindowSpan span = rows.span(a);
         w.joint = span.joint;
         w.gap = span.gap;
         w.r0 = r0;
+        w.first = rows.first;
+        w.last = rows.last;
     }
     w.last_tok = tile_token<WINDOW>(w, c1 - 1);
     w.addr = make_row_addr<G, PAGED>(a.own, b, h);
@@ -389,15 +402,15 @@ __device__ __forceinline__ void stream_piece(const StreamLaunch& a, char* smem, 
     }
 }
 
-// What rows of a sequence there are none of, and all of one without tokens: zeros (lse: 0, and -infinity for rows that have nothing to attend).
+// Packed rows [from, to) of a sequence, which it does not have or which attend nothing: zeros (lse: 0, and -infinity for rows that it has).
 template <class G>
-__device__ __forceinline__ void write_missing_rows(const StreamLaunch& a, int b, int h, int L)
+__device__ __forceinline__ void write_missing_rows(const StreamLaunch& a, int b, int h, int from, int to)
 {
-    const int R = seq_queries(a, b) * a.G, from = L > 0 ? R : 0, rows = a.Qmax * a.G;
-    for (int f = threadIdx.x; f < (rows - from) * (G::D / 8); f += G::NW * 64)
+    const int R = seq_queries(a, b) * a.G;
+    for (int f = threadIdx.x; f < (to - from) * (G::D / 8); f += G::NW * 64)
         *reinterpret_cast<u32x4*>(a.out + out_index<G::D>(a, b, h, from + f / (G::D / 8)) + f % (G::D / 8) * 8) = u32x4{0, 0, 0, 0};
     if (a.lse_out)
-        for (int row = from + threadIdx.x; row < rows; row += G::NW * 64) a.lse_out[lse_index(a, b, h, row)] = row < R ? -INFINITY : 0.f;
+        for (int row = from + threadIdx.x; row < to; row += G::NW * 64) a.lse_out[lse_index(a, b, h, row)] = row < R ? -INFINITY : 0.f;
 }
 
 // Grid: one workgroup per (kv head, share).  Partials: [kv head][g + b], which no two pieces of a head share.  Direct: per (kv head, sequence).
@@ -407,7 +420,7 @@ __device__ __forceinline__ void stream_share(const StreamLaunch& a, char* smem, 
     const int h = __builtin_amdgcn_readfirstlane(a.rot ? (blockIdx.x + g) % a.Hkv : blockIdx.x);     // (base addresses go through scalar registers)
     if (a.direct) {
         const int L = __builtin_amdgcn_readfirstlane(seq_len(a, g));
-        write_missing_rows<G>(a, g, h, L);
+        write_missing_rows<G>(a, g, h, L > 0 ? seq_queries(a, g) * a.G : 0, a.Qmax * a.G);
         if (L > 0) stream_piece<G, PAGED, false>(a, smem, g, h, L, 0, L, 0, 0);
         return;
     }
@@ -436,10 +449,11 @@ __global__ void __launch_bounds__(G::NW * 64) attn_stream_window(StreamLaunch a)
     const int y = blockIdx.y / a.tiles, r0 = __builtin_amdgcn_readfirstlane((blockIdx.y - y * a.tiles) * G::RP);
     const int b = __builtin_amdgcn_readfirstlane(y / a.groups), share = y - b * a.groups;
     const int h = __builtin_amdgcn_readfirstlane(a.rot ? (blockIdx.x + y) % a.Hkv : blockIdx.x);
-    const int L = __builtin_amdgcn_readfirstlane(seq_len(a, b));
-    if (a.direct && r0 == 0) write_missing_rows<G>(a, b, h, L);
-    if (L <= 0 || r0 >= seq_queries(a, b) * a.G) return;
-    const int len = window_span(a, b, L).len, quanta = (len + G::QUANTUM - 1) / G::QUANTUM, shares = window_shares(a, len);
+    const WindowRows rows(a, b, r0);
+    const int L = __builtin_amdgcn_readfirstlane(rows.L);
+    if (a.direct) write_missing_rows<G>(a, b, h, rows.attend() ? r0 + rows.rows : r0, min(r0 + G::RP, a.Qmax * a.G));
+    if (!rows.attend()) return;
+    const int len = rows.span(a).len, quanta = (len + G::QUANTUM - 1) / G::QUANTUM, shares = window_shares(a, len);
     if (share >= shares) return;
     const int c0 = (int)((int64_t)quanta * share / shares) * G::QUANTUM;
     const int c1 = min((int)((int64_t)quanta * (share + 1) / shares) * G::QUANTUM, len);
@@ -635,8 +649,9 @@ __global__ void __launch_bounds__(D) attn_window_rows_merge(StreamLaunch a, Stre
     const int64_t slot = window_slot(a, b, h, row);
     PartialBlock y;
     y.load<D>(a, slot, a.groups, d);
-    const int L = seq_len(a, b), n = L > 0 ? window_shares(a, window_span(a, b, L).len) : 0;
-    const bool real = row < seq_queries(a, b) * a.G;
+    const WindowRows rows(a, b, row / a.RP * a.RP);
+    const int n = rows.attend() ? window_shares(a, rows.span(a).len) : 0;
+    const bool real = row < rows.Q * a.G;
     RowMerge r;
     float num = 0.f;
     y.fold(real ? n : 0, d, r, num);
@@ -733,39 +748,44 @@ void plan_attn_stream(StreamLaunch& a, int n_cu)
 
 // Row tiles and shares of a sequence's window: those that a simple account finds the fastest.  A workgroup takes a fixed time, of which most is code that each of
 // them runs for the first time, more of it the more blocks of rows it has, and its tokens times a rate, that of its arithmetic or what the memory gives to so many workgroups;
-// the chip takes as many rounds as it is filled by; more than one share cost a second launch.  (us a call, 32 / 8 heads of 128: 64 sequences of 4 rows, 2000 tokens: 84
-// in one share; of 36 rows, 500 tokens: 43 in one share; one sequence of 36 rows, 120 tokens: 10.4 in tiles of 16 rows, 14.3 in one of 48; of 72 rows, 2000 tokens:
-// 13.6 and 17.5; eight of 36 rows, 8000 tokens: 55 in one tile, 61 in two.  The division of the whole batch's tokens into equal shares, which unequal lengths ask for, takes 90 and 65.)
-void plan_attn_stream_window(StreamLaunch& a, int n_cu)
+// the chip takes as many rounds as it is filled by; more than one share cost a second launch, and the partials of many row tiles their way.  (us a call, 32 / 8 heads of
+// 128: 64 sequences of 4 rows, 2000 tokens: 84 in one share; of 36 rows, 500 tokens: 43 in one share; one sequence of 36 rows, 120 tokens: 10.4 in tiles of 16 rows, 14.3
+// in one of 48; of 72 rows, 2000 tokens: 13.6 and 17.5; eight of 36 rows, 8000 tokens: 55 in one tile, 61 in two; one of 400 rows, 1000 tokens, tiles of 16, 32, 48, 96: 16,
+// 20, 23, 31; of 1600 rows 58, 39, 44, 31.  The division of the whole batch's tokens into equal shares, which unequal lengths ask for, takes 90 and 65 in the first two.)
+float plan_attn_stream_window(StreamLaunch& a, int n_cu)
 {
-    const int rows = a.Qmax * a.G, all = (rows + 15) / 16;
-    const int64_t span = (int64_t)a.sinks + a.window + a.Qmax + 2 * kWindowStep, tokens = span < a.max_ctx ? span : a.max_ctx;
-    float best = -1.f;
-    int best_rb = all, best_groups = 1;
-    for (int rb = all; rb >= 1; rb = rb > 3 ? 3 : rb - 1) {
+    const int64_t rows = (int64_t)a.Qmax * a.G;
+    float best = INFINITY;
+    int best_rb = 0, best_groups = 1;
+    for (int rb = rows <= kStreamRows ? (int)(rows + 15) / 16 : kStreamRows / 16; rb >= 1; rb = rb > 3 ? 3 : rb - 1) {
         plan_shares(a, rb, 1);
-        const int tiles = (rows + rb * 16 - 1) / (rb * 16);
-        if ((int64_t)a.B * tiles > 65535 && tiles > 1) continue;          // (a grid's second dimension)
-        const int64_t units = (int64_t)a.B * a.Hkv * tiles, most = (tokens + a.quantum - 1) / a.quantum;
-        const float fixed = rb == 1 ? (tiles > 1 ? 9.f : 7.f) : rb == 2 ? 10.f : rb == 3 ? 13.f : 15.f, a_token = 0.005f + 0.001f * rb;      // us
+        const int64_t tiles = (rows + rb * 16 - 1) / (rb * 16), units = a.B * tiles * a.Hkv;
+        if (a.B * tiles > 65535) continue;                                 // (a grid's second dimension; B alone is at most that)
+        const int64_t positions = tiles > 1 ? (rb * 16 - 1) / a.G + 2 : a.Qmax;
+        const int64_t span = (int64_t)a.sinks + a.window + positions + 2 * kWindowStep, tokens = span < a.max_ctx ? span : a.max_ctx;
+        const int64_t most = (tokens + a.quantum - 1) / a.quantum;
+        const float fixed = rb == 1 ? (tiles > 1 ? 9.f : 7.f) : rb == 2 ? 12.f : rb == 3 ? 14.f : 17.f, a_token = 0.0055f + 0.0012f * rb;    // us
         const float bytes = 4.f * a.D * (0.35f + 0.65f / tiles);           // of which row tiles beside one another share some
         for (int64_t k = 0; k <= 4; ++k) {                                 // shares that fill k rounds
             int64_t groups = k * n_cu / units;
             groups = groups > most ? most : groups < 1 ? 1 : groups;
             const int64_t grid = units * groups, busy = grid < n_cu ? grid : n_cu, rounds = (grid + n_cu - 1) / n_cu;
             const float from_memory = bytes * (float)busy / 6.8e6f, rate = from_memory > a_token ? from_memory : a_token;
-            const float time = (float)rounds * (fixed + rate * (float)tokens / (float)groups) + (groups > 1 ? 2.5f : 0.f);
-            if (best >= 0.f && time >= best) continue;
+            const float partials = groups == 1 ? 0.f : 2.5f + (tiles > 1 ? (float)grid * (rb * 16 * (a.D + 2) * 8) * 0.25e-6f : 0.f);
+            const float time = (float)rounds * (fixed + rate * (float)tokens / (float)groups) + partials;
+            if (time >= best) continue;
             best = time;
             best_rb = rb;
             best_groups = (int)groups;
         }
     }
+    if (best_rb == 0) return best;
     plan_shares(a, best_rb, 1);
-    a.tiles = (rows + best_rb * 16 - 1) / (best_rb * 16);
+    a.tiles = (int)((rows + best_rb * 16 - 1) / (best_rb * 16));
     a.groups = best_groups;
     a.nslots = a.B * a.groups;
     a.direct = a.groups == 1;
+    return best;
 }
 
 void plan_attn_stream_pair(StreamLaunch& own, StreamLaunch& prefix, int n_cu)

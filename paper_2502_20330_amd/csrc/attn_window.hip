@@ -350,13 +350,15 @@ hipError_t configure_attn_window()
     return hipSuccess;
 }
 
-// Rows a workgroup and shares of its tokens: those that a simple account finds the fastest.  A workgroup takes its tokens times a rate that is
-// 0.17 + 0.83 RP / 256 of that of 256 rows (32K positions of 32 / 8 heads of 128, a window of 4096: 128 rows 2456 us, 192 2175, 256 2121, 320 2065, 384
-// 1949; heads of 64 have half of the products but all of the exponentials, and take as long), and a few us besides; the chip takes as many rounds as it is filled by; shares cost their partials' way to memory and back, and a launch.
-void plan_attn_window(StreamLaunch& a, int n_cu)
+// Rows a workgroup and shares of its tokens: those that a simple account finds the fastest.  A workgroup takes a fixed time, most of it code that it runs for the
+// first time and masks, and its tokens times a rate that is 0.17 + 0.83 RP / 256 of that of 256 rows; the chip takes as many rounds as it is filled by; shares cost their
+// partials' way to memory and back, and a launch.  (us a call, 32 / 8 heads of 128, tiles of 128, 256, 384 rows: 400 rows, windows of 256 and 4096: 27, 38, 53 and
+// 88, 149, 202 in one share, 22.5 and 36 in eight; 6400 rows, 1000 tokens: 79, 65, 88; 24000 rows: 237, 191, 180; 32K positions, a window of 4096: 2456, 2121, 1949, and
+// with 192 rows 2175, with 320 2065.  Heads of 64 take 0.6 to 0.8 of the times, in small calls, and the same in large ones.)
+float plan_attn_window(StreamLaunch& a, int n_cu)
 {
     const int64_t R = (int64_t)a.Qmax * a.G, units = (int64_t)a.B * a.Hkv;
-    float best = -1.f;
+    float best = INFINITY;
     for (int rows : kRowTiles) {
         int quantum = 0;
         (void)with_rows(a.D, rows, [&](auto geo) {
@@ -366,14 +368,14 @@ void plan_attn_window(StreamLaunch& a, int n_cu)
         const int64_t tiles = (R + rows - 1) / rows, grid = units * tiles;
         const int64_t span = (int64_t)a.sinks + a.window + rows / a.G + 2 * 64, tokens = span < a.max_ctx ? span : a.max_ctx;
         const int64_t most = (tokens + quantum - 1) / quantum;
-        const float a_token = (0.17f + 0.83f / 256 * rows) * 0.032f;        // us
+        const float fixed = 13.f + rows / 16.f, a_token = (0.17f + 0.83f / 256 * rows) * 0.028f;       // us
         for (int k = 0; k <= 3; ++k) {
             int64_t groups = k * n_cu / grid;
             groups = groups > most ? most : groups < 1 ? 1 : groups;
             const int64_t rounds = (grid * groups + n_cu - 1) / n_cu;
-            const float partials = groups > 1 ? 6.f + (float)(grid * groups) * (rows * (a.D + 2) * 8) * 0.25e-6f : 0.f;
-            const float time = (float)rounds * (6.f + a_token * (float)tokens / (float)groups) + partials;
-            if (best >= 0.f && time >= best) continue;
+            const float partials = groups > 1 ? 2.f + (float)(grid * groups) * (rows * (a.D + 2) * 8) * 0.04e-6f : 0.f;
+            const float time = (float)rounds * (fixed + a_token * (float)tokens / (float)groups) + partials;
+            if (time >= best) continue;
             best = time;
             a.RP = rows;
             a.tiles = (int)tiles;
@@ -384,6 +386,7 @@ void plan_attn_window(StreamLaunch& a, int n_cu)
     a.nslots = a.groups;
     a.rot = 0;
     a.direct = a.groups == 1;
+    return best;
 }
 
 size_t attn_window_workspace_bytes(const StreamLaunch& a)

@@ -365,13 +365,12 @@ StreamLaunch plan_quant(const rapid_ctx* ctx, const rapid_attn_shape* s, const A
     plan_attn_stream(a, compute_units(ctx));
     return a;
 }
-// A window: few rows a kv head are packed and stream the tokens, more are cut into row tiles.
-bool few_rows(const rapid_attn_shape* s) { return (int64_t)s->q_max * (s->n_q_heads / s->n_kv_heads) <= kStreamRows; }
+// A window.
 int check_window_shape(const rapid_attn_shape* s, int window, int sinks)
 {
     int rc = check_attn_shape(s, false);
     if (rc == RAPID_OK && (window < 1 || sinks < 0)) rc = RAPID_EINVAL;
-    if (rc == RAPID_OK && few_rows(s)) rc = check_attn_shape(s);
+    if (rc == RAPID_OK && (int64_t)s->q_max * (s->n_q_heads / s->n_kv_heads) <= kStreamRows) rc = check_attn_shape(s);
     if (rc == RAPID_OK) rc = check_tokens(s->batch, s->max_ctx);
     if (rc != RAPID_OK) return rc;
     // packed rows are counted in 32 bits, and a grid has 2^32 threads, 512 a row tile
@@ -384,9 +383,15 @@ StreamLaunch plan_window(const rapid_ctx* ctx, const rapid_attn_shape* s, int wi
     StreamLaunch a = stream_shape(s, own);
     a.window = window < s->max_ctx ? window : s->max_ctx;                  // (more is all there is)
     a.sinks = sinks < s->max_ctx ? sinks : s->max_ctx;
-    if (few_rows(s)) plan_attn_stream_window(a, compute_units(ctx));
-    else plan_attn_window(a, compute_units(ctx));
-    return a;
+    // up to kStreamRows the streaming kernel; beyond, it or the one of many rows, whichever is expected to be the faster (one sequence of 32 / 8 heads of 128: 220 rows,
+    // 1300 tokens 15.5 us and 33.4; 1600 rows, 1000 tokens 31 and 40, 4000 tokens 70 and 57)
+    const int64_t rows = (int64_t)s->q_max * a.G;
+    StreamLaunch many = a;
+    many.many = 1;
+    const bool small = (int64_t)s->batch * s->q_max * s->n_q_heads * s->head_dim * 2 < (int64_t)1 << 32;       // (of q)
+    const float t = small ? plan_attn_stream_window(a, compute_units(ctx)) : INFINITY;
+    if (rows <= kStreamRows) return a;
+    return plan_attn_window(many, compute_units(ctx)) < t ? many : a;
 }
 // The sequences' own tokens, and the shared prefix with the rows of all of them.
 struct PrefixPlan {
@@ -1169,7 +1174,7 @@ size_t rapid_verify_attn_window_workspace_bytes(const rapid_ctx* ctx, const rapi
 {
     if (check_window_shape(shape, window, sinks) != RAPID_OK) return 0;
     const StreamLaunch a = plan_window(ctx, shape, window, sinks, AttnSource{});
-    return few_rows(shape) ? attn_stream_workspace_bytes(a) : attn_window_workspace_bytes(a);
+    return a.many ? attn_window_workspace_bytes(a) : attn_stream_workspace_bytes(a);
 }
 
 int rapid_verify_attn_window(rapid_ctx* ctx, const rapid_attn_shape* shape, int window, int sinks,
@@ -1183,12 +1188,11 @@ int rapid_verify_attn_window(rapid_ctx* ctx, const rapid_attn_shape* shape, int 
     if (!q || !k_cache || !v_cache || !ctx_lens || !out) return RAPID_EINVAL;
     if (shape->page_size != 0 && !page_table) return RAPID_EINVAL;
     if (!aligned(q, 16) || !aligned(k_cache, 16) || !aligned(v_cache, 16) || !aligned(out, 16)) return RAPID_EALIGN;
-    const bool few = few_rows(shape);
     StreamLaunch a = plan_window(ctx, shape, window, sinks, source_of(shape, k_cache, v_cache, page_table));
-    const size_t need = few ? attn_stream_workspace_bytes(a) : attn_window_workspace_bytes(a);
+    const size_t need = a.many ? attn_window_workspace_bytes(a) : attn_stream_workspace_bytes(a);
     if (!workspace || !aligned(workspace, 256) || workspace_bytes < need) return RAPID_EWORKSPACE;
-    if (few) bind_attn_stream(a, workspace);
-    else bind_attn_window(a, workspace);
+    if (a.many) bind_attn_window(a, workspace);
+    else bind_attn_stream(a, workspace);
     a.q = static_cast<const uint16_t*>(q);
     a.out = static_cast<uint16_t*>(out);
     a.lse_out = lse_out;
@@ -1197,8 +1201,8 @@ int rapid_verify_attn_window(rapid_ctx* ctx, const rapid_attn_shape* shape, int 
     hipStream_t st = static_cast<hipStream_t>(stream);
     DeviceScope dev(ctx->device);
     if (dev.err != hipSuccess) return hip_fail(ctx, dev.err);
-    hipError_t e = few ? launch_attn_stream(a, st) : launch_attn_window(a, st);
-    if (e == hipSuccess && few && !a.direct) e = launch_attn_stream_merge(a, StreamLaunch{}, st);
+    hipError_t e = a.many ? launch_attn_window(a, st) : launch_attn_stream(a, st);
+    if (e == hipSuccess && !a.many && !a.direct) e = launch_attn_stream_merge(a, StreamLaunch{}, st);
     if (e != hipSuccess) return hip_fail(ctx, e);
     return RAPID_OK;
 }

@@ -281,6 +281,84 @@ def test_streams_and_graphs_at_once():
         assert all(torch.equal(a, w) for a, w in zip(outs + eager, want + want))
 
 
+# Calls that have enough row tiles to fill the chip go to the kernel of many rows; the ones above, for the most part, to that of few rows in tiles.
+FULL = [(4, 200, 32, 8, 128, 0), (2, 800, 24, 8, 64, 16), (2, 800, 32, 8, 64, 0), (4, 800, 24, 8, 64, 64), (4, 800, 28, 4, 64, 0),
+        (1, 600, 8, 8, 4000, 16), (4, 30, 32, 8, 4096, 0), (1, 800, 32, 8, 4000, 0)]
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("B,Q,hq,hkv,window,page", FULL)
+def test_every_row_tile_of_a_full_chip(d, B, Q, hq, hkv, window, page):
+    """Row tiles of 128 to 384, in one share of the tokens and in several; full sequences, ones shorter than their rows, an empty one."""
+    rng = np.random.default_rng(Q + B + d)
+    cap = Q + 700 if window < 700 else Q + window
+    lens, gammas = [cap, Q // 2, 0, Q][:B], [Q - 1, Q - 1, 2, Q - 9][:B]
+    some = np.concatenate([[0, 1, Q // 2, Q // 2 + 1, Q - 2, Q - 1], rng.integers(0, Q, 4)])
+    Batch(rng, lens, gammas, Q, hq, hkv, d, window, 5, page, cap).check("head", rows=some)
+
+
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+@pytest.mark.parametrize("d", [64, 128])
+def test_what_is_not_finite_in_many_rows(bad, d):
+    rng = np.random.default_rng(21)
+    Q, hq, hkv, L = 200, 32, 8, 600
+    for n in "vk":
+        batch = Batch(rng, [L, 500, 450, 300], [Q - 1] * 4, Q, hq, hkv, d, 50, 3)
+        for token, head, column in ((2, 0, 5), (L - Q + 2 - 50, hkv - 1, 7), (L - Q + 4 - 50, 0, 9), (L - 2, 0, 1), (L - Q + 3, hkv - 1, 2)):
+            batch.x[n][0][token, head, column] = bad
+        if n == "k" and not np.isnan(bad):                   # (as above)
+            out = rapid().rapid_verify_attn_window(batch.q.cuda(), *batch.caches("token"), i32(batch.lens), 50, **batch.kw())
+        else:
+            out = batch.check(rows=np.concatenate([np.arange(6), np.arange(Q - 4, Q)]))
+        assert torch.isfinite(out[1:]).all()
+        if n == "v":
+            g = hq // hkv
+            assert torch.isfinite(out[0, 4:Q - 2, (hkv - 1) * g:, 7]).all() and not torch.isfinite(out[0, 0, (hkv - 1) * g:, 7]).any()
+            assert not torch.isfinite(out[0, :, :g, 5]).any()
+
+
+@pytest.mark.parametrize("Q,window", [(200, 100), (30, 4096)])
+def test_captured_calls_of_many_rows(Q, window):
+    """One graph for every length up to the bound, rows that attend nothing among them; eager calls between its replays."""
+    rng = np.random.default_rng(22)
+    cap = 4200
+    batch = Batch(rng, [cap] * 4, [Q - 1] * 4, Q, 32, 8, 64, window, 10)
+    r, lens = rapid(), i32(batch.lens)
+    c = [torch.stack(batch.x[n]).cuda() for n in "kv"]
+    q, kw = batch.q.cuda(), batch.kw()
+    out = torch.empty_like(q)
+    r.rapid_verify_attn_window(q, *c, lens, window, out=out, **kw)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        r.rapid_verify_attn_window(q, *c, lens, window, out=out, **kw)
+    whole = batch.x
+    for now in ([cap, 0, Q, 4100], [Q - 3, cap, 1, 2000], [1111, 33, cap, Q + 1]):
+        lens.copy_(i32(now))
+        out.fill_(9.0)
+        graph.replay()
+        eager = r.rapid_verify_attn_window(q, *c, lens, window, **kw)
+        torch.cuda.synchronize()
+        assert torch.equal(out, eager)
+        batch.lens = batch.real = now
+        batch.x = {n: [x[:m] for x, m in zip(whole[n], now)] for n in "kv"}
+        batch.seen = [seen_by(m, Q, Q, window, 10) for m in now]
+        batch.compare(out, None, rows=np.array([0, 1, Q // 2, Q - 1]))
+
+
+def test_pages_of_many_rows_that_are_given_away():
+    rng = np.random.default_rng(23)
+    Q = 200
+    batch = Batch(rng, [900, 1000, 700, 950], [Q - 1] * 4, Q, 32, 8, 64, 100, 20, page=16)
+    want = batch.check(rows=np.array([0, 1, 77, Q - 1]))
+    table = batch.table.copy()
+    for b, n in enumerate(batch.lens):
+        gone = np.arange(-(-20 // 16), (n - Q - 100 + 1) // 16)
+        table[b, gone] = rng.choice([-7, 1 << 30, 0, 3], len(gone))
+    out = rapid().rapid_verify_attn_window(batch.q.cuda(), *batch.caches("token"), i32(batch.lens), 100,
+                                           **dict(batch.kw(), page_table=torch.from_numpy(table).cuda()))
+    assert torch.equal(out, want)
+
+
 def test_a_drafters_prompt_and_steps():
     """The calls as they are used: the prompt's keys are rotated into the cache and attended, then single tokens, on the head in 8-bit integers and
     the draw; every attention is that of the rotated rows in 64 bits."""
