@@ -3,9 +3,10 @@
 // Codes and scales are those of quant_rows.hip: a scale for each row of h and for each vocabulary entry.  The sums are exact in 32 bits (127^2 times
 // up to 2^17 terms stays below 2^31).  Half of the bytes of bf16 weights, which are what bounds the head; the matrix instruction takes 64 codes of a row
 // where that of bf16 takes 32 numbers, from the same 16 bytes a lane, so that tiles, rings and swizzle are those of lm_head.hip
-// (lm_head_stream.h).  Measured, 4096 x 128256 (525 MB, 75.6 us at the rate of a pure read), with the launch that brings h to codes: one row 81.6 us (the
-// product alone 77), 72 rows 98.4, of which about 15 are the logits' stores; 11 rows of 3584 x 152064 89.8 (79.5).
+// (lm_head_stream.h).  Measured, 4096 x 128256 (525 MB, 75.6 us at the rate of a pure read): one row 79.2 us; with the launch that brings h to codes, 72 rows 96 to 98, of
+// which about 15 are the logits' stores; 11 rows of 3584 x 152064 90 (79.5).
 #include "lm_head_stream.h"
+#include "row_codes.h"
 
 namespace {
 
@@ -105,7 +106,114 @@ __global__ void __launch_bounds__(kWaves * 64) lm_head_split(LmHeadLaunch a)
         for (int rb = 0; rb < NR; ++rb)
 #pragma unroll
             for (int w = 0; w < kWaves; ++w) sum[0][rb] += part[((w * kSplitBlocks + wave) * NR + rb) * 64 + lane];
-    finish<Int8Elements, NR>(a, sum, wave < nb ? 1 : 0, v0, reinterpret_cast<float*>(smem + kWaves * kRing));
+    finish<Int8Elements, NR>(a, a.h_scales, sum, wave < nb ? 1 : 0, v0, reinterpret_cast<float*>(smem + kWaves * kRing));
+}
+
+// Few rows that are short: the workgroups bring them to codes by themselves, while their first tiles of W are on the way, which spares a launch and its end.
+// The rows go HBM -> LDS into the slot of each wave's ring that is filled last, a wave takes every fourth piece of 512 values, and the codes stay in LDS: row r's
+// chunk c of 16 codes at c ^ r, so that rows do not meet in a bank.  (One row of 4096 x 128256 80.6 -> 79.2 us, 2048 x 128256 43.7 -> 41.8, 1024 x 50000 12.9 -> 11.2,
+// eight rows of that 13.5 -> 13.0, one of 8192 x 32000 43.7 -> 43.3; beyond, every workgroup doing all rows costs more: 16 rows of 1024 x 50000 13.9 and 15.3.)
+constexpr int kOwnCodes = 8192;                          // n_rows * hidden at most
+struct OwnCodes {
+    static constexpr int CODES = lds_bytes(), SCALES = CODES + kOwnCodes, PART = SCALES + 16 * 4, LDS = PART + kOwnCodes / 512 * 4;
+};
+static_assert(kOwnCodes / kWaves * 2 <= Tile<512>::BYTES, "pieces of a wave, in a slot of its ring");
+bool own_codes(const LmHeadLaunch& a) { return a.n_rows <= 16 && a.hidden % 512 == 0 && (int64_t)a.n_rows * a.hidden <= kOwnCodes && a.nb > kSplitBlocks; }
+__global__ void __launch_bounds__(kWaves * 64) lm_head_own_codes(LmHeadLaunch a, const uint16_t* h)
+{
+    using T = Tile<512>;
+    extern __shared__ __attribute__((aligned(1024))) char smem[];
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int ln = lane & 15, lg = lane >> 4;
+    const int nb = a.nb, nbw = (nb + kWaves - 1 - wave) / kWaves, v0 = blockIdx.x * nb * 16;
+    const uint32_t row_bytes = (uint32_t)a.row_bytes;    // (the hidden size: rows are whole slabs)
+    const int nslab = a.row_bytes / 512, s0 = first_slab<Int8Elements>(nslab);
+    char* ring = smem + wave * kRing;
+    const uint32_t ring_lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)smem + wave * kRing;
+    char* codes = smem + OwnCodes::CODES;
+    float* scales = reinterpret_cast<float*>(smem + OwnCodes::SCALES);
+    uint32_t* part = reinterpret_cast<uint32_t*>(smem + OwnCodes::PART);       // the largest magnitude of each piece
+
+    const int mine = (a.n_rows * nslab + kWaves - 1 - wave) / kWaves;          // pieces wave, wave + 4, ..: at most 4
+    for (int i = 0; i < mine; ++i)
+        dma16_keep(reinterpret_cast<const char*>(h), (uint32_t)((wave + i * kWaves) * 1024 + lane * 16), ring_lds + T::AHEAD * T::BYTES + i * 1024);
+    uint32_t woff[T::NLD];
+#pragma unroll
+    for (int e = 0; e < T::NLD; ++e) {
+        const int row = T::RPI * e + lane / T::CPR;
+        woff[e] = (uint32_t)row * row_bytes + (uint32_t)((lane % T::CPR) ^ (row & 15)) * 16u;
+    }
+    int ps = 0, pj = 0, pt = 0;                          // next tile to request: slab, block, linear number
+    auto request_next = [&]() {
+        const uint32_t dst = ring_lds + (pt & (T::SLOTS - 1)) * T::BYTES;
+        if (ps < nslab) {
+            const char* base = static_cast<const char*>(a.w) + (int64_t)loaded_row0(a, v0 + (pj * kWaves + wave) * 16) * row_bytes +
+                               slab_of<Int8Elements>(ps, s0, nslab) * 512;
+#pragma unroll
+            for (int e = 0; e < T::NLD; ++e) dma16(base, woff[e], dst + e * 1024);
+        } else {                                         // past the end: the first piece of h keeps the count uniform
+#pragma unroll
+            for (int e = 0; e < T::NLD; ++e) dma16_keep(reinterpret_cast<const char*>(h), (uint32_t)lane * 16u, dst + e * 1024);
+        }
+        ++pt;
+        if (++pj >= nbw) { pj = 0; ++ps; }
+    };
+    if (nbw > 0) {
+#pragma unroll
+        for (int j = 0; j < T::AHEAD; ++j) request_next();
+        wait_loads<T::AHEAD * T::NLD>();                 // this wave's pieces of h have landed
+    } else {
+        wait_loads<0>();
+    }
+    const char* raw = ring + T::AHEAD * T::BYTES + lane * 16;
+#pragma unroll 1
+    for (int i = 0; i < mine; ++i) {
+        const uint32_t m = wave_max(largest_two(*reinterpret_cast<const u32x4*>(raw + i * 1024), 0));
+        if (lane == 0) part[wave + i * kWaves] = m;
+    }
+    __syncthreads();
+#pragma unroll 1
+    for (int i = 0; i < mine; ++i) {
+        const int q = wave + i * kWaves, r = q / nslab, x = q - r * nslab;     // piece x of row r
+        const uint32_t m = wave_max(lane < nslab ? part[r * nslab + lane] : 0);
+        const int chunk = x * 32 + lane / 2;
+        *reinterpret_cast<u32x2*>(codes + r * row_bytes + (chunk ^ r) * 16 + lane % 2 * 8) = Divisor(m).codes(*reinterpret_cast<const u32x4*>(raw + i * 1024));
+        if (x == 0 && lane == 0) scales[r] = scale_of(m);
+    }
+    lds_reads_done();                                    // the last slot is free from here on
+    __syncthreads();
+
+    intx4 acc[kNBW][1];
+#pragma unroll
+    for (int j = 0; j < kNBW; ++j) acc[j][0] = intx4{0, 0, 0, 0};
+    if (nbw > 0) {
+        const int r = min(ln, a.n_rows - 1);
+        const char* my_row = codes + r * row_bytes;
+        const int rd_row = ln * 512;
+        int t = 0;
+        for (int s = 0; s < nslab; ++s) {
+            const int first = slab_of<Int8Elements>(s, s0, nslab) * 32 + lg;
+            intx4 hreg[T::KS];
+#pragma unroll
+            for (int ks = 0; ks < T::KS; ++ks) hreg[ks] = *reinterpret_cast<const intx4*>(my_row + ((first + ks * 4) ^ r) * 16);
+#pragma unroll
+            for (int j = 0; j < kNBW; ++j) {
+                if (j < nbw) {
+                    wait_loads<(T::AHEAD - 1) * T::NLD>();
+                    request_next();
+                    const char* tile = ring + (t & (T::SLOTS - 1)) * T::BYTES;
+                    ++t;
+#pragma unroll
+                    for (int ks = 0; ks < T::KS; ++ks)
+                        acc[j][0] = Int8Elements::mma(*reinterpret_cast<const intx4*>(tile + rd_row + (((ks * 4 + lg) ^ ln) * 16)), hreg[ks], acc[j][0]);
+                    lds_reads_done();
+                }
+            }
+        }
+        wait_loads<0>();
+    }
+    finish<Int8Elements, 1>(a, scales, acc, nbw, v0, reinterpret_cast<float*>(smem + kWaves * kRing));
 }
 
 enum Kind { kNarrow, kWide, kSplitNarrow, kSplitWide };  // slabs of 256 bytes, of 512
@@ -136,6 +244,8 @@ hipError_t for_build(int nr, Kind kind, F f)
 
 hipError_t configure_lm_head_quant()
 {
+    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(lm_head_own_codes), hipFuncAttributeMaxDynamicSharedMemorySize, OwnCodes::LDS);
+    if (e != hipSuccess) return e;
     for (int nr = 1; nr <= 6; ++nr)
         for (Kind kind : {kNarrow, kWide, kSplitNarrow, kSplitWide}) {
             const hipError_t e = for_build(nr, kind, [](auto kernel, int lds) {
@@ -146,10 +256,17 @@ hipError_t configure_lm_head_quant()
     return hipSuccess;
 }
 
-hipError_t launch_lm_head_quant(const LmHeadLaunch& a, hipStream_t stream)
+hipError_t launch_lm_head_quant(const LmHeadLaunch& a, const QuantRowsLaunch& rows, hipStream_t stream)
 {
     if (a.row_bytes % 256 != 0 || a.nb < 1 || a.nb > kNB) return hipErrorInvalidValue;
     const int nwg = (a.vocab + a.nb * 16 - 1) / (a.nb * 16);
+    if (own_codes(a)) {
+        static_assert(OwnCodes::LDS <= 160 * 1024, "LDS of a compute unit");
+        hipLaunchKernelGGL(lm_head_own_codes, dim3(nwg), dim3(kWaves * 64), OwnCodes::LDS, stream, a, rows.x);
+        return hipGetLastError();
+    }
+    const hipError_t e = launch_quant_rows(rows, stream);
+    if (e != hipSuccess) return e;
     const bool narrow = a.row_bytes % 512 != 0, split = a.nb <= kSplitBlocks;
     return for_build((a.n_rows + 15) / 16, split ? (narrow ? kSplitNarrow : kSplitWide) : narrow ? kNarrow : kWide, [&](auto kernel, int lds) {
         hipLaunchKernelGGL(kernel, dim3(nwg), dim3(kWaves * 64), lds, stream, a);

@@ -156,7 +156,7 @@ __device__ __forceinline__ void epilogue(const LmHeadLaunch& a, const floatx4 (&
 // A sum of 8-bit products becomes a logit: times the row's scale, times the vocabulary entry's.  The sum itself is exact, and three roundings of
 // half a step, 2^-24 of the value, follow: of a sum beyond 2^24, and of either product.
 template <class E, int NR>
-__device__ __forceinline__ void finish(const LmHeadLaunch& a, const typename E::Acc (&acc)[kNBW][NR], int nbw, int v0, float* red)
+__device__ __forceinline__ void finish(const LmHeadLaunch& a, const float* h_scales, const typename E::Acc (&acc)[kNBW][NR], int nbw, int v0, float* red)
 {
     if constexpr (!E::INT8) {
         epilogue<NR>(a, acc, nbw, v0, red);
@@ -165,7 +165,7 @@ __device__ __forceinline__ void finish(const LmHeadLaunch& a, const typename E::
         const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
         float hs[NR];
 #pragma unroll
-        for (int rb = 0; rb < NR; ++rb) hs[rb] = a.h_scales[min(rb * 16 + ln, a.n_rows - 1)];
+        for (int rb = 0; rb < NR; ++rb) hs[rb] = h_scales[min(rb * 16 + ln, a.n_rows - 1)];
         floatx4 z[kNBW][NR];
 #pragma unroll
         for (int jj = 0; jj < kNBW; ++jj) {
@@ -299,7 +299,7 @@ __global__ void __launch_bounds__(kWaves * 64) lm_head_stream(LmHeadLaunch a)
         wait_loads<0>();
     }
 
-    finish<E, NR>(a, acc, nbw, v0, reinterpret_cast<float*>(smem + kWaves * kRing));
+    finish<E, NR>(a, a.h_scales, acc, nbw, v0, reinterpret_cast<float*>(smem + kWaves * kRing));
 }
 
 // ---------------------------------------------------------------- many rows: one copy of h per workgroup
@@ -422,7 +422,7 @@ __global__ void __launch_bounds__(kWaves * 64) lm_head_shared(LmHeadLaunch a)
             }
     }
     wait_loads<0>();
-    finish<E, NR>(a, acc, nbw, v0, reinterpret_cast<float*>(smem + S::HBYTES + kWaves * S::SLOTS * S::UNIT));
+    finish<E, NR>(a, a.h_scales, acc, nbw, v0, reinterpret_cast<float*>(smem + S::HBYTES + kWaves * S::SLOTS * S::UNIT));
 }
 
 }  // namespace

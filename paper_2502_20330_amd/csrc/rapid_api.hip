@@ -838,8 +838,7 @@ int rapid_lm_head_quant(rapid_ctx* ctx, int n_rows, int hidden, int vocab,
     const QuantRowsLaunch rows = quant_rows_of(n_rows, hidden, h, hidden, workspace, const_cast<float*>(a.h_scales));
     DeviceScope dev(ctx->device);
     if (dev.err != hipSuccess) return hip_fail(ctx, dev.err);
-    hipError_t e = launch_quant_rows(rows, static_cast<hipStream_t>(stream));
-    if (e == hipSuccess) e = launch_lm_head_quant(a, static_cast<hipStream_t>(stream));
+    const hipError_t e = launch_lm_head_quant(a, rows, static_cast<hipStream_t>(stream));
     if (e != hipSuccess) return hip_fail(ctx, e);
     return RAPID_OK;
 }

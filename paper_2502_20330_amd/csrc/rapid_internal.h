@@ -117,7 +117,6 @@ struct LmHeadLaunch {
 };
 hipError_t launch_lm_head(const LmHeadLaunch& a, hipStream_t stream);
 hipError_t configure_lm_head();
-hipError_t launch_lm_head_quant(const LmHeadLaunch& a, hipStream_t stream);
 hipError_t configure_lm_head_quant();
 
 // ---- cache bookkeeping (kv_cache.hip)
@@ -195,6 +194,7 @@ struct QuantRowsLaunch {
     int32_t cols, pitch;
 };
 hipError_t launch_quant_rows(const QuantRowsLaunch& a, hipStream_t stream);
+hipError_t launch_lm_head_quant(const LmHeadLaunch& a, const QuantRowsLaunch& rows, hipStream_t stream);       // rows: of h, to a.h and a.h_scales
 
 // ---- retrieval chunk selection (retrieve.hip)
 struct RetrieveLaunch {

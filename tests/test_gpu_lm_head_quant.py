@@ -118,6 +118,50 @@ def test_vocabularies(vocab, rows):
     assert none is None and torch.equal(again, logits)
 
 
+# Short rows of which there are few are brought to codes by the product's own workgroups, where the vocabulary gives each of them more than 32 entries.
+SHORT = [(1, 512), (16, 512), (17, 512), (8, 1024), (9, 1024), (1, 4096), (2, 4096), (3, 4096), (1, 5120), (4, 2048), (5, 1536), (6, 1536), (1, 8192), (1, 8704)]
+
+
+@pytest.mark.parametrize("vocab", [12001, 17000])
+@pytest.mark.parametrize("rows,hidden", SHORT)
+def test_few_short_rows(rows, hidden, vocab):
+    """Either side of both limits; waves without a block; vocabularies that end inside one."""
+    head = Head(np.random.default_rng(rows * hidden + vocab), rows, hidden, vocab)
+    logits, stats = rapid().rapid_lm_head_quant(head.h.cuda(), head.codes, head.scales, temperature=1.3)
+    head.check(logits, stats, temperature=1.3)
+
+
+@pytest.mark.parametrize("rows,hidden", [(4, 512), (8, 1024), (4, 2048)])
+def test_few_short_rows_without_a_scale(rows, hidden):
+    """Zeros, not a number and infinity, each in a row of its own and at either end; the last row is as ever."""
+    head = Head(np.random.default_rng(8), rows, hidden, 10000)
+    head.h[0] = 0
+    head.h[1, hidden - 1], head.h[2, 0] = float("nan"), -float("inf")
+    logits, stats = rapid().rapid_lm_head_quant(head.h.cuda(), head.codes, head.scales)
+    head.check(logits)
+    assert (logits[0] == 0).all() and torch.isnan(logits[1:3]).all() and torch.isfinite(logits[3:]).all() and torch.isfinite(stats[3:]).all()
+
+
+def test_few_short_rows_in_a_graph():
+    """The rows are read by every replay, with eager calls of other sizes between them."""
+    rng = np.random.default_rng(9)
+    head, other = Head(rng, 3, 1024, 20000), Head(rng, 40, 512, 20000)
+    r, h = rapid(), head.h.cuda()
+    logits, _ = r.rapid_lm_head_quant(h, head.codes, head.scales, want_stats=False)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        r.rapid_lm_head_quant(h, head.codes, head.scales, want_stats=False, logits=logits)
+    for k in range(3):
+        head.h = qu.bf16(rng, (3, 1024)) * 2.0 ** k
+        h.copy_(head.h)
+        logits.zero_()
+        graph.replay()
+        eager, _ = r.rapid_lm_head_quant(other.h.cuda(), other.codes, other.scales, want_stats=False)
+        torch.cuda.synchronize()
+        head.check(logits)
+        other.check(eager)
+
+
 def test_sums_beyond_24_bits():
     """All codes 127, the longest rows: 2^17 * 127^2, just below 2^31; and the same with one sign less."""
     h = torch.ones((2, 1 << 17), dtype=torch.bfloat16)
