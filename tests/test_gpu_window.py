@@ -178,10 +178,10 @@ def test_a_window_over_everything_is_plain_attention():
 def test_offsets_past_32_bits():
     """Pages at the far end of pools of 4.6 GB, and a contiguous cache whose second sequence begins past 2^32 bytes."""
     rng = np.random.default_rng(14)
-    for Q in (3, 60):
-        batch = Batch(rng, [500, 400], [Q - 1] * 2, Q, 4, 2, 128, 200, 5, page=16)
-        far = (1 << 32) // (16 * 2 * 128 * 2) + 35000
-        pools = [torch.empty((far, 16, 2, 128), dtype=torch.bfloat16, device="cuda") for _ in "kv"]
+    for Q, hq, hkv in ((3, 4, 2), (60, 4, 2), (400, 32, 8)):             # (the last: the kernel of many rows)
+        batch = Batch(rng, [500, 400], [Q - 1] * 2, Q, hq, hkv, 128, 200, 5, page=16)
+        far = (1 << 32) // (16 * hkv * 128 * 2) + 35000
+        pools = [torch.empty((far, 16, hkv, 128), dtype=torch.bfloat16, device="cuda") for _ in "kv"]
         small = batch.caches("token")
         for pool, c in zip(pools, small):
             pool[-c.shape[0]:] = c
@@ -190,7 +190,7 @@ def test_offsets_past_32_bits():
                                                page_table=table, max_ctx=batch.cap)
         batch.compare(out, None, rows=np.arange(0, Q, 1 + Q // 8))
         del pools, pool
-        batch = Batch(rng, [500, 400], [Q - 1] * 2, Q, 4, 2, 128, 200, 5)
+        batch = Batch(rng, [500, 400], [Q - 1] * 2, Q, hq, hkv, 128, 200, 5)
         wide = []
         for c in batch.caches("token"):
             t = torch.empty((1 << 31) + (1 << 20), dtype=torch.bfloat16, device="cuda")
@@ -200,6 +200,21 @@ def test_offsets_past_32_bits():
         out = rapid().rapid_verify_attn_window(batch.q.cuda(), *wide, i32(batch.lens), 200, sinks=5, gammas=i32(batch.gammas), max_ctx=batch.cap)
         batch.compare(out, None, rows=np.arange(0, Q, 1 + Q // 8))
         del wide, t
+
+
+def test_queries_past_32_bits():
+    """A prompt whose queries and results are 4.3 GB each: rows at both ends and around 2^32 bytes."""
+    g = torch.Generator(device="cuda").manual_seed(15)
+    Q, hq, hkv, d, window = (1 << 19) + 1000, 32, 8, 128, 70
+    q, k, v = (torch.randn((1, Q, n, d), generator=g, device="cuda", dtype=torch.bfloat16) for n in (hq, hkv, hkv))
+    out = rapid().rapid_verify_attn_window(q, k, v, i32([Q]), window, sinks=3)
+    edge = (1 << 32) // (hq * d * 2)
+    for p in (0, 5, 4000, edge - 1, edge, edge + 1, Q - 1):
+        j = sorted(set(range(min(3, p + 1))) | set(range(max(0, p - window + 1), p + 1)))
+        for h in (0, hq - 1):
+            kk, vv = (x[0, j, h // (hq // hkv)].double().cpu().numpy() for x in (k, v))
+            ref, _, w, reach = qu.attention(q[0, p:p + 1, h].double().cpu().numpy(), kk, vv, np.ones((1, len(j)), bool), d ** -0.5)
+            qu.close(out[0, p:p + 1, h].double().cpu().numpy(), ref, qu.tolerance(ref, w, reach, d, len(j)), f"position {p} head {h}")
 
 
 def test_pages_that_are_given_away():
