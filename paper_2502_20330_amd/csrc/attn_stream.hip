@@ -1,4 +1,5 @@
-// Verification attention over a cache in 8 bits (gfx950), and over the sequences' own tokens behind a shared prefix.
+// Verification attention over a cache in 8 bits (gfx950), over the sequences' own tokens behind a shared prefix, and over a sliding window (there the tokens
+// of each sequence, or of each tile of its rows, are divided by themselves: attn_stream_window).
 //
 // The mathematics is that of verify_attn.hip: softmax(scale <q, k>) v with a running maximum m and sum l per query row; partial
 // results (m, l, O) of disjoint token ranges are joined as O = sum 2^(m_i - M) O_i, l likewise.
