@@ -1,9 +1,11 @@
 // sizes(*tensors) -> bytes: what the checks of a call go by, each tensor's type, device, sizes and strides (a single byte for None).
 //
 // A key for the plans that the binding keeps.  Asked for one by one from Python, the four of eleven tensors took 5 us of a call whose kernel takes
-// four; here they are copied out of the tensors in one go.
+// four; here they are copied out of the tensors in one go.  What torch throws on the way (a nested tensor has no sizes, a subclass may have its own
+// in Python) becomes a Python exception: nothing may pass through the interpreter's C frames.
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
+#include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <cstring>
@@ -14,6 +16,7 @@ constexpr int kMostDims = 8, kMostTensors = 32;
 
 PyObject* sizes(PyObject*, PyObject* const* args, Py_ssize_t n)
 {
+    HANDLE_TH_ERRORS
     int64_t words[kMostTensors * (1 + 2 * kMostDims)];
     size_t at = 0;
     if (n > kMostTensors) {
@@ -30,7 +33,7 @@ PyObject* sizes(PyObject*, PyObject* const* args, Py_ssize_t n)
             return nullptr;
         }
         const at::Tensor& t = THPVariable_Unpack(args[i]);
-        const int64_t dims = t.dim();
+        const int64_t dims = t.is_nested() ? kMostDims + 1 : t.dim();
         if (dims > kMostDims || t.layout() != at::kStrided) {
             PyErr_SetString(PyExc_TypeError, "a strided tensor of at most eight dimensions is wanted");
             return nullptr;
@@ -42,6 +45,7 @@ PyObject* sizes(PyObject*, PyObject* const* args, Py_ssize_t n)
         at += 2 * dims;
     }
     return PyBytes_FromStringAndSize(reinterpret_cast<const char*>(words), (Py_ssize_t)(at * sizeof(int64_t)));
+    END_HANDLE_TH_ERRORS
 }
 
 PyMethodDef methods[] = {{"sizes", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(sizes)), METH_FASTCALL, nullptr}, {nullptr, nullptr, 0, nullptr}};

@@ -26,3 +26,25 @@ def test_what_is_no_tensor():
             binding._sizes(bad)
     with pytest.raises(ValueError):
         binding._sizes(*[None] * 33)
+
+
+class NoSizes(torch.Tensor):
+    """A subclass whose sizes are asked for in Python, where there is an error."""
+    @staticmethod
+    def __new__(cls):
+        return torch.Tensor._make_wrapper_subclass(cls, (2, 3), dispatch_sizes_strides_policy="sizes")
+
+    @classmethod
+    def __torch_dispatch__(cls, func, types, args=(), kwargs=None):
+        raise ValueError("no sizes")
+
+
+def test_what_torch_throws_is_an_exception():
+    """Tensors whose sizes or strides torch refuses to give: an error like any other, and the process lives."""
+    rows = [torch.zeros((2, 3)), torch.zeros((4, 3))]
+    for layout in (torch.strided, torch.jagged):
+        with pytest.raises(TypeError):
+            binding._sizes(torch.zeros(2), torch.nested.nested_tensor(rows, layout=layout))
+    with pytest.raises(ValueError, match="no sizes"):
+        binding._sizes(torch.zeros(2), NoSizes())
+    assert binding._sizes(torch.zeros(2), None) == binding._sizes(torch.ones(2), None)
