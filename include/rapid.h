@@ -291,7 +291,8 @@ int rapid_lm_head_stat_chunks(const rapid_ctx* ctx, int vocab, int n_rows);
  * (the weights are read once whatever the row count) and, when `stats` is given, per row and per chunk c of
  * rapid_lm_head_chunk() consecutive entries
  *     stats[r][c] = ( max_v logits[r][v], sum_v exp((logits[r][v] - max) / temperature) )
- * which is what rapid_accept_prestats consumes (the pieces of softmax(z/T), Alg. 1).
+ * which is what rapid_accept_prestats consumes (the pieces of softmax(z/T), Alg. 1).  A logit that is NaN has no part in its chunk's
+ * maximum, and is left out of the sum together with some of the chunk's other entries.
  *
  *   n_rows       1..96 (the gamma+1 rows of one sequence or of a batch, ordered [sequence][position])
  *   hidden       a multiple of 128 (multiples of 256 take the faster path)
@@ -329,7 +330,9 @@ int rapid_quant_rows(rapid_ctx* ctx, int64_t rows, int cols, const void* x, int6
  *   h             bf16 [n_rows, hidden], contiguous, 16-byte aligned
  *   w_codes       int8 [vocab, pitch] (pitch: hidden rounded up to a multiple of 256; what lies behind hidden has no effect), 16-byte aligned
  *   w_scales      fp32 [vocab]
- *   temperature, logits, logits_row_stride, stats   as for rapid_lm_head, with the same chunks
+ *   temperature, logits, logits_row_stride, stats   as for rapid_lm_head, with the same chunks.  A NaN among a chunk's logits makes its sum
+ *                 NaN, and the maximum is that of the numbers: rapid_accept_prestats leaves such a chunk out of the row's sums, as rapid_accept
+ *                 does a slice with a NaN
  *   workspace     >= rapid_lm_head_quant_workspace_bytes(), 256-byte aligned, any content
  */
 size_t rapid_lm_head_quant_workspace_bytes(const rapid_ctx* ctx, int n_rows, int hidden);   /* 0 on bad sizes */
@@ -345,7 +348,7 @@ int rapid_lm_head_quant(rapid_ctx* ctx, int n_rows, int hidden, int vocab,
  *   target_stats fp32 [B*(gamma_max+1), target_chunks, 2] or NULL; row b*(gamma_max+1)+k
  *   draft_stats  fp32 [B*gamma_max,     draft_chunks,  2] or NULL
  * each pair = (max of the raw logits of the chunk, sum exp((z - max)/temperature)) for ANY
- * partition of the vocabulary into chunks (an empty chunk: sum 0, any maximum); the temperature must be the
+ * partition of the vocabulary into chunks (an empty chunk: sum 0, any maximum; a sum that is NaN: left out of the row's sums); the temperature must be the
  * one passed here.  A NULL side is computed from the logits as in rapid_accept.  Everything
  * else, including the workspace size, is as for rapid_accept.
  */

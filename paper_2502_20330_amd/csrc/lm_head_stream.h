@@ -83,7 +83,8 @@ __device__ __forceinline__ int loaded_row0(const LmHeadLaunch& a, int nominal) {
 // acc[jj][rb]: lane (ln, lg) holds, for row rb*16 + ln of h, the four vocabulary
 // entries loaded_row0 + lg*4 .. +3 of block jj.  Logits go out from the registers; the chunk statistics
 // are formed per wave (own maximum) and combined over the four waves by the first threads; red: [kWaves][NR * 16][2].
-template <int NR>
+// A NaN among the logits: NAN_SUM makes the chunk's sum NaN, the maximum is that of the numbers; else the wave that holds it has no part in the sum.
+template <int NR, bool NAN_SUM>
 __device__ __forceinline__ void epilogue(const LmHeadLaunch& a, const floatx4 (&acc)[kNBW][NR], int nbw, int v0, float* red)
 {
     const int tid = threadIdx.x, lane = tid & 63;
@@ -117,7 +118,8 @@ __device__ __forceinline__ void epilogue(const LmHeadLaunch& a, const floatx4 (&
         m = fmaxf(m, __shfl_xor(m, 16));
         m = fmaxf(m, __shfl_xor(m, 32));
         float sum = 0.f;
-        if (m > -INFINITY) {
+        const float base = NAN_SUM && !(m > -INFINITY) ? 0.f : m;           // (entries of -infinity alone: a sum of 0, and of NaN where there is one)
+        if (NAN_SUM || m > -INFINITY) {
 #pragma unroll
             for (int jj = 0; jj < kNBW; ++jj) {
                 const int nominal = v0 + (jj * kWaves + wave) * 16;
@@ -125,7 +127,7 @@ __device__ __forceinline__ void epilogue(const LmHeadLaunch& a, const floatx4 (&
                     const int vi = loaded_row0(a, nominal) + lg * 4;
 #pragma unroll
                     for (int i = 0; i < 4; ++i)
-                        if (vi + i >= nominal) sum += __builtin_amdgcn_exp2f((acc[jj][rb][i] - m) * c);
+                        if (vi + i >= nominal) sum += __builtin_amdgcn_exp2f((acc[jj][rb][i] - base) * c);
                 }
             }
         }
@@ -146,7 +148,7 @@ __device__ __forceinline__ void epilogue(const LmHeadLaunch& a, const floatx4 (&
 #pragma unroll
         for (int w = 0; w < kWaves; ++w) {
             const float mw = red[((w * NR * 16) + tid) * 2], sw = red[((w * NR * 16) + tid) * 2 + 1];
-            if (sw > 0.f) S += sw * __builtin_amdgcn_exp2f((mw - M) * c);
+            if (NAN_SUM ? sw != 0.f : sw > 0.f) S += sw * __builtin_amdgcn_exp2f((mw - M) * c);
         }
         a.stats[((int64_t)tid * gridDim.x + blockIdx.x) * 2 + 0] = M;
         a.stats[((int64_t)tid * gridDim.x + blockIdx.x) * 2 + 1] = S;
@@ -159,7 +161,7 @@ template <class E, int NR>
 __device__ __forceinline__ void finish(const LmHeadLaunch& a, const float* h_scales, const typename E::Acc (&acc)[kNBW][NR], int nbw, int v0, float* red)
 {
     if constexpr (!E::INT8) {
-        epilogue<NR>(a, acc, nbw, v0, red);
+        epilogue<NR, false>(a, acc, nbw, v0, red);
     } else {
         const int lane = threadIdx.x & 63, ln = lane & 15, lg = lane >> 4;
         const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -180,7 +182,7 @@ __device__ __forceinline__ void finish(const LmHeadLaunch& a, const float* h_sca
 #pragma unroll
                 for (int i = 0; i < 4; ++i) z[jj][rb][i] = (float)acc[jj][rb][i] * hs[rb] * ws[i];
         }
-        epilogue<NR>(a, z, nbw, v0, red);
+        epilogue<NR, true>(a, z, nbw, v0, red);
     }
 }
 

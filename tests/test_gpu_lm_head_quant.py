@@ -247,3 +247,51 @@ def test_draws_from_the_quantised_head():
         t = int(tokens[b, 0])
         lo, hi = (0 if t == 0 else c[t - 1]) / c[-1], c[t] / c[-1]
         assert lo - 1e-6 <= float(u[b, 0]) <= hi + 1e-6
+
+
+# One shape for each of the kernels: codes by the product's own workgroups, the hidden dimension shared among the waves (slabs of 512 and of 256 bytes), a copy of h for each
+# wave (likewise), one for the workgroup.
+KERNELS = [(2, 1024, 12001), (5, 512, 5003), (20, 768, 1000), (9, 2304, 12001), (40, 1024, 17000), (72, 1024, 17000)]
+
+
+@pytest.mark.parametrize("rows,hidden,vocab", KERNELS)
+def test_a_chunk_with_a_nan_has_a_sum_that_is_none(rows, hidden, vocab):
+    """Entries without a scale, at either end, beside one another, over a whole chunk; a row without one; a logit that is infinite: a chunk's sum is NaN where the formula's is,
+    its maximum is that of the numbers, and the other chunks' statistics are what they are without."""
+    head = Head(np.random.default_rng(rows + vocab), rows, hidden, vocab)
+    r, chunk = rapid(), rapid().lm_head_chunk(vocab, rows)
+    clean, clean_stats = r.rapid_lm_head_quant(head.h.cuda(), head.codes, head.scales)
+    scales = head.scales.clone()
+    for v in (0, 3 * chunk + 7, 3 * chunk + 8, vocab - 1, *range(5 * chunk, 6 * chunk)):
+        scales[v] = torch.nan
+    scales[7 * chunk + 1] = 1e38                             # (times a scale of about 2^-6 and a sum of some thousands)
+    logits, stats = r.rapid_lm_head_quant(head.h.cuda(), head.codes, scales)
+    z = logits.double().cpu().numpy()
+    assert np.array_equal(np.isnan(z), np.broadcast_to(torch.isnan(scales).cpu().numpy(), z.shape))
+    s, was = (x.double().cpu().numpy() for x in (stats, clean_stats))
+    for j, v0 in enumerate(range(0, vocab, chunk)):
+        part = z[:, v0:v0 + chunk]
+        bad = np.isnan(part).any(1) | (part == np.inf).any(1)
+        numbers = np.where(np.isnan(part), -np.inf, part)
+        assert np.array_equal(s[:, j, 0], numbers.max(1)), j
+        assert np.array_equal(np.isnan(s[:, j, 1]), bad), j
+        if j not in (0, 3, 5, 7, (vocab - 1) // chunk):
+            assert np.array_equal(s[:, j], was[:, j]), j
+    head.h[rows - 1, 0] = torch.nan
+    z, stats = r.rapid_lm_head_quant(head.h.cuda(), head.codes, head.scales)
+    assert torch.isnan(z[rows - 1]).all() and (stats[rows - 1, :, 0] == -torch.inf).all() and torch.isnan(stats[rows - 1, :, 1]).all()
+    assert torch.equal(z[:rows - 1], clean[:rows - 1]) and torch.equal(stats[:rows - 1], clean_stats[:rows - 1])
+
+
+def test_a_draw_leaves_the_chunk_of_a_nan_out():
+    """Of the row's sums: the token is one that there is, whatever the uniform."""
+    vocab, T = 32000, 0.8
+    head = Head(np.random.default_rng(10), 6, 1024, vocab)
+    r, chunk = rapid(), rapid().lm_head_chunk(32000, 6)
+    head.scales[3 * chunk + 5] = torch.nan
+    logits, stats = r.rapid_lm_head_quant(head.h.cuda(), head.codes, head.scales, temperature=T)
+    none = dict(draft_logits=torch.empty((6, 0, vocab), device="cuda"), draft_tokens=torch.empty((6, 0), dtype=torch.int32, device="cuda"))
+    for u in (0.0, 0.3, 0.999):
+        _, tokens, _ = r.rapid_accept(logits[:, None], none["draft_logits"], none["draft_tokens"], 0.0, torch.full((6, 1), u, device="cuda"), temperature=T,
+                                      target_stats=stats)
+        assert ((tokens >= 0) & (tokens < vocab)).all()
