@@ -295,3 +295,30 @@ def test_a_draw_leaves_the_chunk_of_a_nan_out():
         _, tokens, _ = r.rapid_accept(logits[:, None], none["draft_logits"], none["draft_tokens"], 0.0, torch.full((6, 1), u, device="cuda"), temperature=T,
                                       target_stats=stats)
         assert ((tokens >= 0) & (tokens < vocab)).all()
+
+
+def check_row_counts(counts, hidden, vocab, kind):
+    """The first rows of one matrix; `kind` names the kernel that takes them, which goes by the entries a workgroup has and by the width."""
+    head = Head(np.random.default_rng(hidden + vocab), max(counts), hidden, vocab)
+    z, h = head.reference(), head.h
+    assert rapid().lm_head_chunk(vocab) > 32 and {"narrow": hidden % 512 == 256, "wide": hidden % 512 == 0}[kind]
+    for rows in counts:
+        head.h, head.reference = h[:rows].contiguous(), lambda: z[:rows]
+        head.check(*rapid().rapid_lm_head_quant(head.h.cuda(), head.codes, head.scales, temperature=0.9), temperature=0.9)
+
+
+@pytest.mark.parametrize("hidden,vocab", [(512, 17000), (1024, 12001), (1536, 17000), (4096, 12001)])
+def test_row_counts_where_the_waves_share_a_copy(hidden, vocab):
+    """From 49 rows on, with one slab and with several, and what is just below."""
+    check_row_counts([17, 32, 33, 48, 49, 64, 65, 72, 80, 81, 95, 96], hidden, vocab, "wide")
+
+
+@pytest.mark.parametrize("hidden,vocab", [(256, 12001), (768, 17000), (2304, 12001)])
+def test_row_counts_of_narrow_slabs(hidden, vocab):
+    """Rows that are no multiple of 512 bytes: slabs of 256, one and several, at which the workgroups begin in turn."""
+    check_row_counts([1, 2, 16, 17, 33, 48, 49, 64, 65, 81, 96], hidden, vocab, "narrow")
+
+
+@pytest.mark.parametrize("hidden,vocab", [(8192, 9000), (3584, 12001)])
+def test_row_counts_of_wide_rows(hidden, vocab):
+    check_row_counts([2, 16, 31, 47, 60, 96], hidden, vocab, "wide")
