@@ -119,6 +119,34 @@ def test_quotients_of_32_bits_fall_on_the_right_side():
     assert np.where(keep & (got > 0), gap, 1.0).min() >= 2.0 ** -17
 
 
+@pytest.mark.parametrize("off", [0, 1, -1])
+def test_quotients_by_the_reciprocal_fall_on_the_right_side(off):
+    """The kernels' sequence for 127 x / m: r = t (1/m), then r + (t - r m) (1/m), each fused operation rounded once to 32 bits, and the whole number from the last bits of a
+    sum with 1.5 * 2^23; for every two significands of 8 bits and every power of two between them that matters, also with a reciprocal that is one last place off."""
+    f = np.float32
+    wide = np.longdouble                                     # both fused operations are exact in 64 bits before they are rounded
+    assert np.finfo(wide).nmant >= 63
+    m = np.arange(128, 256)[:, None, None]
+    x = np.arange(128, 256)[None, :, None]
+    e = np.arange(0, 12)[None, None, :]
+    keep = (x <= m) | (e > 0)
+    inv = f(1) / m.astype(f)
+    inv = inv if off == 0 else np.nextafter(inv, f(off) * f(np.inf))
+    t = f(127) * x.astype(f) * f(2.0) ** -e.astype(f)
+    r = t * inv
+    rest = (t.astype(wide) - r.astype(wide) * m).astype(f)
+    q = (r.astype(wide) + rest.astype(wide) * inv.astype(wide)).astype(f)
+    assert inv.dtype == t.dtype == r.dtype == q.dtype == f
+    got = (q + f(1.5 * 2 ** 23)).view(np.int32) & 0xff
+    num, den = 127 * x, m << e
+    floor, twice = num // den, 2 * (num % den)
+    want = np.where(twice > den, floor + 1, np.where(twice < den, floor, floor + floor % 2))
+    assert np.array_equal(np.where(keep, got, 0), np.where(keep, want, 0))
+    # of the product with the reciprocal alone this is not so
+    alone = np.rint(t * inv).astype(np.int64)
+    assert off or not np.array_equal(np.where(keep, alone, 0), np.where(keep, want, 0))
+
+
 def window_call(s, window=100, sinks=4, **kw):
     lib = binding.load_library()
     p = dict(ctx=ctx(), q=P, k=P, v=P, lens=P, table=P if s.page_size else None, out=P, ws=P, nbytes=1 << 40)

@@ -322,3 +322,16 @@ def test_row_counts_of_narrow_slabs(hidden, vocab):
 @pytest.mark.parametrize("hidden,vocab", [(8192, 9000), (3584, 12001)])
 def test_row_counts_of_wide_rows(hidden, vocab):
     check_row_counts([2, 16, 31, 47, 60, 96], hidden, vocab, "wide")
+
+
+def test_borders_between_codes_of_all_maxima():
+    """All quotients of two 8-bit significands, over twelve powers of two, a row for each maximum."""
+    x = np.concatenate([np.arange(128, 256) * 2.0 ** -e for e in range(12)])
+    rows = np.zeros((128, 2 * len(x) + 8))
+    for i, top in enumerate(range(128, 256)):
+        y = np.concatenate([[top], x[x <= top]])
+        rows[i, :2 * len(y)] = np.concatenate([y, -y])
+    for scale in (0, 63, 100, -63, -110, 119, -124):
+        t = torch.from_numpy(np.ldexp(rows, scale)).to(torch.bfloat16)
+        assert torch.isfinite(t).all()
+        check_rows(t, *rapid().rapid_quant_rows(t.cuda()), t.shape[1])
