@@ -527,6 +527,9 @@ int rapid_kv_append_rope_quant(rapid_ctx* ctx, const rapid_attn_shape* shape, co
  *   workspace     >= rapid_verify_attn_window_workspace_bytes(), 256-byte aligned, any content
  */
 size_t rapid_verify_attn_window_workspace_bytes(const rapid_ctx* ctx, const rapid_attn_shape* shape, int window, int sinks);   /* 0 on a bad shape */
+/* How a call of this shape is divided: plan[0] the packed rows (q_max * group of a sequence and kv head) that a workgroup takes, plan[1] the shares that the
+ * tokens of each such row tile are cut into (1: one launch, no partial results), plan[2] 1 for the kernel of many rows, 0 for the streaming one. */
+int rapid_verify_attn_window_plan(const rapid_ctx* ctx, const rapid_attn_shape* shape, int window, int sinks, int32_t* plan);
 int rapid_verify_attn_window(rapid_ctx* ctx, const rapid_attn_shape* shape, int window, int sinks,
                              const void* q, const void* k_cache, const void* v_cache,
                              const int32_t* ctx_lens, const int32_t* gammas, const int32_t* page_table,

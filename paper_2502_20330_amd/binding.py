@@ -27,7 +27,7 @@ EXPORTS = ["rapid_create", "rapid_destroy", "rapid_strerror", "rapid_last_hip_er
            "rapid_kv_commit_pages",
            "rapid_kv_append_quant", "rapid_kv_read_quant", "rapid_verify_attn_quant", "rapid_verify_attn_quant_workspace_bytes",
            "rapid_verify_attn_prefix", "rapid_verify_attn_prefix_workspace_bytes",
-           "rapid_verify_attn_window", "rapid_verify_attn_window_workspace_bytes",
+           "rapid_verify_attn_window", "rapid_verify_attn_window_workspace_bytes", "rapid_verify_attn_window_plan",
            "rapid_kv_append_rope", "rapid_kv_append_rope_quant", "rapid_quant_rows", "rapid_lm_head_quant",
            "rapid_lm_head_quant_workspace_bytes",
            "rapid_retrieve", "rapid_hbm_read_probe"]
@@ -151,6 +151,8 @@ def load_library() -> ctypes.CDLL:
     lib.rapid_verify_attn_prefix.restype = ctypes.c_int
     lib.rapid_verify_attn_window_workspace_bytes.argtypes = [vp, shape_p, ctypes.c_int, ctypes.c_int]
     lib.rapid_verify_attn_window_workspace_bytes.restype = ctypes.c_size_t
+    lib.rapid_verify_attn_window_plan.argtypes = [vp, shape_p, ctypes.c_int, ctypes.c_int, i32p]
+    lib.rapid_verify_attn_window_plan.restype = ctypes.c_int
     lib.rapid_verify_attn_window.argtypes = [vp, shape_p, ctypes.c_int, ctypes.c_int, vp, vp, vp, i32p, i32p, i32p, vp, f32p,
                                              vp, ctypes.c_size_t, vp]
     lib.rapid_verify_attn_window.restype = ctypes.c_int

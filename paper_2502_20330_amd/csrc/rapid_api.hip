@@ -1176,6 +1176,18 @@ size_t rapid_verify_attn_window_workspace_bytes(const rapid_ctx* ctx, const rapi
     return a.many ? attn_window_workspace_bytes(a) : attn_stream_workspace_bytes(a);
 }
 
+int rapid_verify_attn_window_plan(const rapid_ctx* ctx, const rapid_attn_shape* shape, int window, int sinks, int32_t* plan)
+{
+    if (!plan) return RAPID_EINVAL;
+    const int rc = check_window_shape(shape, window, sinks);
+    if (rc != RAPID_OK) return rc;
+    const StreamLaunch a = plan_window(ctx, shape, window, sinks, AttnSource{});
+    plan[0] = a.RP;
+    plan[1] = a.groups;
+    plan[2] = a.many;
+    return RAPID_OK;
+}
+
 int rapid_verify_attn_window(rapid_ctx* ctx, const rapid_attn_shape* shape, int window, int sinks,
                              const void* q, const void* k_cache, const void* v_cache,
                              const int32_t* ctx_lens, const int32_t* gammas, const int32_t* page_table,
