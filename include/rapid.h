@@ -323,7 +323,8 @@ int rapid_quant_rows(rapid_ctx* ctx, int64_t rows, int cols, const void* x, int6
 /*
  * rapid_lm_head on an output embedding in 8-bit integers (rapid_quant_rows of it): the rows of h are brought to codes in the same way, and
  *     logits[r][v] = s_h[r] * w_scales[v] * sum_k c_h[r][k] * w_codes[v][k]
- * The sum is exact; at most three roundings of 2^-24 follow.  Half of the bytes of bf16 weights.  Made for a drafter: whatever its distribution
+ * The sum is exact; at most three roundings of 2^-24 follow (the sum's, that of its product with s_h, and that of this with w_scales; what leaves the
+ * range of normal fp32 numbers on the way is rounded as such).  Half of the bytes of bf16 weights.  Made for a drafter: whatever its distribution
  * is, rapid_accept takes it into account, as long as the drafts were drawn from these very logits.  A row of h with a NaN or an infinity
  * has logits that are NaN, and so does an entry whose scale is NaN.
  *   n_rows 1..96, hidden a multiple of 8 and at most 2^17, vocab >= 16

@@ -8,8 +8,8 @@
 // attn_prefix.hip: eight waves hold the rows, the tokens go HBM -> LDS once a workgroup, and a row tile's neighbours, which read nearly the same
 // tokens, follow it on the same die, whose L2 serves them: with the hint that a tile is read once, which serves the other kernels, 384 rows of 32K positions took
 // 2272 us instead of 1949.
-// Measured (32K positions, 32 / 8 heads of 128, a window of 4096 and 64 sinks, 2.09 TFLOP of scores that count): 1947 us, 1073 TFLOP/s, where a large product of the
-// library reaches 1295.  By counters the clock is held at 2.0 GHz, the matrix cores are busy in 44 % of the cycles, LDS in 15 %, 88 % of the L2's requests hit.  What the chip
+// Measured (32K positions, 32 / 8 heads of 128, a window of 4096 and 64 sinks, 2.09 TFLOP of scores that count): 1950 to 2030 us from card to card, 1030 to 1073 TFLOP/s, where a large
+// product of the library reaches 1295.  By counters the clock is held at 2.0 GHz, the matrix cores are busy in 44 % of the cycles, LDS in 15 %, 88 % of the L2's requests hit.  What the chip
 // may draw bounds it as much as anything: with 256 rows the same loop without softmax and loads takes 1520 us, without loads 1850, and a schedule that
 // interleaves products and exponentials of neighbouring tiles in each wave (their issue then overlaps by the listing) 2120 like this one.
 #include "attn_rows.h"

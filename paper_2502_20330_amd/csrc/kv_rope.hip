@@ -139,8 +139,8 @@ __global__ void __launch_bounds__(kMostThreads) kv_append_rope(KvRopeLaunch a)
 
 // A row of q, k and v to a workgroup, with as many threads as its heads take, or the half, third .. of them that is at most 512.  The more workgroups a compute
 // unit has, the more of their waits for lengths, pages and angles pass under others' loads, but a thread that has a second head to do waits twice.
-// 64K rows of 32 / 8 / 8 heads of 128, which take 384 threads: 287 us with these, 295 with 256, 301 with 128, 310 with 64 (two rows to a workgroup: 307, four
-// 317, eight 334); 72 such rows 3.4, 4.9 with 64; 2800 rows of 16 / 8 / 8 heads of 64 in 8 bits, which take 128: 8.5, 10.2 with 256, 13.7 with 384.
+// 64K rows of 32 / 8 / 8 heads of 128, which take 384 threads: 282 us with these, 292 with 256, 297 with 128, 307 with 64 (two rows to a workgroup: 20 us more, four
+// 30, eight 47); into 8 bits 281, with 256 threads 272; 72 such rows 3.3, 4.9 with 64, in 8 bits 3.6 and 5.3; 2800 rows of 16 / 8 / 8 heads of 64 in 8 bits, which take 128: 8.5, 10.2 with 256, 13.7 with 384.
 template <int D, bool QUANT, bool ADJACENT>
 hipError_t launch(const KvRopeLaunch& a, hipStream_t stream)
 {
