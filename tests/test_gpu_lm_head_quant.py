@@ -335,3 +335,25 @@ def test_borders_between_codes_of_all_maxima():
         t = torch.from_numpy(np.ldexp(rows, scale)).to(torch.bfloat16)
         assert torch.isfinite(t).all()
         check_rows(t, *rapid().rapid_quant_rows(t.cuda()), t.shape[1])
+
+
+@pytest.mark.parametrize("eta", [0.0, 5.0])
+def test_the_accept_pass_leaves_a_sum_that_is_nan_out(eta):
+    """Ratios, tokens and counts are those with a chunk of no weight, on either side and on both; a chunk that does not hold the row's maximum."""
+    B, g, vocab = 2, 3, 32000
+    head = Head(np.random.default_rng(11), B * (2 * g + 1), 1024, vocab)
+    logits, stats = rapid().rapid_lm_head_quant(head.h.cuda(), head.codes, head.scales)
+    zt, zd = logits[:B * (g + 1)].reshape(B, g + 1, vocab).contiguous(), logits[B * (g + 1):].reshape(B, g, vocab).contiguous()
+    st, sd = stats[:B * (g + 1)].contiguous(), stats[B * (g + 1):].contiguous()
+    tokens, u = zd.argmax(-1).int(), torch.full((B, g + 1), 0.6, device="cuda")
+    for sides in ((st,), (sd,), (st, sd)):
+        results = []
+        for weight in (0.0, float("nan")):
+            t, d = st.clone(), sd.clone()
+            for x in (y for y, z in ((t, st), (d, sd)) if any(z is s for s in sides)):
+                for row in range(len(x)):
+                    chunk = int(x[row, :, 0].argmin())
+                    x[row, chunk, 1] = weight
+            results.append(rapid().rapid_accept(zt, zd, tokens, eta, u, target_stats=t, draft_stats=d))
+        for a, b in zip(*results):
+            assert torch.equal(a, b) and torch.isfinite(a.double()).all()
